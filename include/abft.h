@@ -222,6 +222,57 @@ int abft_gemm_bias(abft_ctx *ctx, const void *A, const void *B, const void *bias
 int abft_gemm_static(const void *A, const void *B, void *C, abft_dtype dtype, int mode,
                      const abft_shape *s, const abft_result *r, void *stream);
 
+/* ---- Quantised layers and mixtures of experts ---------------------------------------------------------- */
+
+/* Rows to int8 (the tokens ahead of a quantised layer).  X: rows x cols of ABFT_BF16 or ABFT_F16, rows ldx apart; Q: int8, rows ldq
+ * apart; scale: DEVICE, [rows] float.  For each row scale = max|x| / 127 (rounded to fp32) and
+ * q = 127 x / max|x| rounded to the nearest integer, ties to even, as exact arithmetic gives it; a row of zeros gets scale 0 and zeros, a row
+ * that holds an Inf or a NaN scale NaN and zeros.  X and Q as the matrices above (16 bytes); what lies between cols and ldq stays as it
+ * is.  Needs no context; the current device's. */
+int abft_quantize_rows(const void *X, abft_dtype dtype, int64_t rows, int64_t cols, int64_t ldx, void *Q,
+                       int64_t ldq, float *scale, void *stream);
+
+/* Scales of an int8 product, all DEVICE: C[i][j] = (A B)[i][j] * row[i] * col[j] + bias[j], each step
+ * rounded to fp32 (the last product and sum together), the result once more to C's type. */
+typedef struct {
+    const float *row;    /* [M]: of the rows of A (tokens); NULL: ones */
+    const float *col;    /* [batch][N]: of the columns of B (channels), of each group's; NULL: ones */
+    const float *bias;   /* [N], shared by all groups; NULL: none */
+    int32_t out;         /* type of C: ABFT_BF16 or ABFT_F16 */
+    int32_t reserved;    /* 0 */
+} abft_scales;
+
+/* The quantised layer: int8 A (M x K) and B, C in the type scales->out (ldc in its elements).  mode: ABFT_OFF or ABFT_DETECT, which may
+ * be OR-ed with ABFT_B_CHECKSUM_CACHED (others: ABFT_EINVAL).  What is checked are the int32 sums ahead of the scales, by
+ * equality as in abft_gemm, so every single fault of the product shows whatever the scales are; faults behind the sums (scales, rounding,
+ * C in memory) do not.  batch must be 1 (ABFT_ESHAPE); K may exceed 4096, K * 2^14 < 2^31.
+ * abft_verify, abft_correct and abft_discrepancy have nothing to go by behind this call (ABFT_ESTATE). */
+int abft_gemm_scaled(abft_ctx *ctx, const void *A, const void *B, const abft_scales *scales, void *C, int mode,
+                     const abft_shape *s, const abft_result *r, void *stream);
+
+/* Products grouped by expert: the rows of A and C are sorted by group; group e (of s->batch) has rows offsets[e] ..
+ * offsets[e+1] of them and its own B, at B + e * strideB.  s->M: rows of A and C over all groups (strideA and strideC are
+ * not looked at).  offsets: DEVICE, [batch + 1] int32, not falling, within [0, M]; the host never reads them, so they may come from a router's
+ * kernel on the same stream.  Groups may have no rows; rows ahead of offsets[0] and behind offsets[batch] belong to none and their C is left
+ * as it was.  (Offsets that fall or point outside [0, M] address nothing outside A and C; what is then written to rows
+ * of C, and flagged, is unspecified.)
+ * scales: NULL: C as in abft_gemm (int32 for ABFT_I8); ABFT_I8 with scales: as in abft_gemm_scaled.
+ * mode, K and what may follow the call: as in abft_gemm_scaled.  ABFT_DETECT: row_flag [M] (0 for rows of no group), col_flag [batch][N]; the
+ * checksums, max|A|, max|B| and with them the tolerance are a group's own.  abft_encode_b with this shape encodes the B of all groups.
+ * abft_workspace has no vectors of this call.  The context serves s->M <= max_rows, batch * N <= max_cols,
+ * batch * (K rounded up to 128) <= max_depth, batch <= max_batch.
+ * The backward pass with respect to A is this call again: dA = dC B^T, that is, A := dC, B as it lies with transB
+ * inverted, and N and K exchanged. */
+int abft_gemm_grouped(abft_ctx *ctx, const void *A, const void *B, const int32_t *offsets, const abft_scales *scales,
+                      void *C, abft_dtype dtype, int mode, const abft_shape *s, const abft_result *r, void *stream);
+
+/* Its backward pass with respect to B: for each group the sum over its rows of the products of dY and X,
+ * dW[e] = dY_e^T X_e (N x K, transB = 1) or X_e^T dY_e (K x N, transB = 0), as B lies in memory.  s: the shape of the
+ * forward call: X is its A (lda), dY has the layout of its C (ldc, elements of dtype), dW that of its B (ldb, strideB, which must keep the
+ * groups apart: ABFT_ESHAPE).  ABFT_BF16 or ABFT_F16, sums in fp32, rounded once.  A group without rows gets zeros.  Unprotected. */
+int abft_gemm_grouped_wgrad(abft_ctx *ctx, const void *X, const void *dY, const int32_t *offsets, void *dW,
+                            abft_dtype dtype, const abft_shape *s, void *stream);
+
 /* Producer-side input checksum for the next abft_gemm / abft_gemm_bias on this context called with
  * ABFT_A_CHECKSUM_GIVEN (Sec. V "Optimizations" (2): the checksum is generated while the tensor is
  * produced, so the consumer does not form it again).  a: DEVICE, [batch][K] words (float for

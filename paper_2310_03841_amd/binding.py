@@ -20,7 +20,8 @@ __all__ = [
     "ABFT_INJECT_STORED_C", "ABFT_INJECT_ACCUMULATOR", "ABFT_INJECT_OPERAND_A", "ABFT_INJECT_OPERAND_B",
     "ABFT_WS_A_SUM", "ABFT_WS_B_SUM", "ABFT_WS_CC_PRED", "ABFT_WS_RC_PRED", "ABFT_WS_CC_OBS",
     "ABFT_WS_RC_OBS", "ABFT_WS_CC_VOBS", "ABFT_WS_RC_VOBS", "ABFT_WS_TAU", "ABFT_WS_S_PRED", "ABFT_WS_MAXABS", "ABFT_WS_CC_STO", "ABFT_WS_RC_STO",
-    "abft_shape", "abft_config", "abft_result", "AbftError", "lib", "lib_path", "exported_symbols",
+    "abft_shape", "abft_config", "abft_result", "abft_scales", "make_scales",
+    "abft_gemm_scaled", "abft_gemm_grouped", "abft_gemm_grouped_wgrad", "abft_quantize_rows", "AbftError", "lib", "lib_path", "exported_symbols",
     "abft_create", "abft_destroy", "abft_encode_b", "abft_gemm", "abft_gemm_bias", "abft_gemm_static", "abft_verify", "abft_correct",
     "abft_correct_checksum", "abft_inject", "abft_discrepancy", "abft_workspace", "abft_tile_shape", "abft_strerror", "abft_last_hip_error",
     "abft_version", "abft_mfma_peak", "abft_profile_begin", "abft_profile_end", "make_shape", "make_result", "DTYPE_CODE",
@@ -60,6 +61,11 @@ class abft_result(ctypes.Structure):
                 ("tau", ctypes.c_float), ("tau_cols", ctypes.c_float)]
 
 
+class abft_scales(ctypes.Structure):
+    _fields_ = [("row", ctypes.c_void_p), ("col", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("out", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 class AbftError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -80,6 +86,17 @@ _SIGS = {
     "abft_gemm_static": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                                         ctypes.c_int, ctypes.c_int, ctypes.POINTER(abft_shape),
                                         ctypes.POINTER(abft_result), ctypes.c_void_p]),
+    "abft_gemm_scaled": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(abft_scales),
+                                        ctypes.c_void_p, ctypes.c_int, ctypes.POINTER(abft_shape),
+                                        ctypes.POINTER(abft_result), ctypes.c_void_p]),
+    "abft_gemm_grouped": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                         ctypes.POINTER(abft_scales), ctypes.c_void_p, ctypes.c_int, ctypes.c_int,
+                                         ctypes.POINTER(abft_shape), ctypes.POINTER(abft_result), ctypes.c_void_p]),
+    "abft_gemm_grouped_wgrad": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                               ctypes.c_void_p, ctypes.c_int, ctypes.POINTER(abft_shape),
+                                               ctypes.c_void_p]),
+    "abft_quantize_rows": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64,
+                                          ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p]),
     "abft_supply_a": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
     "abft_gemm_done_event": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
     "abft_verify": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.POINTER(abft_shape),
@@ -193,6 +210,10 @@ def make_result(row_flag, col_flag, counts, tau: float = 0.0, tau_cols: float = 
     return abft_result(_ptr(row_flag), _ptr(col_flag), _ptr(counts), float(tau), float(tau_cols))
 
 
+def make_scales(row=None, col=None, bias=None, out: int = ABFT_BF16) -> abft_scales:
+    return abft_scales(_ptr(row), _ptr(col), _ptr(bias), int(out), 0)
+
+
 def abft_strerror(code: int) -> str:
     return lib().abft_strerror(int(code)).decode()
 
@@ -241,6 +262,30 @@ def abft_gemm_static(A, B, C, dtype: int, mode: int, shape: abft_shape, result: 
     r = ctypes.byref(result) if result is not None else None
     return int(lib().abft_gemm_static(_ptr(A), _ptr(B), _ptr(C), dtype, mode, ctypes.byref(shape), r,
                                       _stream(stream)))
+
+
+def abft_gemm_scaled(ctx, A, B, scales: abft_scales, C, mode: int, shape: abft_shape, result: abft_result | None = None,
+                     stream=None) -> int:
+    r = ctypes.byref(result) if result is not None else None
+    q = ctypes.byref(scales) if scales is not None else None
+    return int(lib().abft_gemm_scaled(ctx, _ptr(A), _ptr(B), q, _ptr(C), mode, ctypes.byref(shape), r, _stream(stream)))
+
+
+def abft_gemm_grouped(ctx, A, B, offsets, scales: abft_scales | None, C, dtype: int, mode: int, shape: abft_shape,
+                      result: abft_result | None = None, stream=None) -> int:
+    r = ctypes.byref(result) if result is not None else None
+    q = ctypes.byref(scales) if scales is not None else None
+    return int(lib().abft_gemm_grouped(ctx, _ptr(A), _ptr(B), _ptr(offsets), q, _ptr(C), dtype, mode, ctypes.byref(shape), r,
+                                       _stream(stream)))
+
+
+def abft_gemm_grouped_wgrad(ctx, X, dY, offsets, dW, dtype: int, shape: abft_shape, stream=None) -> int:
+    return int(lib().abft_gemm_grouped_wgrad(ctx, _ptr(X), _ptr(dY), _ptr(offsets), _ptr(dW), dtype, ctypes.byref(shape),
+                                             _stream(stream)))
+
+
+def abft_quantize_rows(X, dtype: int, rows: int, cols: int, ldx: int, Q, ldq: int, scale, stream=None) -> int:
+    return int(lib().abft_quantize_rows(_ptr(X), dtype, rows, cols, ldx, _ptr(Q), ldq, _ptr(scale), _stream(stream)))
 
 
 def abft_gemm_done_event(ctx, event) -> int:

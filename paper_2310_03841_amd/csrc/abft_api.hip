@@ -8,6 +8,7 @@
 
 #include "../../include/abft.h"
 #include "abft_internal.h"
+#include "group_args.h"
 
 using namespace abft;
 
@@ -202,7 +203,8 @@ static int check_shape(const abft_ctx *c, int dt, const abft_shape *s, int need,
         if ((need & 4) && (s->strideC < s->M * s->ldc || (s->strideC * os) % 16)) return ABFT_EALIGN;
     }
     const int64_t Kp = round_up(s->K, SLAB_BYTES / es);
-    if (s->batch * s->M > c->cfg.max_rows || s->batch * s->N > c->cfg.max_cols ||
+    // (a call on B alone keeps nothing for the rows of A, which groups share out among them)
+    if ((need != 2 && s->batch * s->M > c->cfg.max_rows) || s->batch * s->N > c->cfg.max_cols ||
         s->batch * Kp > c->cfg.max_depth || s->batch > c->cfg.max_batch)
         return ABFT_EWORKSPACE;
     o->M = (int)s->M; o->N = (int)s->N; o->K = (int)s->K; o->batch = (int)s->batch; o->transB = s->transB;
@@ -214,9 +216,10 @@ static int check_shape(const abft_ctx *c, int dt, const abft_shape *s, int need,
     return ABFT_OK;
 }
 
-static void carve(const abft_ctx *c, int dt, const Shape &s, Workspace *w)
+// bM: rows over all batch items
+static void carve_rows(const abft_ctx *c, int dt, const Shape &s, size_t bM, Workspace *w)
 {
-    const size_t bK = (size_t)s.batch * s.K, bM = (size_t)s.batch * s.M, bN = (size_t)s.batch * s.N;
+    const size_t bK = (size_t)s.batch * s.K, bN = (size_t)s.batch * s.N;
     const size_t D = (size_t)c->cfg.max_depth, Bt = (size_t)c->cfg.max_batch;
     w->b_sum = c->pool_depth + (size_t)c->bslot * c->bslot_words;
     w->b_max = w->b_sum + D;
@@ -253,6 +256,8 @@ static void carve(const abft_ctx *c, int dt, const Shape &s, Workspace *w)
     w->bias = nullptr;
     w->a_given = w->amax_given = nullptr;
 }
+
+static void carve(const abft_ctx *c, int dt, const Shape &s, Workspace *w) { carve_rows(c, dt, s, (size_t)s.batch * s.M, w); }
 
 static bool same_b(const abft_shape &x, const abft_shape &y)
 {
@@ -662,6 +667,185 @@ extern "C" int abft_gemm_static(const void *A, const void *B, void *C, abft_dtyp
         }
     }
     return abft_gemm(ctx, A, B, C, dtype, mode, s, r, stream);
+}
+
+// ------------------------------------------------------------------------------------------
+// Products over groups of rows, with scales or without.
+
+// M: rows over all groups; batch: groups.  os: bytes of an element of C.
+static int check_group_shape(const abft_ctx *c, int dt, int os, const abft_shape *s, Shape *o)
+{
+    if (!c || !s) return ABFT_EINVAL;
+    if (s->M < 1 || s->N < 1 || s->K < 1 || s->batch < 1) return ABFT_ESHAPE;
+    if (s->M > (1 << 30) || s->N > (1 << 30) || s->K > (1 << 30) || s->batch > 65535) return ABFT_ESHAPE;
+    if (s->transB != 0 && s->transB != 1) return ABFT_EINVAL;
+    const int es = elem_size(dt);
+    if (dt == ABFT_I8 && s->K >= (1 << 17)) return ABFT_ESHAPE;       // K * 2^14 must stay below 2^31
+    if (s->lda < s->K || s->ldb < (s->transB ? s->K : s->N) || s->ldc < s->N) return ABFT_ESHAPE;
+    if ((s->lda * es) % 16 || (s->ldb * es) % 16 || (s->ldc * os) % 16) return ABFT_EALIGN;
+    if (s->batch > 1 && (s->strideB < 0 || (s->strideB * es) % 16)) return ABFT_EALIGN;
+    const int64_t Kp = round_up(s->K, SLAB_BYTES / es);
+    if (s->M > c->cfg.max_rows || s->batch * s->N > c->cfg.max_cols || s->batch * Kp > c->cfg.max_depth ||
+        s->batch > c->cfg.max_batch)
+        return ABFT_EWORKSPACE;
+    o->M = (int)s->M; o->N = (int)s->N; o->K = (int)s->K; o->batch = (int)s->batch; o->transB = s->transB;
+    o->lda = s->lda; o->ldb = s->ldb; o->ldc = s->ldc;
+    o->sA = o->sC = 0;
+    o->sB = s->batch > 1 ? s->strideB : 0;
+    o->Kp = (int)Kp;
+    return ABFT_OK;
+}
+
+static GroupArgs group_args(const void *A, const void *B, void *C, const int32_t *offsets, const Shape &sh)
+{
+    GroupArgs g;
+    memset(&g, 0, sizeof(g));
+    g.A = (const uint8_t *)A; g.B = (const uint8_t *)B; g.C = (uint8_t *)C;
+    g.offsets = offsets;
+    g.M = sh.M; g.N = sh.N; g.K = sh.K; g.groups = sh.batch;
+    g.lda = sh.lda; g.ldb = sh.ldb; g.ldc = sh.ldc; g.sB = sh.sB;
+    g.inj_b = -1;
+    return g;
+}
+
+// The kernels of a protected call: the pass over the matrices (unless their encoding is cached), the product, whose launch also passes
+// over A, and the check.  The regions it accumulates into alternate as those of enqueue_tiled.
+static int enqueue_group(abft_ctx *ctx, int dtype, int ot, bool cached, GroupArgs &g, const void *B, const Shape &sh, const Verdict &v,
+                         hipStream_t st)
+{
+    const bool gm = in_graph_mode(ctx, st);
+    const int prev = ctx->cur;
+    if (!gm) ctx->cur ^= 1;
+    if (!cached) {
+        int rc = begin_b_pass(ctx, st);
+        if (rc) return rc;
+    }
+    Workspace w;
+    carve_rows(ctx, dtype, sh, (size_t)sh.M, &w);
+    w.zero_words = (size_t)(reinterpret_cast<uint32_t *>(w.rc_acc + sh.M) - w.cc_obs);
+    g.cc_obs = w.cc_obs; g.rc_obs = w.rc_obs; g.rc_pred = w.rc_pred; g.a_sum = w.a_sum; g.a_max = w.a_max; g.b_sum = w.b_sum;
+    g.cc_acc = w.cc_acc;
+    g.rc_acc = w.rc_acc;
+    g.counts = v.counts;
+    size_t stale = ctx->dirty[ctx->cur];
+    if (gm && stale < w.zero_words) stale = w.zero_words;
+    ctx->dirty[ctx->cur] = ctx->region_words;            // until everything below is enqueued
+    OneLaunch end = {v, nullptr, nullptr, 0, 0};
+    if (!gm) {
+        const int other = ctx->bslot ^ 1;
+        end.zero_ptr = ctx->pool_obs + (size_t)prev * ctx->region_words;
+        end.zero_words = ctx->dirty[prev];
+        ctx->dirty[prev] = ctx->region_words;
+        if (!ctx->bclean[other]) {
+            end.zero2_ptr = ctx->pool_depth + (size_t)other * ctx->bslot_words;
+            end.zero2_words = ctx->bslot_words;
+        }
+    }
+    if (!cached) HIP_TRY(launch_encode_b(dtype, B, sh, w, w.cc_obs, stale, st));
+    else if (stale) HIP_TRY(launch_zero(w.cc_obs, stale, st));
+    ctx->sto_valid = false;
+    HIP_TRY(launch_group(dtype, ot, true, sh.transB != 0, g, st));
+    if (ctx->done_event && !gm) HIP_TRY(hipEventRecord(ctx->done_event, st));
+    HIP_TRY(launch_group_check(dtype, g, sh.transB != 0, w, v, end, st));
+    if (!gm) {
+        ctx->bclean[ctx->bslot ^ 1] = true;
+        ctx->dirty[prev] = 0;
+    }
+    ctx->dirty[ctx->cur] = w.zero_words;
+    return ABFT_OK;
+}
+
+// offsets: null, one group of all rows
+static int group_impl(abft_ctx *ctx, const void *A, const void *B, const int32_t *offsets, const abft_scales *q, void *C, int dtype, int mode,
+                      const abft_shape *s, const abft_result *r, hipStream_t st)
+{
+    const int base = mode & ABFT_MODE_MASK;
+    if (base != ABFT_OFF && base != ABFT_DETECT) return ABFT_EINVAL;
+    if (mode & ~(ABFT_MODE_MASK | ABFT_B_CHECKSUM_CACHED)) return ABFT_EINVAL;
+    if (dtype != ABFT_I8 && dtype != ABFT_BF16 && dtype != ABFT_F16) return ABFT_EINVAL;
+    int ot = dtype;
+    if (q) {
+        if (dtype != ABFT_I8 || (q->out != ABFT_BF16 && q->out != ABFT_F16) || q->reserved) return ABFT_EINVAL;
+        if (((uintptr_t)q->row & 3u) || ((uintptr_t)q->col & 3u) || ((uintptr_t)q->bias & 3u)) return ABFT_EALIGN;
+        ot = q->out;
+    }
+    Shape sh;
+    int rc = check_group_shape(ctx, dtype, out_size(ot), s, &sh);
+    if (rc) return rc;
+    if (!A || !B || !C) return ABFT_EINVAL;
+    if (!aligned16(A) || !aligned16(B) || !aligned16(C) || ((uintptr_t)offsets & 3u)) return ABFT_EALIGN;
+    const InjectArm arm = ctx->arm;
+    if (arm.batch >= 0 && (arm.batch >= sh.batch || arm.row >= sh.M || arm.col >= sh.N)) return ABFT_EINVAL;
+    GroupArgs g = group_args(A, B, C, offsets, sh);
+    g.inj_b = arm.batch; g.inj_row = arm.row; g.inj_col = arm.col; g.inj_bit = arm.bit;
+    if (q) { g.row_scale = q->row; g.col_scale = q->col; g.bias = q->bias; }
+    if (base == ABFT_OFF) {
+        ctx->arm.batch = -1;
+        HIP_TRY(launch_group(dtype, ot, false, sh.transB != 0, g, st));
+        if (ctx->done_event && !capturing(st)) HIP_TRY(hipEventRecord(ctx->done_event, st));
+        return ABFT_OK;
+    }
+    Verdict v;
+    rc = check_verdict(r, &v);
+    if (rc) return rc;
+    const bool cached = (mode & ABFT_B_CHECKSUM_CACHED) != 0;
+    if (cached && !(ctx->b_valid && ctx->b_dt == dtype && same_b(ctx->b_shape, *s))) return ABFT_ESTATE;
+    ctx->pred_valid = false;
+    ctx->vobs_valid = false;
+    if (!cached) ctx->b_valid = false;
+    ctx->arm.batch = -1;
+    rc = enqueue_group(ctx, dtype, ot, cached, g, B, sh, v, st);
+    if (rc) return rc;
+    ctx->b_valid = true;
+    ctx->b_dt = dtype;
+    ctx->b_shape = *s;
+    return ABFT_OK;
+}
+
+extern "C" int abft_gemm_scaled(abft_ctx *ctx, const void *A, const void *B, const abft_scales *scales, void *C, int mode,
+                                const abft_shape *s, const abft_result *r, void *stream)
+{
+    if (!scales || !s) return ABFT_EINVAL;
+    if (s->batch != 1) return ABFT_ESHAPE;
+    return group_impl(ctx, A, B, nullptr, scales, C, ABFT_I8, mode, s, r, (hipStream_t)stream);
+}
+
+extern "C" int abft_gemm_grouped(abft_ctx *ctx, const void *A, const void *B, const int32_t *offsets, const abft_scales *scales, void *C,
+                                 abft_dtype dtype, int mode, const abft_shape *s, const abft_result *r, void *stream)
+{
+    if (!offsets) return ABFT_EINVAL;
+    return group_impl(ctx, A, B, offsets, scales, C, dtype, mode, s, r, (hipStream_t)stream);
+}
+
+extern "C" int abft_gemm_grouped_wgrad(abft_ctx *ctx, const void *X, const void *dY, const int32_t *offsets, void *dW, abft_dtype dtype,
+                                       const abft_shape *s, void *stream)
+{
+    if (dtype != ABFT_BF16 && dtype != ABFT_F16) return ABFT_EINVAL;
+    Shape sh;
+    int rc = check_group_shape(ctx, dtype, elem_size(dtype), s, &sh);
+    if (rc) return rc;
+    if (!X || !dY || !offsets || !dW) return ABFT_EINVAL;
+    if (!aligned16(X) || !aligned16(dY) || !aligned16(dW) || ((uintptr_t)offsets & 3u)) return ABFT_EALIGN;
+    if (sh.batch > 1 && sh.sB < (sh.transB ? sh.N : sh.K) * sh.ldb) return ABFT_ESHAPE;     // gradients that overlap
+    // the product's rows and columns: N x K as the weights lie, or K x N
+    GroupArgs g = group_args(sh.transB ? dY : X, sh.transB ? X : dY, dW, offsets, sh);
+    g.lda = sh.transB ? sh.ldc : sh.lda;
+    g.ldb = sh.transB ? sh.lda : sh.ldc;
+    g.ldc = sh.ldb;
+    g.K = sh.transB ? sh.N : sh.K;
+    g.N = sh.transB ? sh.K : sh.N;
+    HIP_TRY(launch_group_wgrad(dtype, g, (hipStream_t)stream));
+    return ABFT_OK;
+}
+
+extern "C" int abft_quantize_rows(const void *X, abft_dtype dtype, int64_t rows, int64_t cols, int64_t ldx, void *Q, int64_t ldq, float *scale,
+                                  void *stream)
+{
+    if (dtype != ABFT_BF16 && dtype != ABFT_F16) return ABFT_EINVAL;
+    if (rows < 1 || cols < 1 || rows > (1 << 30) || cols > (1 << 30) || ldx < cols || ldq < cols) return ABFT_ESHAPE;
+    if (!X || !Q || !scale) return ABFT_EINVAL;
+    if (!aligned16(X) || !aligned16(Q) || (ldx * 2) % 16 || ldq % 16 || ((uintptr_t)scale & 3u)) return ABFT_EALIGN;
+    return launch_quantize_rows(dtype, X, (int)rows, (int)cols, ldx, Q, ldq, scale, (hipStream_t)stream) == hipSuccess ? ABFT_OK : ABFT_EHIP;
 }
 
 extern "C" int abft_gemm_done_event(abft_ctx *ctx, void *event)

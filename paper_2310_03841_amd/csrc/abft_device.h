@@ -374,4 +374,11 @@ __device__ __forceinline__ i32x4 mask_chunk(i32x4 v, int nbytes)
     return v;
 }
 
+// Swizzle of B stored K x N: 16-byte slot of a row of k <-> chunk of columns.  ROWB: bytes per row.
+template <int ES, int ROWB> __device__ __forceinline__ int kn_swizzle(int k)
+{
+    if constexpr (ES == 2) return ROWB == 128 ? ((k >> 1) & 1) << 2 : (k & 3) << 2;      // 32-byte pieces of 4 rows
+    else return ROWB == 64 ? ((k >> 2) & 1) << 1 : ((k >> 1) & 3) << 1;                  // 16-byte pieces of 8 rows
+}
+
 }  // namespace abft

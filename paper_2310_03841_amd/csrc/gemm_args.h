@@ -41,10 +41,9 @@ struct GemmArgs {
 // has none, took 830 of the 3200 clocks before a tile's first load.)
 constexpr int GROUP_M = 4;              // measured against 2, 3, 6, 8, 16: best or equal on every Linear shape
 inline uint32_t map_inverse(int tiles_n) { return (uint32_t)((1ull << 32) / ((uint64_t)GROUP_M * tiles_n)); }
-__device__ __forceinline__ void map_tile(int bid, int nb, int tiles_m, int tiles_n, uint32_t group_inv, int *tm, int *tn)
+// Tile L of a region in that order.
+__device__ __forceinline__ void tile_at(int L, int tiles_m, int tiles_n, uint32_t group_inv, int *tm, int *tn)
 {
-    const int q = nb >> 3, r = nb & 7, xcd = bid & 7;
-    const int L = xcd * q + (xcd < r ? xcd : r) + (bid >> 3);
     const int per_group = GROUP_M * tiles_n;
     int grp = (int)__umulhi((uint32_t)L, group_inv), in_grp = L - grp * per_group;
     if (in_grp >= per_group) { ++grp; in_grp -= per_group; }
@@ -53,6 +52,11 @@ __device__ __forceinline__ void map_tile(int bid, int nb, int tiles_m, int tiles
     const int col = gsz >= 4 ? in_grp >> 2 : gsz == 3 ? (int)__umulhi((uint32_t)in_grp, 0x55555556u) : gsz == 2 ? in_grp >> 1 : in_grp;
     *tm = first_m + in_grp - col * (gsz < GROUP_M ? gsz : GROUP_M);
     *tn = col;
+}
+__device__ __forceinline__ void map_tile(int bid, int nb, int tiles_m, int tiles_n, uint32_t group_inv, int *tm, int *tn)
+{
+    const int q = nb >> 3, r = nb & 7, xcd = bid & 7;
+    tile_at(xcd * q + (xcd < r ? xcd : r) + (bid >> 3), tiles_m, tiles_n, group_inv, tm, tn);
 }
 
 // Fast path (gemm_fast.hip): B stored N x K, K a whole number of 128-byte slabs.

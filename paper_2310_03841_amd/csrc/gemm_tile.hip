@@ -89,13 +89,6 @@ __host__ __device__ constexpr int tile_lds_bytes(int BM, int BN, int ns)
     return loop > epi ? loop : epi;
 }
 
-// Swizzle of B stored K x N: 16-byte slot of a row of k <-> chunk of columns.  ROWB: bytes per row.
-template <int ES, int ROWB> __device__ __forceinline__ int kn_swizzle(int k)
-{
-    if constexpr (ES == 2) return ROWB == 128 ? ((k >> 1) & 1) << 2 : (k & 3) << 2;      // 32-byte pieces of 4 rows
-    else return ROWB == 64 ? ((k >> 2) & 1) << 1 : ((k >> 1) & 3) << 1;                  // 16-byte pieces of 8 rows
-}
-
 // ONE: the whole protected call (predict_pass.h)
 template <int DT, int BM, int BN, int NS, bool PROT, bool TRANSB, bool APASS, bool ONE>
 __global__ __launch_bounds__(256) void gemm_tile_kernel(typename KernelArgs<PROT, ONE>::type whole)

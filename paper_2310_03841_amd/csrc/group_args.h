@@ -1,0 +1,122 @@
+// Products over groups of rows: what their kernels share.  The rows of A and C are sorted by group; group e has the rows
+// offsets[e] .. offsets[e + 1] and a matrix B of its own.  The offsets lie in device memory, so the host knows only how many rows and
+// groups there are; it launches as many workgroups as any split of the rows needs, and each finds its tile.
+#pragma once
+#include "abft_device.h"
+#include "gemm_args.h"
+
+namespace abft {
+
+struct GroupArgs {
+    const uint8_t *A, *B;
+    uint8_t *C;
+    const int *offsets;                   // [groups + 1]; null: one group of all rows
+    int M, N, K, groups;                  // M: rows over all groups (of a gradient of weights: the depth)
+    long lda, ldb, ldc, sB;               // elements
+    int tiles_n;
+    uint32_t group_inv;                   // map_inverse(tiles_n)
+    int inj_b, inj_row, inj_col, inj_bit; // armed accumulator flip (inj_b < 0: none); the row counts from its group's first
+    const float *row_scale, *col_scale;   // [M], [groups][N], or null
+    const float *bias;                    // [N], or null; behind the scales
+    // protected: sums start at zero and are added to with atomics
+    uint32_t *cc_obs, *rc_obs;            // observed sums of C  [groups][N], [M]: integers
+    double *cc_acc, *rc_acc;              // floating point: the same in doubles, whose rounding hides the order of additions
+    uint32_t *rc_pred;                    // A b of each row's group  [M]
+    uint32_t *a_sum, *a_max;              // e^T A and max|A| of a group's rows  [groups][K], [groups]
+    const uint32_t *b_sum;                // B e of each group  [groups][K]
+    uint32_t *counts;                     // cleared for the check kernel
+    int n_pass, pass_rows, pass_win;      // workgroups ahead of the tiles that pass over A; rows to a wave; windows along K
+};
+
+// The rows of group e: whatever the offsets hold, inside [0, M].
+__device__ __forceinline__ void group_rows(const int *offsets, int M, int e, int *first, int *rows)
+{
+    if (!offsets) { *first = 0; *rows = M; return; }
+    int a = offsets[e], b = offsets[e + 1];
+    a = a < 0 ? 0 : a > M ? M : a;
+    b = b < a ? a : b > M ? M : b;
+    *first = a;
+    *rows = b - a;
+}
+
+// The group that row r belongs to, -1: none.  By halving: of the groups that start at or ahead of r, the last.
+__device__ __forceinline__ int group_of(const int *offsets, int M, int groups, int r, int *end)
+{
+    if (!offsets) { *end = M; return 0; }
+    int lo = 0, hi = groups;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (offsets[mid] <= r) lo = mid;
+        else hi = mid;
+    }
+    int first, rows;
+    group_rows(offsets, M, lo, &first, &rows);
+    *end = first + rows;
+    return r >= first && r < first + rows ? lo : -1;
+}
+
+// Sum over the lanes up to and with this one.
+__device__ __forceinline__ int wave_prefix(int v, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int up = __shfl_up(v, d);
+        if (lane >= d) v += up;
+    }
+    return v;
+}
+
+struct GroupTile { int e, tm, tn, first, rows; };
+
+// The tile of workgroup `bid` of those that take tiles, of BM rows each: false, there is none for it.  Every wave finds it by itself, 64 groups at
+// a time.  Consecutive tiles of an XCD are a group's, in the order of map_tile, so what shares rows of A or B meets in one L2.
+template <int BM> __device__ __forceinline__ bool find_tile(const GroupArgs &g, int bid, GroupTile *t)
+{
+    const int lane = threadIdx.x & 63, tiles_n = g.tiles_n;
+    auto tiles_of = [&](int e) __attribute__((always_inline)) {
+        int first = 0, rows = 0;
+        if (e < g.groups) group_rows(g.offsets, g.M, e, &first, &rows);
+        return (rows + BM - 1) / BM * tiles_n;
+    };
+    auto at = [&](int nb) __attribute__((always_inline)) {                 // -1: more workgroups than tiles
+        const int q = nb >> 3, r = nb & 7, xcd = bid & 7, i = bid >> 3;
+        return i < q + (xcd < r ? 1 : 0) ? xcd * q + (xcd < r ? xcd : r) + i : -1;
+    };
+    int L;
+    if (g.groups == 1) {
+        group_rows(g.offsets, g.M, 0, &t->first, &t->rows);
+        t->e = 0;
+        L = at((t->rows + BM - 1) / BM * tiles_n);
+        if (L < 0) return false;
+    } else {
+        int total = 0, mine = 0;
+        for (int e0 = 0; e0 < g.groups; e0 += 64) {
+            mine = tiles_of(e0 + lane);
+            total += wave_sum(mine);
+        }
+        L = at(__builtin_amdgcn_readfirstlane(total));
+        if (L < 0) return false;
+        int base = 0, e = -1;
+        for (int e0 = 0; e0 < g.groups; e0 += 64) {
+            if (g.groups > 64) mine = tiles_of(e0 + lane);
+            const int upto = base + wave_prefix(mine, lane);
+            const uint64_t behind = __ballot(upto > L);
+            if (behind) {
+                const int l = __builtin_ctzll(behind);
+                e = e0 + l;
+                L -= __builtin_amdgcn_readlane(upto - mine, l);
+                break;
+            }
+            base = __builtin_amdgcn_readlane(upto, 63);
+        }
+        if (e < 0) return false;
+        t->e = e;
+        group_rows(g.offsets, g.M, e, &t->first, &t->rows);
+        t->first = __builtin_amdgcn_readfirstlane(t->first);
+        t->rows = __builtin_amdgcn_readfirstlane(t->rows);
+    }
+    tile_at(L, (t->rows + BM - 1) / BM, tiles_n, g.group_inv, &t->tm, &t->tn);
+    return true;
+}
+
+}  // namespace abft
