@@ -10,8 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libabft.so")
-SOURCES = ["gemm_tile.hip", "gemm_fast.hip", "gemm_item_rows.hip", "gemm_item_cols.hip", "gemm_item.hip", "gemm_group.hip", "group_check.hip", "quantize.hip", "aux_kernels.hip", "abft_api.hip"]
-HEADERS = ["abft_internal.h", "abft_device.h", "gemm_args.h", "gemm_epilogue.h", "gemm_apass.h", "gemm_item.h", "block_out.h", "encode_pass.h", "predict_pass.h", "check_dots.h", "group_args.h", "group_passes.h", os.path.join("..", "..", "include", "abft.h")]
+SOURCES = ["gemm_tile.hip", "gemm_fast.hip", "gemm_item_rows.hip", "gemm_item_cols.hip", "gemm_item.hip", "gemm_group.hip", "gemm_group_big_i8.hip", "gemm_group_big_bf16.hip", "gemm_group_big_f16.hip", "gemm_group_big_wgrad.hip", "group_check.hip", "quantize.hip", "aux_kernels.hip", "abft_api.hip"]
+HEADERS = ["abft_internal.h", "abft_device.h", "gemm_args.h", "gemm_epilogue.h", "gemm_apass.h", "gemm_item.h", "block_out.h", "encode_pass.h", "predict_pass.h", "check_dots.h", "gemm_fast_tile.h", "group_args.h", "gemm_group_big.h", "group_passes.h", os.path.join("..", "..", "include", "abft.h")]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-munsafe-fp-atomics",
@@ -23,7 +23,7 @@ FLAGS = [
 
 # The fast GEMM kernels count their outstanding loads by hand and keep up to 128 accumulators per lane, two waves to a SIMD:
 # a register spilled to scratch memory inside them costs speed at best.  The build fails on one.
-NO_SPILL_SOURCES = ["gemm_fast.hip"]
+NO_SPILL_SOURCES = ["gemm_fast.hip", "gemm_group_big_i8.hip", "gemm_group_big_bf16.hip", "gemm_group_big_f16.hip", "gemm_group_big_wgrad.hip"]
 
 
 def _check_no_spills(remarks: str) -> None:
@@ -31,7 +31,7 @@ def _check_no_spills(remarks: str) -> None:
     for line in remarks.splitlines():
         if "Function Name:" in line:
             name = line.split("Function Name:")[1].split()[0]
-        elif "ScratchSize [bytes/lane]:" in line and name and "gemm_fast_kernel" in name:
+        elif "ScratchSize [bytes/lane]:" in line and name and ("gemm_fast_kernel" in name or "gemm_group_big_kernel" in name):
             size = int(line.split("ScratchSize [bytes/lane]:")[1].split()[0])
             if size != 0:
                 raise RuntimeError(f"{name} spills {size} bytes per lane to scratch memory")

@@ -100,6 +100,19 @@ template <int DT, int MI> struct EpiProt {
     float back;               // fp16: what undoes the scale of b's terms
 };
 
+// Where a tile's arguments come from: the launch's own (protected kernels read them anew where they need them).
+struct LaunchSource {
+    static constexpr bool LAYER_BIAS = true;             // a bias [N] that is part of the checked product
+    template <bool AGAIN> __device__ __forceinline__ const GemmArgs &get(const GemmArgs &tile) const
+    {
+        if constexpr (AGAIN) return kernel_args<GemmArgs>();
+        else return tile;
+    }
+};
+// Scales of int8 products (OT: a 16-bit type): thread t's, of row t and of column t of the tile, and the bias of that column.  Asked for ahead of the
+// tile's slabs, put into LDS behind them.
+struct EpiScale { float row, col, bias; };
+
 // Sums along K by matrix instructions that are not finite, formed again from memory.  A wave does it together, 16 bytes to a lane and
 // several loads on their way: with an Inf or NaN in an operand these are some of a tile's sums (its own row or column, and what
 // it reached through products with zeros) or, with one in B, the dots of all of a tile's rows.  A thread to a sum, a trip to memory for
@@ -217,17 +230,19 @@ __device__ __forceinline__ void stored_mfmas(typename Acc4<DT>::type &c, typenam
 #undef ABFT_STORED16
 }
 
-template <int DT, int BM, bool PROT, int STO, bool BIAS>
-__device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, typename Traits<DT>::accv_t (&acc)[BM / 64][2],
-                                              uint8_t *smem, int m0, int n0, int bz, const EpiProt<DT, BM / 64> &ep)
+// OT: type of C, that of the operands or, of int8 products with scales, a 16-bit one
+template <int DT, int OT, int BM, bool PROT, int STO, bool BIAS, typename SRC>
+__device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, SRC source, typename Traits<DT>::accv_t (&acc)[BM / 64][2],
+                                              uint8_t *smem, int m0, int n0, int bz, const EpiProt<DT, BM / 64> &ep, const EpiScale &sc)
 {
-    const GemmArgs &g = PROT ? kernel_args<GemmArgs>() : tile;
+    const GemmArgs &g = source.template get<PROT>(tile);
     using T = Traits<DT>;
+    constexpr bool SCALED = OT != DT;
     typedef typename T::acc_t acc_t;
     constexpr int BN = 256, THREADS = 64 * FAST_WAVES;
     constexpr int TM = BM / 2, TN = BN / 4;         // waves: two rows of four
     constexpr int MI = TM / 32, NI = TN / 32;
-    constexpr int OS = T::OS;
+    constexpr int OS = Traits<OT>::OS;
     constexpr int KE = SLAB_BYTES / T::ES;
     static_assert(TN == 64, "a lane to a column where a wave walks a row");
     constexpr bool AGPR = STO == STO_256;
@@ -255,6 +270,14 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, typenam
         for (int t = tid; t < BN; t += THREADS) bias_lds[t] = n0 + t < N ? from_word<acc_t>(g.bias[n0 + t]) : T::zero();
         __syncthreads();
     }
+    float *const scol = reinterpret_cast<float *>(amax_w + FAST_WAVES), *const sbias = scol + BN, *const srow = sbias + BN;
+    if constexpr (SCALED) {
+        if (tid < BN) { scol[tid] = sc.col; sbias[tid] = sc.bias; }
+        if (tid < BM) srow[tid] = sc.row;
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    // each step one rounding of fp32: the sum, times the row's scale, times the column's, the bias with it
+    auto scaled = [&](acc_t v, float row, float col, float b) __attribute__((always_inline)) { return __builtin_fmaf((float)v * row, col, b); };
     if (PROT && ep.owned > 0) {
         // what the pass over A's slabs left in registers (nothing in a tile that reduced no slab: where K has fewer slabs than the
         // tile row has tiles, that is most tiles)
@@ -383,6 +406,8 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, typenam
         if (cols_full && br + 32 <= M) {
             // ---- register path: one read of every accumulator serves the sums and the store
             acc_t rowsum = T::zero();
+            float rscale = 1.f;
+            if constexpr (SCALED) rscale = srow[wm * TM + mi * 32 + l32];
             static_for<0, NI>([&](auto ni_c) {
                 constexpr int ni = decltype(ni_c)::value;
                 static_for<0, 4>([&](auto q_c) {
@@ -405,7 +430,15 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, typenam
                         rowsum = add_t(rowsum, add_t(add_t(v0, v1), add_t(v2, v3)));
                     }
                     uint8_t *d = wbuf + l32 * CROW + (ni * 32 + 8 * q + 4 * lh) * OS;
-                    if constexpr (DT == DT_I8) {
+                    if constexpr (SCALED) {
+                        const int c = wn * TN + ni * 32 + 8 * q + 4 * lh;
+                        const i32x4 c4 = *reinterpret_cast<const i32x4 *>(scol + c), b4 = *reinterpret_cast<const i32x4 *>(sbias + c);
+                        auto f = [&](int e) __attribute__((always_inline)) { return __uint_as_float((uint32_t)e); };
+                        uint2 w;
+                        w.x = pack2<OT>(scaled(v0, rscale, f(c4[0]), f(b4[0])), scaled(v1, rscale, f(c4[1]), f(b4[1])));
+                        w.y = pack2<OT>(scaled(v2, rscale, f(c4[2]), f(b4[2])), scaled(v3, rscale, f(c4[3]), f(b4[3])));
+                        *reinterpret_cast<uint2 *>(d) = w;
+                    } else if constexpr (DT == DT_I8) {
                         *reinterpret_cast<i32x4 *>(d) = i32x4{(int)v0, (int)v1, (int)v2, (int)v3};
                     } else {
                         uint2 w;
@@ -462,7 +495,9 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, typenam
             for (int r = 0; r < nrow && gc < N; ++r) {
                 acc_t v = from_word<acc_t>(*reinterpret_cast<const uint32_t *>(wbuf + r * SROW + lane * 4));
                 if (has_bias) v = add_t(v, bias_lds[wn * TN + lane]);
-                T::store_c(Cb, (long)(br + r) * g.ldc + gc, v);
+                if constexpr (SCALED)
+                    Traits<OT>::store_c(Cb, (long)(br + r) * g.ldc + gc, scaled(v, srow[wm * TM + mi * 32 + r], scol[wn * TN + lane], sbias[wn * TN + lane]));
+                else T::store_c(Cb, (long)(br + r) * g.ldc + gc, v);
                 if (PROT) colacc = add_t(colacc, v);
                 if constexpr (STO) {
                     const float sv = stored_value<DT>((float)v);
@@ -533,7 +568,7 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, typenam
         // Barrier over LDS traffic only: the partial sums meet in LDS, and a full barrier would
         // also wait until every store of C issued above has been acknowledged.
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        const GemmArgs &g = kernel_args<GemmArgs>();
+        const GemmArgs &g = source.template get<true>(tile);
         const int M = g.M, N = g.N;
         uint32_t amax = 0u;
         if (!T::IS_INT && ep.owned > 0) {
@@ -604,13 +639,18 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, typenam
 
 // With and without a layer bias: two copies of the epilogue behind one uniform branch (a test per
 // group of four values inside one copy costs a branch per group).
-template <int DT, int BM, bool PROT, int STO>
-__device__ __forceinline__ void gemm_epilogue(const GemmArgs &g,
+template <int DT, int OT, int BM, bool PROT, int STO, typename SRC>
+__device__ __forceinline__ void gemm_epilogue(const GemmArgs &g, SRC source,
                                               typename Traits<DT>::accv_t (&acc)[BM / 64][2],
-                                              uint8_t *smem, int m0, int n0, int bz, const EpiProt<DT, BM / 64> &ep)
+                                              uint8_t *smem, int m0, int n0, int bz, const EpiProt<DT, BM / 64> &ep, const EpiScale &sc)
 {
-    if (g.bias != nullptr) gemm_epilogue_impl<DT, BM, PROT, STO, true>(g, acc, smem, m0, n0, bz, ep);
-    else gemm_epilogue_impl<DT, BM, PROT, STO, false>(g, acc, smem, m0, n0, bz, ep);
+    if constexpr (SRC::LAYER_BIAS) {
+        if (g.bias != nullptr) {
+            gemm_epilogue_impl<DT, OT, BM, PROT, STO, true>(g, source, acc, smem, m0, n0, bz, ep, sc);
+            return;
+        }
+    }
+    gemm_epilogue_impl<DT, OT, BM, PROT, STO, false>(g, source, acc, smem, m0, n0, bz, ep, sc);
 }
 
 }  // namespace abft

@@ -13,6 +13,7 @@
 
 #include "abft_device.h"
 #include "block_out.h"
+#include "gemm_group_big.h"
 #include "group_args.h"
 #include "group_passes.h"
 
@@ -446,6 +447,27 @@ template <int DT, int OT> static hipError_t launch_type(bool protect, bool trans
                                : launch_rows<DT, OT, 64, 64, 4>(protect, transB, g, st);
 }
 
+// The pass over A ahead of tiles that leave no room beside them.
+template <int DT> __global__ __launch_bounds__(256) void group_pass_kernel(GroupArgs g)
+{
+    fetch_args<GroupArgs>();
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    group_pass<DT>(g, (int)blockIdx.x * 4 + wave);
+}
+
+// Whether the tiles of gemm_group_big.h take a product of `rows` rows over `groups` groups: enough of them to fill the chip.
+static bool fills_chip(long rows, int groups, int N)
+{
+    return groups <= 256 && rows >= 128L * groups && ceil_div(rows, 256) * ceil_div(N, 256) >= 64;
+}
+static bool takes_big(int dt, bool transB, const GroupArgs &g)
+{
+    const int es = elem_size(dt), ke = SLAB_BYTES / es;
+    constexpr long ROW = 1L << 23, ALL = 1L << 31;               // 32-bit offsets: of a row inside a tile; of all rows of k
+    return g.K % ke == 0 && g.K >= 3 * ke && g.lda * es < ROW && (transB ? g.ldb * es < ROW : es == 2 && g.K * g.ldb * es < ALL) &&
+           fills_chip(g.M, g.groups, g.N);
+}
+
 hipError_t launch_group(int dt, int ot, bool protect, bool transB, GroupArgs &g, hipStream_t st)
 {
     if (protect) {
@@ -453,6 +475,24 @@ hipError_t launch_group(int dt, int ot, bool protect, bool transB, GroupArgs &g,
         g.pass_win = (int)ceil_div(chunks, 64);
         g.pass_rows = 4 * PASS_ROWS;
         g.n_pass = (int)ceil_div((long)g.pass_win * ceil_div(g.M, g.pass_rows), 4);
+    }
+    if (takes_big(dt, transB, g)) {
+        if (protect) {
+            if (dt != DT_I8) g.cc_acc = g.rc_acc = nullptr;      // these tiles add to the sums themselves
+            const dim3 grid((unsigned)g.n_pass);
+            switch (dt) {
+            case DT_I8:   hipLaunchKernelGGL(group_pass_kernel<DT_I8>, grid, dim3(256), 0, st, g); break;
+            case DT_BF16: hipLaunchKernelGGL(group_pass_kernel<DT_BF16>, grid, dim3(256), 0, st, g); break;
+            default:      hipLaunchKernelGGL(group_pass_kernel<DT_F16>, grid, dim3(256), 0, st, g); break;
+            }
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        switch (dt) {
+        case DT_I8:   return launch_group_big_i8(ot, protect, g, st);
+        case DT_BF16: return launch_group_big_bf16(protect, transB, g, st);
+        default:      return launch_group_big_f16(protect, transB, g, st);
+        }
     }
     if (dt == DT_I8)
         return ot == DT_I8   ? launch_type<DT_I8, DT_I8>(protect, transB, g, st)
@@ -463,6 +503,11 @@ hipError_t launch_group(int dt, int ot, bool protect, bool transB, GroupArgs &g,
 
 hipError_t launch_group_wgrad(int dt, GroupArgs &g, hipStream_t st)
 {
+    constexpr long ALL = 1L << 31;
+    // (a group's depth may be nearly all rows; of a slab more than there are, three at least, is asked for)
+    const long most = ((long)g.M + 4 * 64) * 2;
+    if (most * g.lda < ALL && most * g.ldb < ALL && ceil_div(g.K, 256) * ceil_div(g.N, 256) * g.groups >= 64 && g.groups <= 4096)
+        return launch_group_big_wgrad(dt, g, st);
     return dt == DT_BF16 ? launch_one<DT_BF16, DT_BF16, 128, 128, 3, false, GROUP_DEPTH, false>(g, st)
                          : launch_one<DT_F16, DT_F16, 128, 128, 3, false, GROUP_DEPTH, false>(g, st);
 }

@@ -1,0 +1,182 @@
+// Products over groups of rows that fill the chip: the tiles of the fast GEMM kernel (gemm_fast_tile.h) over the groups of group_args.h, and over
+// the depths of the groups for the gradient of their matrices.
+//
+// A group's rows are covered by tiles of 256, the last 128 of them, where no more are left over, by one of 128.  One workgroup to a compute unit walks
+// the list: the tiles of 256 first, a round of the machine at a time; what would be a last round of few of them is dealt out as twice as many of 128 rows
+// where that ends sooner (a tile of 128 rows takes 0.57 of the time of one of 256, protected 0.66); then the tiles of left-over rows.
+#pragma once
+#include "gemm_fast_tile.h"
+#include "group_args.h"
+
+namespace abft {
+
+enum { BIG_ROWS, BIG_DEPTH };
+
+// The arguments of one tile, formed where they are used: behind the main loop they are read again rather than held across it.
+template <int OT, int GROUP> struct GroupSource {
+    static constexpr bool LAYER_BIAS = false;            // (a bias of scaled products is outside the checked sums)
+    int e, first, rows;
+    template <bool AGAIN> __device__ __forceinline__ GemmArgs get(const GemmArgs &) const
+    {
+        const GroupArgs &a = kernel_args<GroupArgs>();
+        GemmArgs g = {};
+        g.C = a.C + (GROUP == BIG_DEPTH ? (long)e * a.sB : (long)first * a.ldc) * Traits<OT>::OS;
+        g.M = GROUP == BIG_DEPTH ? a.K : rows;
+        g.N = a.N;
+        g.ldc = a.ldc;
+        g.inj_b = a.inj_b == e ? 0 : -1;
+        g.inj_row = a.inj_row; g.inj_col = a.inj_col; g.inj_bit = a.inj_bit;
+        g.cc_obs = a.cc_obs + (long)e * a.N;
+        g.rc_obs = a.rc_obs + first;
+        g.a_given = 1;                                   // the pass over A is another kernel's
+        return g;
+    }
+    __device__ __forceinline__ EpiScale scales(int m0, int n0, int t, int M, int N) const
+    {
+        const GroupArgs &a = kernel_args<GroupArgs>();
+        const int r = first + (m0 + t < M ? m0 + t : M - 1), c = n0 + t < N ? n0 + t : N - 1;
+        EpiScale s = {1.f, 1.f, 0.f};
+        if (a.row_scale) s.row = a.row_scale[r];
+        if (a.col_scale) s.col = a.col_scale[(long)e * N + c];
+        if (a.bias) s.bias = a.bias[c];
+        return s;
+    }
+};
+
+struct BigTile { int e, first, rows, m0, tn; bool tall; };
+
+// Tile t of the list: false, there is none.
+template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const GroupArgs &g, int t, int wgs, BigTile *o)
+{
+    const int lane = threadIdx.x & 63, tiles_n = g.tiles_n;
+    // rows of tiles of 256, of 128, of a product of so many rows
+    auto tall_of = [&](int rows) __attribute__((always_inline)) { return (rows >> 8) + ((rows & 255) > 128); };
+    auto small_of = [&](int rows) __attribute__((always_inline)) { return ((rows & 255) + 127) >> 7 & 1; };
+    auto rows_of = [&](int e) __attribute__((always_inline)) {
+        int first = 0, rows = 0;
+        if (e < g.groups) group_rows(g.offsets, g.M, e, &first, &rows);
+        return rows;
+    };
+    int mine = 0, talls, smalls;                                 // rows of this lane's group; of tiles of all
+    if constexpr (GROUP == BIG_DEPTH) {
+        talls = tall_of(g.K) * g.groups;
+        smalls = small_of(g.K) * g.groups;
+    } else {
+        talls = smalls = 0;
+        for (int e0 = 0; e0 < g.groups; e0 += 64) {
+            mine = rows_of(e0 + lane);
+            talls += wave_sum(tall_of(mine));
+            smalls += wave_sum(small_of(mine));
+        }
+        talls = __builtin_amdgcn_readfirstlane(talls);
+        smalls = __builtin_amdgcn_readfirstlane(smalls);
+    }
+    const int nt = talls * tiles_n, ns = smalls * tiles_n, over = nt % wgs;
+    constexpr int HALF = PROT ? 66 : 57;                         // of 100
+    auto rounds = [&](int n) __attribute__((always_inline)) { return (n + wgs - 1) / wgs; };
+    const bool split = over > 0 && HALF * rounds(2 * over + ns) < 100 + HALF * rounds(max(over + ns - wgs, 0));
+    const int whole = split ? nt - over : nt, halves = split ? 2 * over : 0;
+    // as map_tile: what runs on one XCD at a time lies together
+    auto deal = [&](int i, int n) __attribute__((always_inline)) {
+        const int q = n >> 3, r = n & 7, xcd = i & 7;
+        return xcd * q + (xcd < r ? xcd : r) + (i >> 3);
+    };
+    int L, half = 0;
+    bool left_over = false;
+    o->tall = false;
+    if (t < whole) {
+        L = deal(t, whole);
+        o->tall = true;
+    } else if ((t -= whole) < halves) {
+        const int h = deal(t, halves);
+        L = whole + (h >> 1);
+        half = h & 1;
+    } else if ((t -= halves) < ns) {
+        L = deal(t, ns);
+        left_over = true;
+    } else {
+        return false;
+    }
+    if constexpr (GROUP == BIG_DEPTH) {
+        const int per = (left_over ? small_of(g.K) : tall_of(g.K)) * tiles_n;
+        o->e = L / per;
+        L -= o->e * per;
+        group_rows(g.offsets, g.M, o->e, &o->first, &o->rows);
+    } else {
+        int base = 0, e = -1;
+        for (int e0 = 0; e0 < g.groups; e0 += 64) {
+            if (g.groups > 64) mine = rows_of(e0 + lane);
+            const int n = (left_over ? small_of(mine) : tall_of(mine)) * tiles_n, upto = base + wave_prefix(n, lane);
+            const uint64_t behind = __ballot(upto > L);
+            if (behind) {
+                const int l = __builtin_ctzll(behind);
+                e = e0 + l;
+                L -= __builtin_amdgcn_readlane(upto - n, l);
+                break;
+            }
+            base = __builtin_amdgcn_readlane(upto, 63);
+        }
+        if (e < 0) return false;
+        o->e = e;
+        int first, rows;
+        group_rows(g.offsets, g.M, e, &first, &rows);
+        o->first = __builtin_amdgcn_readfirstlane(first);
+        o->rows = __builtin_amdgcn_readfirstlane(rows);
+    }
+    const int height = GROUP == BIG_DEPTH ? g.K : o->rows;
+    int tm = 0, tn = 0;
+    tile_at(L, tall_of(height), tiles_n, g.group_inv, &tm, &tn);             // (of no use to a tile of left-over rows, whose column L is)
+    o->m0 = left_over ? height & ~255 : tm * 256 + half * 128;
+    o->tn = left_over ? L : tn;
+    return true;
+}
+
+template <int DT, int OT, bool PROT, int GROUP, bool BT>
+__global__ __launch_bounds__(64 * FAST_WAVES) void gemm_group_big_kernel(GroupArgs)
+{
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    constexpr bool DEPTH = GROUP == BIG_DEPTH;
+    constexpr int MODE = PROT ? FAST_BESIDE : FAST_PLAIN, ES = Traits<DT>::ES;
+    fetch_args<GroupArgs>();
+    for (int t = blockIdx.x;; t += gridDim.x) {
+        const GroupArgs &a = kernel_args<GroupArgs>();
+        if (PROT && t == 0 && threadIdx.x < 5) a.counts[threadIdx.x] = 0u;       // completed by the check kernel
+        BigTile b;
+        if (!big_tile<GROUP, PROT>(a, t, (int)gridDim.x, &b)) break;
+        // the operands are done with in LDS: the epilogue's last reads of it precede the next tile's first writes
+        if (t != (int)blockIdx.x) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        GemmArgs g = {};
+        g.A = a.A + (long)b.first * a.lda * ES;
+        g.B = a.B + (DEPTH ? (long)b.first * a.ldb : (long)b.e * a.sB) * ES;
+        g.M = DEPTH ? a.K : b.rows;
+        g.N = a.N;
+        g.K = DEPTH ? b.rows : a.K;
+        g.lda = a.lda; g.ldb = a.ldb;
+        const GroupSource<OT, GROUP> source = {b.e, b.first, b.rows};
+        if (b.tall) fast_tile<DT, OT, 256, MODE, STO_NO, DEPTH, BT>(g, source, smem, b.m0, b.tn * 256, 0, b.tn);
+        else fast_tile<DT, OT, 128, MODE, STO_NO, DEPTH, BT>(g, source, smem, b.m0, b.tn * 256, 0, b.tn);
+    }
+}
+
+template <int DT, int OT, bool PROT, int GROUP, bool BT> static hipError_t launch_big_one(GroupArgs &g, hipStream_t st)
+{
+    hipError_t e;
+    const int cus = device_cu_count(&e);
+    if (e != hipSuccess) return e;
+    constexpr int smem = fast_lds_bytes<PROT ? FAST_BESIDE : FAST_PLAIN>();
+    auto kern = gemm_group_big_kernel<DT, OT, PROT, GROUP, BT>;
+    e = ensure_max_lds(reinterpret_cast<const void *>(kern), smem);
+    if (e != hipSuccess) return e;
+    g.tiles_n = (g.N + 255) / 256;
+    g.group_inv = map_inverse(g.tiles_n);
+    hipLaunchKernelGGL(kern, dim3((unsigned)cus), dim3(64 * FAST_WAVES), smem, st, g);
+    return hipGetLastError();
+}
+
+// Each in a file of its own, for the time it takes to compile them.
+hipError_t launch_group_big_i8(int ot, bool protect, GroupArgs &g, hipStream_t st);
+hipError_t launch_group_big_bf16(bool protect, bool transB, GroupArgs &g, hipStream_t st);
+hipError_t launch_group_big_f16(bool protect, bool transB, GroupArgs &g, hipStream_t st);
+hipError_t launch_group_big_wgrad(int dt, GroupArgs &g, hipStream_t st);
+
+}  // namespace abft

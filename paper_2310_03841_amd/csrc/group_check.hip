@@ -42,7 +42,7 @@ __global__ __launch_bounds__(256) void group_check_kernel(GroupCheckArgs f)
     };
     auto tolerance_cols = [&](int e) __attribute__((always_inline)) { return f.tau_override_cols > 0.f ? f.tau_override_cols : tolerance(e); };
     auto observed = [&](uint32_t *sum, const double *acc, long o) __attribute__((always_inline)) {
-        if constexpr (T::IS_INT) return sum[o];
+        if (T::IS_INT || !acc) return sum[o];
         const uint32_t w = __float_as_uint((float)acc[o]);
         sum[o] = w;
         return w;

@@ -152,12 +152,23 @@ SHAPES = [
     ([0] * 66 + [7, 7, 40], 64, 96, True),              # more groups than lanes, nearly all empty
     (list(range(0, 130 * 3, 3)), 72, 200, False),
 ]
+# Enough for tiles of 256: left-over rows of every kind, a group without rows, columns that end inside a tile, K of the fewest slabs and of many, rows of no
+# group; more than 64 groups; fewer tiles than compute units, and some rounds of them
+BIG = [
+    ([7, 100, 1124, 1124, 2500, 4100], 1030, 384, True),
+    ([0, 256, 512, 640, 769, 4097], 1024, 1152, True),
+    ([0, 1, 2, 130, 4224], 1030, 384, False),
+    ([0, 1500, 1500, 4100], 1001, 448, False),
+    (list(range(0, 131 * 130, 130)), 264, 384, True),
+    ([0, 8192], 512, 384, True),
+    ([0, 4000, 12600], 2056, 384, True),
+]
 TYPES = [("i8", None), ("i8", "bf16"), ("i8", "f16"), ("bf16", None), ("f16", None)]
 
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype,out", TYPES)
-@pytest.mark.parametrize("ends,N,K,trans_b", SHAPES)
+@pytest.mark.parametrize("ends,N,K,trans_b", SHAPES + BIG)
 def test_grouped_matches_plain(dtype, out, ends, N, K, trans_b):
     print(f"case {dtype} {out} {ends[:8]} {N} {K} {trans_b}", flush=True)
     p = Group(dtype, ends, N, K, trans_b, M=ends[-1] + 5, out=out, bias=bool(N % 2), seed=N + K)
@@ -223,7 +234,8 @@ def flips(p, g, i, j, bit, mode):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype,out", TYPES)
-@pytest.mark.parametrize("ends,N,K,trans_b", [([0, 3, 3, 8], 70, 96, True), ([0, 130, 200, 290], 200, 136, False), ([0, 600, 1500], 520, 384, True)])
+@pytest.mark.parametrize("ends,N,K,trans_b", [([0, 3, 3, 8], 70, 96, True), ([0, 130, 200, 290], 200, 136, False), ([0, 600, 1500], 520, 384, True),
+                                               ([0, 1300, 1300, 4200], 1030, 384, True), ([0, 1300, 1300, 4200], 1030, 384, False)])
 def test_a_flip_in_an_accumulator_is_found(dtype, out, ends, N, K, trans_b):
     p = Group(dtype, ends, N, K, trans_b, M=ends[-1], out=out, seed=5)
     try:
@@ -264,7 +276,8 @@ def test_a_weight_that_changed_behind_its_encoding_shows_in_rows(dtype, out):
 @pytest.mark.gpu
 @pytest.mark.parametrize("value", [float("inf"), float("nan")])
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("ends,N,K,trans_b", [([0, 2, 5], 40, 72, True), ([0, 70, 190], 136, 200, False), ([0, 300, 700], 520, 512, True)])
+@pytest.mark.parametrize("ends,N,K,trans_b", [([0, 2, 5], 40, 72, True), ([0, 70, 190], 136, 200, False), ([0, 300, 700], 520, 512, True), ([0, 1300, 4200], 1030, 512, True),
+                                               ([0, 1300, 4200], 1030, 512, False)])
 def test_values_that_are_not_finite_stay_in_their_rows_and_columns(dtype, value, ends, N, K, trans_b):
     p = Group(dtype, ends, N, K, trans_b, seed=7)
     try:
@@ -316,7 +329,9 @@ def wgrad(dtype, ends, N, K, trans_b, M=None, seed=0, guard=0):
 
 
 WGRAD = [([0, 1], 1, 1), ([0, 0, 5, 5], 40, 72), ([3, 60, 61, 189], 130, 100), ([0, 64, 192, 200], 128, 128), ([0, 700, 701, 1500], 257, 136),
-         ([0, 500, 1300], 520, 264), (list(range(0, 72)), 33, 40), ([5, 5], 16, 24)]
+         ([0, 500, 1300], 520, 264), (list(range(0, 72)), 33, 40), ([5, 5], 16, 24),
+         # enough for tiles of 256: depths of no, one and some slabs and a part of one
+         ([2, 2, 3, 66, 131, 300, 1000], 1030, 520), ([0, 64, 128, 320, 1345], 1024, 1001), ([0, 700, 4001], 2056, 1024)]
 
 
 @pytest.mark.gpu
