@@ -145,7 +145,7 @@ __global__ __launch_bounds__(256) void gemm_group_kernel(GroupArgs g)
     if constexpr (PROT) {
         if (blockIdx.x == 0 && tid < 5) g.counts[tid] = 0u;
         if ((int)blockIdx.x < g.n_pass) {
-            group_pass<DT>(g, (int)blockIdx.x * 4 + wave);
+            group_pass<DT>(g, (int)blockIdx.x, smem);
             return;
         }
     }
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(256) void gemm_group_kernel(GroupArgs g)
         Bb = g.B + (long)t.first * g.ldb * ES;
         Cb = g.C + (long)t.e * g.sB * OS;
     } else {
-        if (!find_tile<BM>(g, bid, &t)) return;
+        if (!find_tile<BM>(g, g.tiles_n, g.group_inv, bid, &t)) return;
         M = t.rows;
         K = g.K;
         Ab = g.A + (long)t.first * g.lda * ES;
@@ -413,19 +413,20 @@ __global__ __launch_bounds__(256) void gemm_group_kernel(GroupArgs g)
 // ------------------------------------------------------------------------------------------
 static long ceil_div(long a, long b) { return (a + b - 1) / b; }
 
+// Most tiles along the rows, whatever their split: a tile that is not full for each group that has rows.
+static long row_tiles(int M, int groups, int BM) { return groups == 1 ? ceil_div(M, BM) : M / BM + std::min(M, groups); }
+
 template <int DT, int OT, int BM, int BN, int NS, bool PROT, int GROUP, bool TRANSB>
 static hipError_t launch_one(GroupArgs &g, hipStream_t st)
 {
     constexpr int smem = group_lds_bytes(BM, BN, NS, OT != DT);
+    static_assert(smem >= group_pass_lds<DT>(), "the pass over A runs in the LDS of a tile");
     auto kern = gemm_group_kernel<DT, OT, BM, BN, NS, PROT, GROUP, TRANSB>;
     hipError_t e = ensure_max_lds(reinterpret_cast<const void *>(kern), smem);
     if (e != hipSuccess) return e;
     g.tiles_n = (int)ceil_div(g.N, BN);
     g.group_inv = map_inverse(g.tiles_n);
-    // whatever the split of the rows: a tile that is not full for each group that has rows
-    const long tiles_m = GROUP == GROUP_DEPTH ? ceil_div(g.K, BM) * g.groups
-                         : g.groups == 1    ? ceil_div(g.M, BM)
-                                            : g.M / BM + std::min(g.M, g.groups);
+    const long tiles_m = GROUP == GROUP_DEPTH ? ceil_div(g.K, BM) * g.groups : row_tiles(g.M, g.groups, BM);
     const long wgs = (PROT ? g.n_pass : 0) + ceil_div(tiles_m * g.tiles_n, 8) * 8;
     if (wgs > MAX_GRID_X) return hipErrorInvalidValue;
     hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), smem, st, g);
@@ -450,9 +451,9 @@ template <int DT, int OT> static hipError_t launch_type(bool protect, bool trans
 // The pass over A ahead of tiles that leave no room beside them.
 template <int DT> __global__ __launch_bounds__(256) void group_pass_kernel(GroupArgs g)
 {
+    __shared__ __attribute__((aligned(16))) uint8_t smem[group_pass_lds<DT>()];
     fetch_args<GroupArgs>();
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    group_pass<DT>(g, (int)blockIdx.x * 4 + wave);
+    group_pass<DT>(g, (int)blockIdx.x, smem);
 }
 
 // Whether the tiles of gemm_group_big.h take a product of `rows` rows over `groups` groups: enough of them to fill the chip.
@@ -471,10 +472,11 @@ static bool takes_big(int dt, bool transB, const GroupArgs &g)
 hipError_t launch_group(int dt, int ot, bool protect, bool transB, GroupArgs &g, hipStream_t st)
 {
     if (protect) {
-        const int chunks = (int)ceil_div((long)g.K * elem_size(dt), 16);
-        g.pass_win = (int)ceil_div(chunks, 64);
-        g.pass_rows = 4 * PASS_ROWS;
-        g.n_pass = (int)ceil_div((long)g.pass_win * ceil_div(g.M, g.pass_rows), 4);
+        g.pass_win = (int)ceil_div((long)g.K * elem_size(dt), 16 * PASS_CHUNKS);
+        g.pass_inv = map_inverse(g.pass_win);
+        const long units = row_tiles(g.M, g.groups, PASS_ROWS) * g.pass_win;
+        if (units > MAX_GRID_X) return hipErrorInvalidValue;
+        g.n_pass = (int)ceil_div(units, 8) * 8;
     }
     if (takes_big(dt, transB, g)) {
         if (protect) {

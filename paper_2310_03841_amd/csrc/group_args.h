@@ -25,7 +25,8 @@ struct GroupArgs {
     uint32_t *a_sum, *a_max;              // e^T A and max|A| of a group's rows  [groups][K], [groups]
     const uint32_t *b_sum;                // B e of each group  [groups][K]
     uint32_t *counts;                     // cleared for the check kernel
-    int n_pass, pass_rows, pass_win;      // workgroups ahead of the tiles that pass over A; rows to a wave; windows along K
+    int n_pass, pass_win;                 // workgroups ahead of the tiles that pass over A; their windows along K
+    uint32_t pass_inv;                    // map_inverse(pass_win)
 };
 
 // The rows of group e: whatever the offsets hold, inside [0, M].
@@ -70,9 +71,10 @@ struct GroupTile { int e, tm, tn, first, rows; };
 
 // The tile of workgroup `bid` of those that take tiles, of BM rows each: false, there is none for it.  Every wave finds it by itself, 64 groups at
 // a time.  Consecutive tiles of an XCD are a group's, in the order of map_tile, so what shares rows of A or B meets in one L2.
-template <int BM> __device__ __forceinline__ bool find_tile(const GroupArgs &g, int bid, GroupTile *t)
+// tiles_n, inv: tiles along the other direction, map_inverse of them.
+template <int BM> __device__ __forceinline__ bool find_tile(const GroupArgs &g, int tiles_n, uint32_t inv, int bid, GroupTile *t)
 {
-    const int lane = threadIdx.x & 63, tiles_n = g.tiles_n;
+    const int lane = threadIdx.x & 63;
     auto tiles_of = [&](int e) __attribute__((always_inline)) {
         int first = 0, rows = 0;
         if (e < g.groups) group_rows(g.offsets, g.M, e, &first, &rows);
@@ -115,7 +117,7 @@ template <int BM> __device__ __forceinline__ bool find_tile(const GroupArgs &g, 
         t->first = __builtin_amdgcn_readfirstlane(t->first);
         t->rows = __builtin_amdgcn_readfirstlane(t->rows);
     }
-    tile_at(L, (t->rows + BM - 1) / BM, tiles_n, g.group_inv, &t->tm, &t->tn);
+    tile_at(L, (t->rows + BM - 1) / BM, tiles_n, inv, &t->tm, &t->tn);
     return true;
 }
 
