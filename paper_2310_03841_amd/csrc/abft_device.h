@@ -7,6 +7,7 @@
 namespace abft {
 
 typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef int i32x4_word __attribute__((ext_vector_type(4), aligned(4)));     // at any word
 typedef __attribute__((ext_vector_type(16))) int i32x16;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;

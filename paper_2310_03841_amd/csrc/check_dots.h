@@ -32,7 +32,6 @@ __device__ __forceinline__ void report_flags(uint32_t *counts, int side, unsigne
 // start on any word: batch items of a ragged K do, and a caller's may.  (The kernel, with a branch around each load / with a path of loads
 // without them for whole chunks and aligned vectors, word by word otherwise / so: int8 10624 x 221 x 2360 14.8 / 20.6 / 11.8 us; 570 x 570 x 48, 48
 // items, where the second 64 lanes of a trip have nothing, 19.1 / 21.8 / 11.7; bf16 640 x 2880 x 1535 4.7 / 6.6 / 4.8.)
-typedef int i32x4_word __attribute__((ext_vector_type(4), aligned(4)));
 template <int DT, int RW>
 __device__ __forceinline__ void row_dots(const uint8_t *X, long ld, int row0, int rows, int K, const uint32_t *vec,
                                          bool split, typename Traits<DT>::acc_t (&dot)[RW])

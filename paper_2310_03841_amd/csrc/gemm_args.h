@@ -40,7 +40,7 @@ struct GemmArgs {
 // group_inv: 2^32 / (4 tiles_n) rounded down (map_inverse): a quotient by it is the true one or one less.  (Three divisions, of which a scalar unit
 // has none, took 830 of the 3200 clocks before a tile's first load.)
 constexpr int GROUP_M = 4;              // measured against 2, 3, 6, 8, 16: best or equal on every Linear shape
-inline uint32_t map_inverse(int tiles_n) { return (uint32_t)((1ull << 32) / ((uint64_t)GROUP_M * tiles_n)); }
+__host__ __device__ constexpr uint32_t map_inverse(int tiles_n) { return (uint32_t)((1ull << 32) / ((uint64_t)GROUP_M * tiles_n)); }
 // Tile L of a region in that order.
 __device__ __forceinline__ void tile_at(int L, int tiles_m, int tiles_n, uint32_t group_inv, int *tm, int *tn)
 {

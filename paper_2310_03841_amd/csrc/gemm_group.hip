@@ -145,7 +145,9 @@ __global__ __launch_bounds__(256) void gemm_group_kernel(GroupArgs g)
     if constexpr (PROT) {
         if (blockIdx.x == 0 && tid < 5) g.counts[tid] = 0u;
         if ((int)blockIdx.x < g.n_pass) {
-            group_pass<DT>(g, (int)blockIdx.x, smem);
+            GroupTile t;
+            if (find_tile<4 * PASS_ROWS>(g, g.pass_win, g.pass_inv, (int)blockIdx.x, &t))
+                group_pass<DT, 4>(g, t.e, t.first, t.rows, t.tm * 4 * PASS_ROWS, t.tn, smem);
             return;
         }
     }
@@ -420,7 +422,7 @@ template <int DT, int OT, int BM, int BN, int NS, bool PROT, int GROUP, bool TRA
 static hipError_t launch_one(GroupArgs &g, hipStream_t st)
 {
     constexpr int smem = group_lds_bytes(BM, BN, NS, OT != DT);
-    static_assert(smem >= group_pass_lds<DT>(), "the pass over A runs in the LDS of a tile");
+    static_assert(smem >= group_pass_lds<DT, 4>(), "the pass over A runs in the LDS of a tile");
     auto kern = gemm_group_kernel<DT, OT, BM, BN, NS, PROT, GROUP, TRANSB>;
     hipError_t e = ensure_max_lds(reinterpret_cast<const void *>(kern), smem);
     if (e != hipSuccess) return e;
@@ -448,14 +450,6 @@ template <int DT, int OT> static hipError_t launch_type(bool protect, bool trans
                                : launch_rows<DT, OT, 64, 64, 4>(protect, transB, g, st);
 }
 
-// The pass over A ahead of tiles that leave no room beside them.
-template <int DT> __global__ __launch_bounds__(256) void group_pass_kernel(GroupArgs g)
-{
-    __shared__ __attribute__((aligned(16))) uint8_t smem[group_pass_lds<DT>()];
-    fetch_args<GroupArgs>();
-    group_pass<DT>(g, (int)blockIdx.x, smem);
-}
-
 // Whether the tiles of gemm_group_big.h take a product of `rows` rows over `groups` groups: enough of them to fill the chip.
 static bool fills_chip(long rows, int groups, int N)
 {
@@ -472,24 +466,14 @@ static bool takes_big(int dt, bool transB, const GroupArgs &g)
 hipError_t launch_group(int dt, int ot, bool protect, bool transB, GroupArgs &g, hipStream_t st)
 {
     if (protect) {
-        g.pass_win = (int)ceil_div((long)g.K * elem_size(dt), 16 * PASS_CHUNKS);
+        g.pass_win = (int)ceil_div((long)g.K * elem_size(dt), PASS_BYTES);
         g.pass_inv = map_inverse(g.pass_win);
-        const long units = row_tiles(g.M, g.groups, PASS_ROWS) * g.pass_win;
+        const long units = row_tiles(g.M, g.groups, 4 * PASS_ROWS) * g.pass_win;
         if (units > MAX_GRID_X) return hipErrorInvalidValue;
         g.n_pass = (int)ceil_div(units, 8) * 8;
     }
     if (takes_big(dt, transB, g)) {
-        if (protect) {
-            if (dt != DT_I8) g.cc_acc = g.rc_acc = nullptr;      // these tiles add to the sums themselves
-            const dim3 grid((unsigned)g.n_pass);
-            switch (dt) {
-            case DT_I8:   hipLaunchKernelGGL(group_pass_kernel<DT_I8>, grid, dim3(256), 0, st, g); break;
-            case DT_BF16: hipLaunchKernelGGL(group_pass_kernel<DT_BF16>, grid, dim3(256), 0, st, g); break;
-            default:      hipLaunchKernelGGL(group_pass_kernel<DT_F16>, grid, dim3(256), 0, st, g); break;
-            }
-            const hipError_t e = hipGetLastError();
-            if (e != hipSuccess) return e;
-        }
+        if (dt != DT_I8) g.cc_acc = g.rc_acc = nullptr;          // these tiles add to the sums themselves
         switch (dt) {
         case DT_I8:   return launch_group_big_i8(ot, protect, g, st);
         case DT_BF16: return launch_group_big_bf16(protect, transB, g, st);

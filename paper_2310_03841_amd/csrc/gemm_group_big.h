@@ -3,10 +3,13 @@
 //
 // A group's rows are covered by tiles of 256, the last 128 of them, where no more are left over, by one of 128.  One workgroup to a compute unit walks
 // the list: the tiles of 256 first, a round of the machine at a time; what would be a last round of few of them is dealt out as twice as many of 128 rows
-// where that ends sooner (a tile of 128 rows takes 0.57 of the time of one of 256, protected 0.66); then the tiles of left-over rows.
+// where that ends sooner (a tile of 128 rows takes 0.57 of the time of one of 256, protected 0.66); then the tiles of left-over rows; and
+// protected, last, the pass over A, 64 rows and a window to an item.  Every other round goes through the compute units backwards, so that those with the shorter
+// items of one are the first with those of the next.
 #pragma once
 #include "gemm_fast_tile.h"
 #include "group_args.h"
+#include "group_passes.h"
 
 namespace abft {
 
@@ -43,7 +46,8 @@ template <int OT, int GROUP> struct GroupSource {
     }
 };
 
-struct BigTile { int e, first, rows, m0, tn; bool tall; };
+enum { ITEM_PASS, ITEM_SMALL, ITEM_TALL };
+struct BigTile { int e, first, rows, m0, tn, what; };
 
 // Tile t of the list: false, there is none.
 template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const GroupArgs &g, int t, int wgs, BigTile *o)
@@ -57,7 +61,8 @@ template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const G
         if (e < g.groups) group_rows(g.offsets, g.M, e, &first, &rows);
         return rows;
     };
-    int mine = 0, talls, smalls;                                 // rows of this lane's group; of tiles of all
+    auto passes_of = [&](int rows) __attribute__((always_inline)) { return (rows + 8 * PASS_ROWS - 1) / (8 * PASS_ROWS) * g.pass_win; };
+    int mine = 0, talls, smalls, passes = 0;                     // rows of this lane's group; of tiles of all
     if constexpr (GROUP == BIG_DEPTH) {
         talls = tall_of(g.K) * g.groups;
         smalls = small_of(g.K) * g.groups;
@@ -67,9 +72,11 @@ template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const G
             mine = rows_of(e0 + lane);
             talls += wave_sum(tall_of(mine));
             smalls += wave_sum(small_of(mine));
+            if constexpr (PROT) passes += wave_sum(passes_of(mine));
         }
         talls = __builtin_amdgcn_readfirstlane(talls);
         smalls = __builtin_amdgcn_readfirstlane(smalls);
+        passes = __builtin_amdgcn_readfirstlane(passes);
     }
     const int nt = talls * tiles_n, ns = smalls * tiles_n, over = nt % wgs;
     constexpr int HALF = PROT ? 66 : 57;                         // of 100
@@ -83,10 +90,10 @@ template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const G
     };
     int L, half = 0;
     bool left_over = false;
-    o->tall = false;
+    o->what = ITEM_SMALL;
     if (t < whole) {
         L = deal(t, whole);
-        o->tall = true;
+        o->what = ITEM_TALL;
     } else if ((t -= whole) < halves) {
         const int h = deal(t, halves);
         L = whole + (h >> 1);
@@ -94,6 +101,9 @@ template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const G
     } else if ((t -= halves) < ns) {
         L = deal(t, ns);
         left_over = true;
+    } else if (PROT && (t -= ns) < passes) {
+        L = t;
+        o->what = ITEM_PASS;
     } else {
         return false;
     }
@@ -106,7 +116,7 @@ template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const G
         int base = 0, e = -1;
         for (int e0 = 0; e0 < g.groups; e0 += 64) {
             if (g.groups > 64) mine = rows_of(e0 + lane);
-            const int n = (left_over ? small_of(mine) : tall_of(mine)) * tiles_n, upto = base + wave_prefix(n, lane);
+            const int n = PROT && o->what == ITEM_PASS ? passes_of(mine) : (left_over ? small_of(mine) : tall_of(mine)) * tiles_n, upto = base + wave_prefix(n, lane);
             const uint64_t behind = __ballot(upto > L);
             if (behind) {
                 const int l = __builtin_ctzll(behind);
@@ -128,6 +138,11 @@ template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const G
     tile_at(L, tall_of(height), tiles_n, g.group_inv, &tm, &tn);             // (of no use to a tile of left-over rows, whose column L is)
     o->m0 = left_over ? height & ~255 : tm * 256 + half * 128;
     o->tn = left_over ? L : tn;
+    if (PROT && o->what == ITEM_PASS) {
+        const int row = L / g.pass_win;
+        o->m0 = row * 8 * PASS_ROWS;
+        o->tn = L - row * g.pass_win;
+    }
     return true;
 }
 
@@ -138,13 +153,18 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void gemm_group_big_kernel(GroupAr
     constexpr bool DEPTH = GROUP == BIG_DEPTH;
     constexpr int MODE = PROT ? FAST_BESIDE : FAST_PLAIN, ES = Traits<DT>::ES;
     fetch_args<GroupArgs>();
-    for (int t = blockIdx.x;; t += gridDim.x) {
+    for (int round = 0;; ++round) {
+        const int wgs = (int)gridDim.x, t = round * wgs + (round & 1 ? wgs - 1 - (int)blockIdx.x : (int)blockIdx.x);
         const GroupArgs &a = kernel_args<GroupArgs>();
         if (PROT && t == 0 && threadIdx.x < 5) a.counts[threadIdx.x] = 0u;       // completed by the check kernel
         BigTile b;
-        if (!big_tile<GROUP, PROT>(a, t, (int)gridDim.x, &b)) break;
+        if (!big_tile<GROUP, PROT>(a, t, wgs, &b)) break;
         // the operands are done with in LDS: the epilogue's last reads of it precede the next tile's first writes
-        if (t != (int)blockIdx.x) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (round) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (PROT && b.what == ITEM_PASS) {
+            group_pass<DT, 8>(a, b.e, b.first, b.rows, b.m0, b.tn, smem);
+            continue;
+        }
         GemmArgs g = {};
         g.A = a.A + (long)b.first * a.lda * ES;
         g.B = a.B + (DEPTH ? (long)b.first * a.ldb : (long)b.e * a.sB) * ES;
@@ -153,7 +173,7 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void gemm_group_big_kernel(GroupAr
         g.K = DEPTH ? b.rows : a.K;
         g.lda = a.lda; g.ldb = a.ldb;
         const GroupSource<OT, GROUP> source = {b.e, b.first, b.rows};
-        if (b.tall) fast_tile<DT, OT, 256, MODE, STO_NO, DEPTH, BT>(g, source, smem, b.m0, b.tn * 256, 0, b.tn);
+        if (b.what == ITEM_TALL) fast_tile<DT, OT, 256, MODE, STO_NO, DEPTH, BT>(g, source, smem, b.m0, b.tn * 256, 0, b.tn);
         else fast_tile<DT, OT, 128, MODE, STO_NO, DEPTH, BT>(g, source, smem, b.m0, b.tn * 256, 0, b.tn);
     }
 }
