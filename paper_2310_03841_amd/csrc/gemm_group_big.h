@@ -49,30 +49,35 @@ template <int OT, int GROUP> struct GroupSource {
 enum { ITEM_PASS, ITEM_SMALL, ITEM_TALL };
 struct BigTile { int e, first, rows, m0, tn, what; };
 
+// The rows of a lane's group, of up to 64: read once and kept, since a trip to memory ahead of every tile is 1 us of its 15 to 30.
+struct GroupLane { int first, rows; };
+__device__ __forceinline__ GroupLane group_lane(const GroupArgs &g, int e)
+{
+    GroupLane l = {0, 0};
+    if (e < g.groups) group_rows(g.offsets, g.M, e, &l.first, &l.rows);
+    return l;
+}
+
 // Tile t of the list: false, there is none.
-template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const GroupArgs &g, int t, int wgs, BigTile *o)
+template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const GroupArgs &g, const GroupLane &kept, int t, int wgs, BigTile *o)
 {
     const int lane = threadIdx.x & 63, tiles_n = g.tiles_n;
     // rows of tiles of 256, of 128, of a product of so many rows
     auto tall_of = [&](int rows) __attribute__((always_inline)) { return (rows >> 8) + ((rows & 255) > 128); };
     auto small_of = [&](int rows) __attribute__((always_inline)) { return ((rows & 255) + 127) >> 7 & 1; };
-    auto rows_of = [&](int e) __attribute__((always_inline)) {
-        int first = 0, rows = 0;
-        if (e < g.groups) group_rows(g.offsets, g.M, e, &first, &rows);
-        return rows;
-    };
     auto passes_of = [&](int rows) __attribute__((always_inline)) { return (rows + 8 * PASS_ROWS - 1) / (8 * PASS_ROWS) * g.pass_win; };
-    int mine = 0, talls, smalls, passes = 0;                     // rows of this lane's group; of tiles of all
+    GroupLane mine = kept;
+    int talls, smalls, passes = 0;                               // rows of tiles of all groups
     if constexpr (GROUP == BIG_DEPTH) {
         talls = tall_of(g.K) * g.groups;
         smalls = small_of(g.K) * g.groups;
     } else {
         talls = smalls = 0;
         for (int e0 = 0; e0 < g.groups; e0 += 64) {
-            mine = rows_of(e0 + lane);
-            talls += wave_sum(tall_of(mine));
-            smalls += wave_sum(small_of(mine));
-            if constexpr (PROT) passes += wave_sum(passes_of(mine));
+            if (g.groups > 64) mine = group_lane(g, e0 + lane);
+            talls += wave_sum(tall_of(mine.rows));
+            smalls += wave_sum(small_of(mine.rows));
+            if constexpr (PROT) passes += wave_sum(passes_of(mine.rows));
         }
         talls = __builtin_amdgcn_readfirstlane(talls);
         smalls = __builtin_amdgcn_readfirstlane(smalls);
@@ -115,23 +120,22 @@ template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const G
     } else {
         int base = 0, e = -1;
         for (int e0 = 0; e0 < g.groups; e0 += 64) {
-            if (g.groups > 64) mine = rows_of(e0 + lane);
-            const int n = PROT && o->what == ITEM_PASS ? passes_of(mine) : (left_over ? small_of(mine) : tall_of(mine)) * tiles_n, upto = base + wave_prefix(n, lane);
+            if (g.groups > 64) mine = group_lane(g, e0 + lane);
+            const int n = PROT && o->what == ITEM_PASS ? passes_of(mine.rows) : (left_over ? small_of(mine.rows) : tall_of(mine.rows)) * tiles_n;
+            const int upto = base + wave_prefix(n);
             const uint64_t behind = __ballot(upto > L);
             if (behind) {
                 const int l = __builtin_ctzll(behind);
                 e = e0 + l;
                 L -= __builtin_amdgcn_readlane(upto - n, l);
+                o->first = __builtin_amdgcn_readlane(mine.first, l);
+                o->rows = __builtin_amdgcn_readlane(mine.rows, l);
                 break;
             }
             base = __builtin_amdgcn_readlane(upto, 63);
         }
         if (e < 0) return false;
         o->e = e;
-        int first, rows;
-        group_rows(g.offsets, g.M, e, &first, &rows);
-        o->first = __builtin_amdgcn_readfirstlane(first);
-        o->rows = __builtin_amdgcn_readfirstlane(rows);
     }
     const int height = GROUP == BIG_DEPTH ? g.K : o->rows;
     int tm = 0, tn = 0;
@@ -153,12 +157,14 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void gemm_group_big_kernel(GroupAr
     constexpr bool DEPTH = GROUP == BIG_DEPTH;
     constexpr int MODE = PROT ? FAST_BESIDE : FAST_PLAIN, ES = Traits<DT>::ES;
     fetch_args<GroupArgs>();
+    GroupLane kept = {0, 0};
+    if constexpr (!DEPTH) kept = group_lane(kernel_args<GroupArgs>(), threadIdx.x & 63);
     for (int round = 0;; ++round) {
         const int wgs = (int)gridDim.x, t = round * wgs + (round & 1 ? wgs - 1 - (int)blockIdx.x : (int)blockIdx.x);
         const GroupArgs &a = kernel_args<GroupArgs>();
         if (PROT && t == 0 && threadIdx.x < 5) a.counts[threadIdx.x] = 0u;       // completed by the check kernel
         BigTile b;
-        if (!big_tile<GROUP, PROT>(a, t, wgs, &b)) break;
+        if (!big_tile<GROUP, PROT>(a, kept, t, wgs, &b)) break;
         // the operands are done with in LDS: the epilogue's last reads of it precede the next tile's first writes
         if (round) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (PROT && b.what == ITEM_PASS) {

@@ -57,13 +57,14 @@ __device__ __forceinline__ int group_of(const int *offsets, int M, int groups, i
 }
 
 // Sum over the lanes up to and with this one.
-__device__ __forceinline__ int wave_prefix(int v, int lane)
+__device__ __forceinline__ int wave_prefix(int v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int up = __shfl_up(v, d);
-        if (lane >= d) v += up;
-    }
+    v += dpp_mov<0x111>(v);                                      // row_shr:1, 2, 4, 8 inside 16 lanes
+    v += dpp_mov<0x112>(v);
+    v += dpp_mov<0x114>(v);
+    v += dpp_mov<0x118>(v);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);     // row_bcast:15 into rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);     // row_bcast:31 into rows 2 and 3
     return v;
 }
 
@@ -101,7 +102,7 @@ template <int BM> __device__ __forceinline__ bool find_tile(const GroupArgs &g, 
         int base = 0, e = -1;
         for (int e0 = 0; e0 < g.groups; e0 += 64) {
             if (g.groups > 64) mine = tiles_of(e0 + lane);
-            const int upto = base + wave_prefix(mine, lane);
+            const int upto = base + wave_prefix(mine);
             const uint64_t behind = __ballot(upto > L);
             if (behind) {
                 const int l = __builtin_ctzll(behind);

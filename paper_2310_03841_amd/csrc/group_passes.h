@@ -87,7 +87,7 @@ template <int DT, int WAVES> __device__ __forceinline__ void group_pass(const Gr
         mine = lane == u ? s : mine;
     }
     if (lane < PASS_ROWS && r0 + lane < rows) atomic_add_word(g.rc_pred + first + r0 + lane, mine);
-    __syncthreads();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // (over LDS alone: not for the additions above)
 #pragma unroll
     for (int c = tid; c < COLS; c += 64 * WAVES) {
         if (k0 + c < K) {
