@@ -400,6 +400,19 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, SRC sou
             for (int i = 0; i < 16; ++i) cp[ni][i] = T::zero();
     }
 
+    // scales and bias of the lane's columns, in registers: read again with every group of rows they were 512 KB of LDS traffic to a tile
+    // (protected, there are registers for the scales alone)
+    i32x4 col4[SCALED ? NI : 1][4], bias4[SCALED && !PROT ? NI : 1][4];
+    if constexpr (SCALED) {
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = wn * TN + ni * 32 + 8 * q + 4 * lh;
+                col4[ni][q] = *reinterpret_cast<const i32x4 *>(scol + c);
+                if constexpr (!PROT) bias4[ni][q] = *reinterpret_cast<const i32x4 *>(sbias + c);
+            }
+    }
     static_for<0, MI>([&](auto mi_c) {
         constexpr int mi = decltype(mi_c)::value;
         const int br = wr0 + mi * 32;                                      // first row of this 32-row group
@@ -431,8 +444,8 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, SRC sou
                     }
                     uint8_t *d = wbuf + l32 * CROW + (ni * 32 + 8 * q + 4 * lh) * OS;
                     if constexpr (SCALED) {
-                        const int c = wn * TN + ni * 32 + 8 * q + 4 * lh;
-                        const i32x4 c4 = *reinterpret_cast<const i32x4 *>(scol + c), b4 = *reinterpret_cast<const i32x4 *>(sbias + c);
+                        const i32x4 c4 = col4[ni][q];
+                        const i32x4 b4 = PROT ? *reinterpret_cast<const i32x4 *>(sbias + wn * TN + ni * 32 + 8 * q + 4 * lh) : bias4[PROT ? 0 : ni][q];
                         auto f = [&](int e) __attribute__((always_inline)) { return __uint_as_float((uint32_t)e); };
                         uint2 w;
                         w.x = pack2<OT>(scaled(v0, rscale, f(c4[0]), f(b4[0])), scaled(v1, rscale, f(c4[1]), f(b4[1])));

@@ -2,10 +2,11 @@
 // the depths of the groups for the gradient of their matrices.
 //
 // A group's rows are covered by tiles of 256, the last 128 of them, where no more are left over, by one of 128.  One workgroup to a compute unit walks
-// the list: the tiles of 256 first, a round of the machine at a time; what would be a last round of few of them is dealt out as twice as many of 128 rows
-// where that ends sooner (a tile of 128 rows takes 0.57 of the time of one of 256, protected 0.66); then the tiles of left-over rows; and
-// protected, last, the pass over A, 64 rows and a window to an item.  Every other round goes through the compute units backwards, so that those with the shorter
-// items of one are the first with those of the next.
+// the list with the grid's stride.  What would be a last round of few tiles of 256 is dealt out as twice as many of 128 rows where that ends sooner (a tile of
+// 128 rows takes 0.57 of the time of one of 256, protected 0.66).  Tiles of 128 rows come first, as in the fast kernel: the compute units that start
+// with one are ahead of the others from then on, so that not all store C at once, and they are the first with what is left in the last round (all tiles
+// of 256 first / so, one group, unprotected: bf16 12608 x 3072 x 768 61.3 / 54.0 us, int8 54.8 / 48.3).  Protected, the
+// pass over A comes last, 64 rows and a window to an item, by the compute units that have no tile in the last round, unless those are few.
 #pragma once
 #include "gemm_fast_tile.h"
 #include "group_args.h"
@@ -46,8 +47,7 @@ template <int OT, int GROUP> struct GroupSource {
     }
 };
 
-enum { ITEM_PASS, ITEM_SMALL, ITEM_TALL };
-struct BigTile { int e, first, rows, m0, tn, what; };
+struct BigTile { int e, first, rows, m0, tn; bool tall; };
 
 // The rows of a lane's group, of up to 64: read once and kept, since a trip to memory ahead of every tile is 1 us of its 15 to 30.
 struct GroupLane { int first, rows; };
@@ -58,16 +58,37 @@ __device__ __forceinline__ GroupLane group_lane(const GroupArgs &g, int e)
     return l;
 }
 
-// Tile t of the list: false, there is none.
-template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const GroupArgs &g, const GroupLane &kept, int t, int wgs, BigTile *o)
+// The group that item L of a list belongs to, and its place among that group's; of a group of so many rows there are of(rows) items.
+template <typename OF> __device__ __forceinline__ bool big_group(const GroupArgs &g, GroupLane mine, const OF &of, int *L, BigTile *o)
+{
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int e0 = 0; e0 < g.groups; e0 += 64) {
+        if (g.groups > 64) mine = group_lane(g, e0 + lane);
+        const int n = of(mine.rows), upto = base + wave_prefix(n);
+        const uint64_t behind = __ballot(upto > *L);
+        if (behind) {
+            const int l = __builtin_ctzll(behind);
+            o->e = e0 + l;
+            *L -= __builtin_amdgcn_readlane(upto - n, l);
+            o->first = __builtin_amdgcn_readlane(mine.first, l);
+            o->rows = __builtin_amdgcn_readlane(mine.rows, l);
+            return true;
+        }
+        base = __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
+// Tile t of the list: false, there is none, and *tiles are all.
+template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const GroupArgs &g, const GroupLane &kept, int t, int wgs, BigTile *o, int *tiles)
 {
     const int lane = threadIdx.x & 63, tiles_n = g.tiles_n;
     // rows of tiles of 256, of 128, of a product of so many rows
     auto tall_of = [&](int rows) __attribute__((always_inline)) { return (rows >> 8) + ((rows & 255) > 128); };
     auto small_of = [&](int rows) __attribute__((always_inline)) { return ((rows & 255) + 127) >> 7 & 1; };
-    auto passes_of = [&](int rows) __attribute__((always_inline)) { return (rows + 8 * PASS_ROWS - 1) / (8 * PASS_ROWS) * g.pass_win; };
     GroupLane mine = kept;
-    int talls, smalls, passes = 0;                               // rows of tiles of all groups
+    int talls, smalls;                                           // rows of tiles of all groups
     if constexpr (GROUP == BIG_DEPTH) {
         talls = tall_of(g.K) * g.groups;
         smalls = small_of(g.K) * g.groups;
@@ -77,11 +98,9 @@ template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const G
             if (g.groups > 64) mine = group_lane(g, e0 + lane);
             talls += wave_sum(tall_of(mine.rows));
             smalls += wave_sum(small_of(mine.rows));
-            if constexpr (PROT) passes += wave_sum(passes_of(mine.rows));
         }
         talls = __builtin_amdgcn_readfirstlane(talls);
         smalls = __builtin_amdgcn_readfirstlane(smalls);
-        passes = __builtin_amdgcn_readfirstlane(passes);
     }
     const int nt = talls * tiles_n, ns = smalls * tiles_n, over = nt % wgs;
     constexpr int HALF = PROT ? 66 : 57;                         // of 100
@@ -95,20 +114,18 @@ template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const G
     };
     int L, half = 0;
     bool left_over = false;
-    o->what = ITEM_SMALL;
-    if (t < whole) {
-        L = deal(t, whole);
-        o->what = ITEM_TALL;
-    } else if ((t -= whole) < halves) {
+    o->tall = false;
+    *tiles = halves + ns + whole;
+    if (t < halves) {
         const int h = deal(t, halves);
         L = whole + (h >> 1);
         half = h & 1;
     } else if ((t -= halves) < ns) {
         L = deal(t, ns);
         left_over = true;
-    } else if (PROT && (t -= ns) < passes) {
-        L = t;
-        o->what = ITEM_PASS;
+    } else if ((t -= ns) < whole) {
+        L = deal(t, whole);
+        o->tall = true;
     } else {
         return false;
     }
@@ -118,35 +135,14 @@ template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const G
         L -= o->e * per;
         group_rows(g.offsets, g.M, o->e, &o->first, &o->rows);
     } else {
-        int base = 0, e = -1;
-        for (int e0 = 0; e0 < g.groups; e0 += 64) {
-            if (g.groups > 64) mine = group_lane(g, e0 + lane);
-            const int n = PROT && o->what == ITEM_PASS ? passes_of(mine.rows) : (left_over ? small_of(mine.rows) : tall_of(mine.rows)) * tiles_n;
-            const int upto = base + wave_prefix(n);
-            const uint64_t behind = __ballot(upto > L);
-            if (behind) {
-                const int l = __builtin_ctzll(behind);
-                e = e0 + l;
-                L -= __builtin_amdgcn_readlane(upto - n, l);
-                o->first = __builtin_amdgcn_readlane(mine.first, l);
-                o->rows = __builtin_amdgcn_readlane(mine.rows, l);
-                break;
-            }
-            base = __builtin_amdgcn_readlane(upto, 63);
-        }
-        if (e < 0) return false;
-        o->e = e;
+        const bool found = big_group(g, kept, [&](int rows) { return (left_over ? small_of(rows) : tall_of(rows)) * tiles_n; }, &L, o);
+        if (!found) return false;
     }
     const int height = GROUP == BIG_DEPTH ? g.K : o->rows;
     int tm = 0, tn = 0;
     tile_at(L, tall_of(height), tiles_n, g.group_inv, &tm, &tn);             // (of no use to a tile of left-over rows, whose column L is)
     o->m0 = left_over ? height & ~255 : tm * 256 + half * 128;
     o->tn = left_over ? L : tn;
-    if (PROT && o->what == ITEM_PASS) {
-        const int row = L / g.pass_win;
-        o->m0 = row * 8 * PASS_ROWS;
-        o->tn = L - row * g.pass_win;
-    }
     return true;
 }
 
@@ -159,18 +155,14 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void gemm_group_big_kernel(GroupAr
     fetch_args<GroupArgs>();
     GroupLane kept = {0, 0};
     if constexpr (!DEPTH) kept = group_lane(kernel_args<GroupArgs>(), threadIdx.x & 63);
-    for (int round = 0;; ++round) {
-        const int wgs = (int)gridDim.x, t = round * wgs + (round & 1 ? wgs - 1 - (int)blockIdx.x : (int)blockIdx.x);
+    int tiles;
+    for (int t = blockIdx.x;; t += gridDim.x) {
         const GroupArgs &a = kernel_args<GroupArgs>();
         if (PROT && t == 0 && threadIdx.x < 5) a.counts[threadIdx.x] = 0u;       // completed by the check kernel
         BigTile b;
-        if (!big_tile<GROUP, PROT>(a, kept, t, wgs, &b)) break;
-        // the operands are done with in LDS: the epilogue's last reads of it precede the next tile's first writes
-        if (round) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (PROT && b.what == ITEM_PASS) {
-            group_pass<DT, 8>(a, b.e, b.first, b.rows, b.m0, b.tn, smem);
-            continue;
-        }
+        if (!big_tile<GROUP, PROT>(a, kept, t, (int)gridDim.x, &b, &tiles)) break;
+        // the epilogue's last reads of LDS precede the next tile's first writes
+        if (t != (int)blockIdx.x) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         GemmArgs g = {};
         g.A = a.A + (long)b.first * a.lda * ES;
         g.B = a.B + (DEPTH ? (long)b.first * a.ldb : (long)b.e * a.sB) * ES;
@@ -179,8 +171,30 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void gemm_group_big_kernel(GroupAr
         g.K = DEPTH ? b.rows : a.K;
         g.lda = a.lda; g.ldb = a.ldb;
         const GroupSource<OT, GROUP> source = {b.e, b.first, b.rows};
-        if (b.what == ITEM_TALL) fast_tile<DT, OT, 256, MODE, STO_NO, DEPTH, BT>(g, source, smem, b.m0, b.tn * 256, 0, b.tn);
+        if (b.tall) fast_tile<DT, OT, 256, MODE, STO_NO, DEPTH, BT>(g, source, smem, b.m0, b.tn * 256, 0, b.tn);
         else fast_tile<DT, OT, 128, MODE, STO_NO, DEPTH, BT>(g, source, smem, b.m0, b.tn * 256, 0, b.tn);
+    }
+    if constexpr (PROT) {
+        constexpr int ROWS = FAST_WAVES * PASS_ROWS;
+        const GroupArgs &a = kernel_args<GroupArgs>();
+        int passes = 0;
+        GroupLane mine = kept;
+        auto passes_of = [&](int rows) __attribute__((always_inline)) { return (rows + ROWS - 1) / ROWS * a.pass_win; };
+        for (int e0 = 0; e0 < a.groups; e0 += 64) {
+            if (a.groups > 64) mine = group_lane(a, e0 + (threadIdx.x & 63));
+            passes += wave_sum(passes_of(mine.rows));
+        }
+        passes = __builtin_amdgcn_readfirstlane(passes);
+        int busy = tiles % (int)gridDim.x, free = (int)gridDim.x - busy;
+        if (passes > 4 * free) { busy = 0; free = (int)gridDim.x; }
+        for (int p = (int)blockIdx.x - busy; p >= 0 && p < passes; p += free) {
+            BigTile b;
+            int L = p;
+            if (!big_group(a, kept, passes_of, &L, &b)) break;
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            const int row = L / a.pass_win;
+            group_pass<DT, FAST_WAVES>(a, b.e, b.first, b.rows, row * ROWS, L - row * a.pass_win, smem);
+        }
     }
 }
 
