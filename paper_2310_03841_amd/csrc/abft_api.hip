@@ -744,7 +744,7 @@ static int enqueue_group(abft_ctx *ctx, int dtype, int ot, bool cached, GroupArg
     if (!cached) HIP_TRY(launch_encode_b(dtype, B, sh, w, w.cc_obs, stale, st));
     else if (stale) HIP_TRY(launch_zero(w.cc_obs, stale, st));
     ctx->sto_valid = false;
-    HIP_TRY(launch_group(dtype, ot, true, sh.transB != 0, g, st));
+    HIP_TRY(launch_group(dtype, ot, true, sh.transB != 0, g, w.b_max, &v, st));
     if (ctx->done_event && !gm) HIP_TRY(hipEventRecord(ctx->done_event, st));
     HIP_TRY(launch_group_check(dtype, g, sh.transB != 0, w, v, end, st));
     if (!gm) {
@@ -781,7 +781,7 @@ static int group_impl(abft_ctx *ctx, const void *A, const void *B, const int32_t
     if (q) { g.row_scale = q->row; g.col_scale = q->col; g.bias = q->bias; }
     if (base == ABFT_OFF) {
         ctx->arm.batch = -1;
-        HIP_TRY(launch_group(dtype, ot, false, sh.transB != 0, g, st));
+        HIP_TRY(launch_group(dtype, ot, false, sh.transB != 0, g, nullptr, nullptr, st));
         if (ctx->done_event && !capturing(st)) HIP_TRY(hipEventRecord(ctx->done_event, st));
         return ABFT_OK;
     }

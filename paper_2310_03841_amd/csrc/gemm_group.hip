@@ -463,7 +463,7 @@ static bool takes_big(int dt, bool transB, const GroupArgs &g)
            fills_chip(g.M, g.groups, g.N);
 }
 
-hipError_t launch_group(int dt, int ot, bool protect, bool transB, GroupArgs &g, hipStream_t st)
+hipError_t launch_group(int dt, int ot, bool protect, bool transB, GroupArgs &g, const uint32_t *b_max, const Verdict *v, hipStream_t st)
 {
     if (protect) {
         g.pass_win = (int)ceil_div((long)g.K * elem_size(dt), PASS_BYTES);
@@ -471,6 +471,10 @@ hipError_t launch_group(int dt, int ot, bool protect, bool transB, GroupArgs &g,
         const long units = row_tiles(g.M, g.groups, 4 * PASS_ROWS) * g.pass_win;
         if (units > MAX_GRID_X) return hipErrorInvalidValue;
         g.n_pass = (int)ceil_div(units, 8) * 8;
+    }
+    if (group_takes_few(dt, transB, g)) {
+        const float tau = !v ? 0.f : v->tau_override_cols > 0.f ? v->tau_override_cols : v->tau_override;
+        return launch_group_few(dt, ot, protect, g, b_max, tau, st);
     }
     if (takes_big(dt, transB, g)) {
         if (dt != DT_I8) g.cc_acc = g.rc_acc = nullptr;          // these tiles add to the sums themselves

@@ -122,4 +122,8 @@ template <int BM> __device__ __forceinline__ bool find_tile(const GroupArgs &g, 
     return true;
 }
 
+// Groups of few rows (gemm_group_few.hip), whose kernel checks the columns itself: cc_obs then holds a mark for each that disagrees.
+bool group_takes_few(int dt, bool transB, const GroupArgs &g);
+hipError_t launch_group_few(int dt, int ot, bool protect, GroupArgs &g, const uint32_t *b_max, float tau_cols, hipStream_t st);
+
 }  // namespace abft

@@ -25,7 +25,10 @@ struct GroupCheckArgs {
 
 constexpr int GCHK_KN_LANES = 4;          // chunk columns of a unit over a B stored K x N (64 lanes run along k)
 
-template <int DT, int RW, bool TRANSB>
+// What is left to do of the columns: their predictions from B stored N x K or K x N, or nothing but to write down what the product's kernel marked.
+enum { COLS_NK, COLS_KN, COLS_MARKED };
+
+template <int DT, int RW, int COLS>
 __global__ __launch_bounds__(256) void group_check_kernel(GroupCheckArgs f)
 {
     using T = Traits<DT>;
@@ -62,6 +65,14 @@ __global__ __launch_bounds__(256) void group_check_kernel(GroupCheckArgs f)
         return;
     }
     u -= f.row_units;
+    if constexpr (COLS == COLS_MARKED) {
+        const int o = u * 256 + tid;                             // over all groups
+        const bool fl = o < f.N * f.groups && f.cc_obs[o] != 0u;
+        if (o < f.N * f.groups) f.col_flag[o] = fl ? 1 : 0;
+        const unsigned nf = __popcll(__ballot(fl));
+        if (nf && lane == 0) report_flags(f.counts, 1, nf);
+        return;
+    }
     const int e = u / f.col_units, unit = u - e * f.col_units;
     const int N = f.N, K = f.K;
     int first, rows;
@@ -71,7 +82,7 @@ __global__ __launch_bounds__(256) void group_check_kernel(GroupCheckArgs f)
     bool mine_ok = false;
     int n = 0;
     acc_t pred = T::zero();
-    if constexpr (TRANSB) {
+    if constexpr (COLS == COLS_NK) {
         const int row0 = (unit * 4 + wave) * RW;
         n = row0 + lane;
         mine_ok = lane < RW && n < N;
@@ -146,15 +157,17 @@ hipError_t launch_group_check(int dt, const GroupArgs &g, bool transB, const Wor
     f.row_flag = v.row_flag; f.col_flag = v.col_flag; f.counts = v.counts;
     f.zero_ptr = end.zero_ptr; f.zero_words = end.zero_ptr ? end.zero_words : 0;
     f.zero2_ptr = end.zero2_ptr; f.zero2_words = end.zero2_ptr ? end.zero2_words : 0;
+    const bool marked = group_takes_few(dt, transB, g);
     const int per = transB ? 4 * RW : GCHK_KN_LANES * (16 / elem_size(dt));
     f.row_units = (g.M + 255) / 256;
     f.col_units = (g.N + per - 1) / per;
-    const long units = f.row_units + (long)f.col_units * g.groups;
-    if (units > MAX_GRID_X) return hipErrorInvalidValue;
+    const long cols = (long)g.N * g.groups, units = f.row_units + (marked ? (cols + 255) / 256 : (long)f.col_units * g.groups);
+    if (units > MAX_GRID_X || cols > 0x7FFFFFFFL) return hipErrorInvalidValue;
     const dim3 grid((unsigned)units);
 #define GROUP_CHECK(DT) \
-    if (transB) hipLaunchKernelGGL((group_check_kernel<DT, RW, true>), grid, dim3(256), 0, st, f); \
-    else        hipLaunchKernelGGL((group_check_kernel<DT, RW, false>), grid, dim3(256), 0, st, f)
+    if (marked)      hipLaunchKernelGGL((group_check_kernel<DT, RW, COLS_MARKED>), grid, dim3(256), 0, st, f); \
+    else if (transB) hipLaunchKernelGGL((group_check_kernel<DT, RW, COLS_NK>), grid, dim3(256), 0, st, f); \
+    else             hipLaunchKernelGGL((group_check_kernel<DT, RW, COLS_KN>), grid, dim3(256), 0, st, f)
     switch (dt) {
     case DT_I8:   GROUP_CHECK(DT_I8); break;
     case DT_BF16: GROUP_CHECK(DT_BF16); break;

@@ -163,12 +163,21 @@ BIG = [
     ([0, 8192], 512, 384, True),
     ([0, 4000, 12600], 2056, 384, True),
 ]
+# Few rows to a group: one and sixteen and seventeen of them, groups of many among them, one piece of K and many, parts of a piece, and both widths of tiles
+FEW = [
+    ([0, 1], 4096, 1024, True),
+    ([0, 16, 17, 49, 49, 50, 64], 100, 4104, True),
+    ([1, 2, 3, 20, 20, 21], 33, 50, True),
+    (list(range(0, 71)), 264, 136, True),
+    ([0] * 40 + [170] + [171] * 23, 264, 200, True),
+    ([0, 13], 1000, 713, True),
+]
 TYPES = [("i8", None), ("i8", "bf16"), ("i8", "f16"), ("bf16", None), ("f16", None)]
 
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype,out", TYPES)
-@pytest.mark.parametrize("ends,N,K,trans_b", SHAPES + BIG)
+@pytest.mark.parametrize("ends,N,K,trans_b", SHAPES + BIG + FEW)
 def test_grouped_matches_plain(dtype, out, ends, N, K, trans_b):
     print(f"case {dtype} {out} {ends[:8]} {N} {K} {trans_b}", flush=True)
     p = Group(dtype, ends, N, K, trans_b, M=ends[-1] + 5, out=out, bias=bool(N % 2), seed=N + K)
@@ -234,7 +243,7 @@ def flips(p, g, i, j, bit, mode):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype,out", TYPES)
-@pytest.mark.parametrize("ends,N,K,trans_b", [([0, 3, 3, 8], 70, 96, True), ([0, 130, 200, 290], 200, 136, False), ([0, 600, 1500], 520, 384, True),
+@pytest.mark.parametrize("ends,N,K,trans_b", [([0, 3, 3, 8], 70, 96, True), ([0, 20, 21, 21, 22, 23], 70, 600, True), ([0, 130, 200, 290], 200, 136, False), ([0, 600, 1500], 520, 384, True),
                                                ([0, 1300, 1300, 4200], 1030, 384, True), ([0, 1300, 1300, 4200], 1030, 384, False)])
 def test_a_flip_in_an_accumulator_is_found(dtype, out, ends, N, K, trans_b):
     p = Group(dtype, ends, N, K, trans_b, M=ends[-1], out=out, seed=5)
@@ -243,7 +252,7 @@ def test_a_flip_in_an_accumulator_is_found(dtype, out, ends, N, K, trans_b):
             rows = p.ends[g + 1] - p.ends[g]
             if not rows:
                 continue
-            i, j = min(rows - 1, p.M // p.groups - 1), N - 1
+            i, j = min(rows, max(1, p.M // p.groups)) - 1, N - 1
             flips(p, g, i, j, 30, ab.ABFT_DETECT)
             rf, cf = p.row_flag.nonzero().flatten().tolist(), p.col_flag.nonzero().flatten().tolist()
             assert rf == [p.ends[g] + i] and cf == [g * N + j], (g, rf, cf)
@@ -276,7 +285,7 @@ def test_a_weight_that_changed_behind_its_encoding_shows_in_rows(dtype, out):
 @pytest.mark.gpu
 @pytest.mark.parametrize("value", [float("inf"), float("nan")])
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("ends,N,K,trans_b", [([0, 2, 5], 40, 72, True), ([0, 70, 190], 136, 200, False), ([0, 300, 700], 520, 512, True), ([0, 1300, 4200], 1030, 512, True),
+@pytest.mark.parametrize("ends,N,K,trans_b", [([0, 2, 5], 40, 72, True), ([0, 20, 31], 40, 712, True), ([0, 70, 190], 136, 200, False), ([0, 300, 700], 520, 512, True), ([0, 1300, 4200], 1030, 512, True),
                                                ([0, 1300, 4200], 1030, 512, False)])
 def test_values_that_are_not_finite_stay_in_their_rows_and_columns(dtype, value, ends, N, K, trans_b):
     p = Group(dtype, ends, N, K, trans_b, seed=7)
