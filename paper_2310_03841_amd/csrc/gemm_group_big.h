@@ -49,37 +49,6 @@ template <int OT, int GROUP> struct GroupSource {
 
 struct BigTile { int e, first, rows, m0, tn; bool tall; };
 
-// The rows of a lane's group, of up to 64: read once and kept, since a trip to memory ahead of every tile is 1 us of its 15 to 30.
-struct GroupLane { int first, rows; };
-__device__ __forceinline__ GroupLane group_lane(const GroupArgs &g, int e)
-{
-    GroupLane l = {0, 0};
-    if (e < g.groups) group_rows(g.offsets, g.M, e, &l.first, &l.rows);
-    return l;
-}
-
-// The group that item L of a list belongs to, and its place among that group's; of a group of so many rows there are of(rows) items.
-template <typename OF> __device__ __forceinline__ bool big_group(const GroupArgs &g, GroupLane mine, const OF &of, int *L, BigTile *o)
-{
-    const int lane = threadIdx.x & 63;
-    int base = 0;
-    for (int e0 = 0; e0 < g.groups; e0 += 64) {
-        if (g.groups > 64) mine = group_lane(g, e0 + lane);
-        const int n = of(mine.rows), upto = base + wave_prefix(n);
-        const uint64_t behind = __ballot(upto > *L);
-        if (behind) {
-            const int l = __builtin_ctzll(behind);
-            o->e = e0 + l;
-            *L -= __builtin_amdgcn_readlane(upto - n, l);
-            o->first = __builtin_amdgcn_readlane(mine.first, l);
-            o->rows = __builtin_amdgcn_readlane(mine.rows, l);
-            return true;
-        }
-        base = __builtin_amdgcn_readlane(upto, 63);
-    }
-    return false;
-}
-
 // Tile t of the list: false, there is none, and *tiles are all.
 template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const GroupArgs &g, const GroupLane &kept, int t, int wgs, BigTile *o, int *tiles)
 {
@@ -135,7 +104,7 @@ template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const G
         L -= o->e * per;
         group_rows(g.offsets, g.M, o->e, &o->first, &o->rows);
     } else {
-        const bool found = big_group(g, kept, [&](int rows) { return (left_over ? small_of(rows) : tall_of(rows)) * tiles_n; }, &L, o);
+        const bool found = find_group(g, kept, [&](int rows) { return (left_over ? small_of(rows) : tall_of(rows)) * tiles_n; }, &L, &o->e, &o->first, &o->rows);
         if (!found) return false;
     }
     const int height = GROUP == BIG_DEPTH ? g.K : o->rows;
@@ -190,7 +159,7 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void gemm_group_big_kernel(GroupAr
         for (int p = (int)blockIdx.x - busy; p >= 0 && p < passes; p += free) {
             BigTile b;
             int L = p;
-            if (!big_group(a, kept, passes_of, &L, &b)) break;
+            if (!find_group(a, kept, passes_of, &L, &b.e, &b.first, &b.rows)) break;
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             const int row = L / a.pass_win;
             group_pass<DT, FAST_WAVES>(a, b.e, b.first, b.rows, row * ROWS, L - row * a.pass_win, smem);

@@ -64,50 +64,82 @@ __global__ __launch_bounds__(256) void gemm_group_few_kernel(FewArgs f)
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) brow[nb] = g.B + ((long)t.e * g.sB + (long)min(n0 + 16 * nb + i16, N - 1) * g.ldb) * ES;
 
-    // ---- e^T A of the tile's rows: integers, |sum| <= 2^11, as two digits of 8 bits, a chunk's sixteen side by side; else words
+    // ---- e^T A of the tile's rows: integers, |sum| <= 2^11, as two digits of 8 bits, a chunk's sixteen side by side; else words.  Four threads to a
+    // chunk, every fourth row to each.
     uint8_t *const sums = smem + f.sums_off;
     float *const tops = reinterpret_cast<float *>(smem + few_part_bytes<DT, NB>() - 16);
-    if constexpr (PROT) {
-        float top = 0.f;
-        for (int c = tid; c < nch; c += 256) {
-            i32x4 x[16];
+    i32x4 ax[4];
+    float top = 0.f;
+    auto load_rows = [&](int c) __attribute__((always_inline)) {
+        const uint8_t *at = At + (long)min(c, nch - 1) * 16;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) x[r] = *reinterpret_cast<const i32x4 *>(At + (long)min(r, rows - 1) * g.lda * ES + (long)c * 16);
+        for (int j = 0; j < 4; ++j) ax[j] = *reinterpret_cast<const i32x4 *>(at + (long)min(4 * j + (tid & 3), rows - 1) * g.lda * ES);
+    };
+    auto sum_rows = [&](int c) __attribute__((always_inline)) {
+        const int keep = K * ES - c * 16;
+        if constexpr (T::IS_INT) {
+            // 16-bit fields: bytes plus 128, so that no sum is negative
+            uint32_t even[4] = {0, 0, 0, 0}, odd[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const i32x4 w = mask_chunk(ax[j], keep);
+                const bool in = 4 * j + (tid & 3) < rows;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t x = in ? (uint32_t)w[i] ^ 0x80808080u : 0u;
+                    even[i] += x & 0x00FF00FFu;
+                    odd[i] += x >> 8 & 0x00FF00FFu;
+                }
+            }
+            // s + 128 + 2^12 in a field: its low byte is the low digit plus 128, what is left the high one plus 16
+            const uint32_t back = (uint32_t)(4096 + 128 - 128 * rows) * 0x10001u;
+            i32x4 lo, hi;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t digits[2][2];
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                    int v = (int)(o ? odd[i] : even[i]);
+                    v += dpp_mov<0xB1>(v);                       // lane ^ 1
+                    v += dpp_mov<0x4E>(v);                       // lane ^ 2
+                    const uint32_t u = (uint32_t)v + back;
+                    digits[o][0] = (u & 0x00FF00FFu) ^ 0x00800080u;
+                    digits[o][1] = ((u >> 8 & 0x00FF00FFu) + 0x00F000F0u) & 0x00FF00FFu;
+                }
+                lo[i] = (int)(digits[0][0] | digits[1][0] << 8);
+                hi[i] = (int)(digits[0][1] | digits[1][1] << 8);
+            }
+            if ((tid & 3) == 0 && c < nch) {
+                *reinterpret_cast<i32x4 *>(sums + c * 32) = lo;
+                *reinterpret_cast<i32x4 *>(sums + c * 32 + 16) = hi;
+            }
+        } else {
             acc_t s[CE];
 #pragma unroll
             for (int q = 0; q < CE; ++q) s[q] = T::zero();
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const i32x4 w = r < rows ? mask_chunk(x[r], K * ES - c * 16) : i32x4{0, 0, 0, 0};
+            for (int j = 0; j < 4; ++j) {
+                const i32x4 w = 4 * j + (tid & 3) < rows ? mask_chunk(ax[j], keep) : i32x4{0, 0, 0, 0};
 #pragma unroll
                 for (int q = 0; q < CE; ++q) {
                     const acc_t v = T::elem(w, q);
                     s[q] = add_t(s[q], v);
-                    if constexpr (!T::IS_INT) top = fmaxf(top, fabsf((float)v));
+                    if (c < nch) top = fmaxf(top, fabsf((float)v));
                 }
             }
-            if constexpr (T::IS_INT) {
-                uint32_t lo[4] = {0, 0, 0, 0}, hi[4] = {0, 0, 0, 0};
 #pragma unroll
-                for (int q = 0; q < CE; ++q) {
-                    const int d = (int)(int8_t)(uint32_t)s[q];
-                    lo[q >> 2] |= ((uint32_t)d & 0xFFu) << (8 * (q & 3));
-                    hi[q >> 2] |= ((uint32_t)(((int)s[q] - d) >> 8) & 0xFFu) << (8 * (q & 3));
-                }
-                *reinterpret_cast<i32x4 *>(sums + c * 32) = i32x4{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3]};
-                *reinterpret_cast<i32x4 *>(sums + c * 32 + 16) = i32x4{(int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-            } else {
+            for (int q = 0; q < CE; ++q) {
+                s[q] = add_t(s[q], dpp_get<0xB1>(s[q]));
+                s[q] = add_t(s[q], dpp_get<0x4E>(s[q]));
+            }
+            if ((tid & 3) == 0 && c < nch) {
 #pragma unroll
                 for (int q4 = 0; q4 < CE / 4; ++q4)
                     *reinterpret_cast<i32x4 *>(sums + c * 32 + 16 * q4) =
                         i32x4{(int)as_word(s[4 * q4]), (int)as_word(s[4 * q4 + 1]), (int)as_word(s[4 * q4 + 2]), (int)as_word(s[4 * q4 + 3])};
             }
         }
-        if constexpr (!T::IS_INT) {
-            top = wave_max(top);
-            if (lane == 0) tops[wave] = top;
-        }
-    }
+    };
 
     // scales of what this wave stores in the end (lane: row lane & 15, columns 4 (lane >> 4) + i of block `wave`), on their way meanwhile
     const int c0 = n0 + 16 * wave + 4 * piece;
@@ -129,11 +161,11 @@ __global__ __launch_bounds__(256) void gemm_group_few_kernel(FewArgs f)
     acc_t pred[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) { acc[nb] = acc4_zero<DT>(); pred[nb] = T::zero(); }
-    bool first = true;
-    for (int p0 = wave; p0 < pairs; p0 += 4 * U) {
-        i32x4 a[U][2], b[U][2][NB];
+    i32x4 a[U][2], b[U][2][NB];
+    auto load = [&](int p0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            if (u && p0 + 4 * u >= pairs) break;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const long at = (long)min((p0 + 4 * u) * 8 + 4 * h + piece, nch - 1) * 16;
@@ -141,12 +173,33 @@ __global__ __launch_bounds__(256) void gemm_group_few_kernel(FewArgs f)
                 for (int nb = 0; nb < NB; ++nb) b[u][h][nb] = *reinterpret_cast<const i32x4 *>(brow[nb] + at);
                 a[u][h] = *reinterpret_cast<const i32x4 *>(arow + at);
             }
-        if (PROT && first) __syncthreads();                      // the sums are in place
-        first = false;
-        // past the end of K nothing is multiplied, whatever both hold there
-        if ((p0 + 4 * (U - 1)) * 8 + 8 > K * ES / 16) {
+        }
+    };
+    // the loads of the last sums and of the first pieces go out together
+    if constexpr (PROT) {
+        int c = tid >> 2;
+        for (; c + 64 < nch + (tid >> 2); c += 64) {
+            load_rows(c);
+            sum_rows(c);
+        }
+        load_rows(c);
+        load(wave);
+        sum_rows(c);
+        if constexpr (!T::IS_INT) {
+            top = wave_max(top);
+            if (lane == 0) tops[wave] = top;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    } else {
+        load(wave);
+    }
+    for (int p0 = wave; p0 < pairs; p0 += 4 * U) {
+        if (p0 != wave) load(p0);
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            if (u && p0 + 4 * u >= pairs) break;
+            // past the end of K nothing is multiplied, whatever both hold there
+            if ((p0 + 4 * u) * 8 + 8 > K * ES / 16) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int keep = K * ES - ((p0 + 4 * u) * 8 + 4 * h + piece) * 16;
@@ -154,9 +207,7 @@ __global__ __launch_bounds__(256) void gemm_group_few_kernel(FewArgs f)
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) b[u][h][nb] = mask_chunk(b[u][h][nb], keep);
                 }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
+            }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -182,8 +233,8 @@ __global__ __launch_bounds__(256) void gemm_group_few_kernel(FewArgs f)
                     }
                 }
             }
+        }
     }
-    if (PROT && first) __syncthreads();                          // (a wave without a piece)
 
     // ---- the waves' sums, in LDS: [wave][nb][lane] of four, then [wave][nb][column] predictions
     acc_t *const ppart = reinterpret_cast<acc_t *>(smem + 4 * NB * 64 * 16);

@@ -68,6 +68,38 @@ __device__ __forceinline__ int wave_prefix(int v)
     return v;
 }
 
+// The rows of a lane's group, of up to 64: read once and kept, since a trip to memory ahead of every tile is 1 us of its 15 to 30.
+struct GroupLane { int first, rows; };
+__device__ __forceinline__ GroupLane group_lane(const GroupArgs &g, int e)
+{
+    GroupLane l = {0, 0};
+    if (e < g.groups) group_rows(g.offsets, g.M, e, &l.first, &l.rows);
+    return l;
+}
+
+// The group that item L of a list belongs to, and its place among that group's; of a group of so many rows there are of(rows) items.
+template <typename OF>
+__device__ __forceinline__ bool find_group(const GroupArgs &g, GroupLane mine, const OF &of, int *L, int *e, int *first, int *rows)
+{
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int e0 = 0; e0 < g.groups; e0 += 64) {
+        if (g.groups > 64) mine = group_lane(g, e0 + lane);
+        const int n = of(mine.rows), upto = base + wave_prefix(n);
+        const uint64_t behind = __ballot(upto > *L);
+        if (behind) {
+            const int l = __builtin_ctzll(behind);
+            *e = e0 + l;
+            *L -= __builtin_amdgcn_readlane(upto - n, l);
+            *first = __builtin_amdgcn_readlane(mine.first, l);
+            *rows = __builtin_amdgcn_readlane(mine.rows, l);
+            return true;
+        }
+        base = __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
 struct GroupTile { int e, tm, tn, first, rows; };
 
 // The tile of workgroup `bid` of those that take tiles, of BM rows each: false, there is none for it.  Every wave finds it by itself, 64 groups at
@@ -76,48 +108,24 @@ struct GroupTile { int e, tm, tn, first, rows; };
 template <int BM> __device__ __forceinline__ bool find_tile(const GroupArgs &g, int tiles_n, uint32_t inv, int bid, GroupTile *t)
 {
     const int lane = threadIdx.x & 63;
-    auto tiles_of = [&](int e) __attribute__((always_inline)) {
-        int first = 0, rows = 0;
-        if (e < g.groups) group_rows(g.offsets, g.M, e, &first, &rows);
-        return (rows + BM - 1) / BM * tiles_n;
-    };
-    auto at = [&](int nb) __attribute__((always_inline)) {                 // -1: more workgroups than tiles
-        const int q = nb >> 3, r = nb & 7, xcd = bid & 7, i = bid >> 3;
-        return i < q + (xcd < r ? 1 : 0) ? xcd * q + (xcd < r ? xcd : r) + i : -1;
-    };
-    int L;
+    auto tiles_of = [&](int rows) __attribute__((always_inline)) { return (rows + BM - 1) / BM * tiles_n; };
+    GroupLane mine = {0, 0};
+    int total = 0;
     if (g.groups == 1) {
         group_rows(g.offsets, g.M, 0, &t->first, &t->rows);
         t->e = 0;
-        L = at((t->rows + BM - 1) / BM * tiles_n);
-        if (L < 0) return false;
+        total = tiles_of(t->rows);
     } else {
-        int total = 0, mine = 0;
         for (int e0 = 0; e0 < g.groups; e0 += 64) {
-            mine = tiles_of(e0 + lane);
-            total += wave_sum(mine);
+            mine = group_lane(g, e0 + lane);
+            total += wave_sum(tiles_of(mine.rows));
         }
-        L = at(__builtin_amdgcn_readfirstlane(total));
-        if (L < 0) return false;
-        int base = 0, e = -1;
-        for (int e0 = 0; e0 < g.groups; e0 += 64) {
-            if (g.groups > 64) mine = tiles_of(e0 + lane);
-            const int upto = base + wave_prefix(mine);
-            const uint64_t behind = __ballot(upto > L);
-            if (behind) {
-                const int l = __builtin_ctzll(behind);
-                e = e0 + l;
-                L -= __builtin_amdgcn_readlane(upto - mine, l);
-                break;
-            }
-            base = __builtin_amdgcn_readlane(upto, 63);
-        }
-        if (e < 0) return false;
-        t->e = e;
-        group_rows(g.offsets, g.M, e, &t->first, &t->rows);
-        t->first = __builtin_amdgcn_readfirstlane(t->first);
-        t->rows = __builtin_amdgcn_readfirstlane(t->rows);
+        total = __builtin_amdgcn_readfirstlane(total);
     }
+    const int q = total >> 3, r = total & 7, xcd = bid & 7, i = bid >> 3;
+    if (i >= q + (xcd < r ? 1 : 0)) return false;                // more workgroups than tiles
+    int L = xcd * q + (xcd < r ? xcd : r) + i;
+    if (g.groups > 1 && !find_group(g, mine, tiles_of, &L, &t->e, &t->first, &t->rows)) return false;
     tile_at(L, (t->rows + BM - 1) / BM, tiles_n, inv, &t->tm, &t->tn);
     return true;
 }
