@@ -132,6 +132,9 @@ template <int BM> __device__ __forceinline__ bool find_tile(const GroupArgs &g, 
 
 // Groups of few rows (gemm_group_few.hip), whose kernel checks the columns itself: cc_obs then holds a mark for each that disagrees.
 bool group_takes_few(int dt, bool transB, const GroupArgs &g);
+// Its shares of the observed sums of rows, for every sixteen columns one after the other, [M] words each: they take the place of the sums in doubles, of which it
+// keeps none: 16 rows to a group make at most M (N / 16 + 1) <= groups N + M words.
+inline uint32_t *group_few_shares(const GroupArgs &g) { return reinterpret_cast<uint32_t *>(g.cc_acc); }
 hipError_t launch_group_few(int dt, int ot, bool protect, GroupArgs &g, const uint32_t *b_max, float tau_cols, hipStream_t st);
 
 }  // namespace abft

@@ -1,5 +1,7 @@
 // Behind a protected product over groups (gemm_group.hip), which has left e^T A and max|A| of each group, the row predictions and the observed
 // sums: the column prediction of each group, a B from one read of its matrix, the comparisons, flags and counts (Sec. III-B.1, item (2)).
+#include <type_traits>
+
 #include "abft_device.h"
 #include "check_dots.h"
 #include "group_args.h"
@@ -15,10 +17,11 @@ struct GroupCheckArgs {
     uint32_t *cc_obs, *rc_obs, *cc_pred;
     const uint32_t *rc_pred;
     const double *cc_acc, *rc_acc;
+    const uint32_t *shares;               // COLS_MARKED: of the observed sums of rows, [(N + 15) / 16][M]
     float tau_override, tau_override_cols;
     uint8_t *row_flag, *col_flag;
     uint32_t *counts;
-    int row_units, col_units;             // of 256 rows each; per group
+    int row_units, col_units;             // of 256 rows each, COLS_MARKED: four; per group
     uint32_t *zero_ptr, *zero2_ptr;       // regions for calls to come, which every workgroup helps to clear
     size_t zero_words, zero2_words;
 };
@@ -51,6 +54,28 @@ __global__ __launch_bounds__(256) void group_check_kernel(GroupCheckArgs f)
         return w;
     };
     int u = blockIdx.x;
+    if (COLS == COLS_MARKED && u < f.row_units) {
+        // a wave to a row: its shares, in doubles where they round
+        const int r = u * 4 + wave, n = (f.N + 15) / 16;
+        if (r >= f.M) return;
+        int end;
+        const int e = group_of(f.offsets, f.M, f.groups, r, &end);
+        bool fl = false;
+        if (e >= 0) {
+            typename std::conditional<T::IS_INT, int, double>::type s = 0;
+            for (int i = lane; i < n; i += 64) s += from_word<acc_t>(f.shares[(long)i * f.M + r]);
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) s += __shfl_xor(s, d);
+            const uint32_t obs = as_word((acc_t)s);
+            if (lane == 0) f.rc_obs[r] = obs;
+            fl = mismatch<T::IS_INT>(obs, f.rc_pred[r], tolerance(e));
+        }
+        if (lane == 0) {
+            f.row_flag[r] = fl ? 1 : 0;
+            if (fl) report_flags(f.counts, 0, 1u);
+        }
+        return;
+    }
     if (u < f.row_units) {
         const int r = u * 256 + tid;
         bool fl = false;
@@ -152,14 +177,14 @@ hipError_t launch_group_check(int dt, const GroupArgs &g, bool transB, const Wor
     f.M = g.M; f.N = g.N; f.K = g.K; f.groups = g.groups; f.ldb = g.ldb; f.sB = g.sB;
     f.a_sum = g.a_sum; f.a_max = g.a_max; f.b_max = w.b_max;
     f.cc_obs = g.cc_obs; f.rc_obs = g.rc_obs; f.cc_pred = w.cc_pred; f.rc_pred = g.rc_pred;
-    f.cc_acc = g.cc_acc; f.rc_acc = g.rc_acc;
+    f.cc_acc = g.cc_acc; f.rc_acc = g.rc_acc; f.shares = group_few_shares(g);
     f.tau_override = v.tau_override; f.tau_override_cols = v.tau_override_cols;
     f.row_flag = v.row_flag; f.col_flag = v.col_flag; f.counts = v.counts;
     f.zero_ptr = end.zero_ptr; f.zero_words = end.zero_ptr ? end.zero_words : 0;
     f.zero2_ptr = end.zero2_ptr; f.zero2_words = end.zero2_ptr ? end.zero2_words : 0;
     const bool marked = group_takes_few(dt, transB, g);
     const int per = transB ? 4 * RW : GCHK_KN_LANES * (16 / elem_size(dt));
-    f.row_units = (g.M + 255) / 256;
+    f.row_units = marked ? (g.M + 3) / 4 : (g.M + 255) / 256;
     f.col_units = (g.N + per - 1) / per;
     const long cols = (long)g.N * g.groups, units = f.row_units + (marked ? (cols + 255) / 256 : (long)f.col_units * g.groups);
     if (units > MAX_GRID_X || cols > 0x7FFFFFFFL) return hipErrorInvalidValue;

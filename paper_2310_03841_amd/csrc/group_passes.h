@@ -16,8 +16,8 @@ constexpr int PASS_BYTES = 1024;             // of a row
 // LDS: each wave's sums of the window's columns, and a maximum to a wave
 template <int DT, int WAVES> constexpr int group_pass_lds() { return WAVES * PASS_BYTES / Traits<DT>::ES * 4 + WAVES * 4; }
 
-// Rows row0 .. of group e (which has `rows` from `first` on), WAVES * PASS_ROWS at most; window win.
-template <int DT, int WAVES> __device__ __forceinline__ void group_pass(const GroupArgs &g, int e, int first, int rows, int row0, int win, uint8_t *smem)
+// Rows row0 .. of group e (which has `rows` from `first` on), WAVES * PASS_ROWS at most; window win.  SUMS: e^T A is wanted too.
+template <int DT, int WAVES, bool SUMS = true> __device__ __forceinline__ void group_pass(const GroupArgs &g, int e, int first, int rows, int row0, int win, uint8_t *smem)
 {
     using T = Traits<DT>;
     typedef typename T::acc_t acc_t;
@@ -63,7 +63,8 @@ template <int DT, int WAVES> __device__ __forceinline__ void group_pass(const Gr
                     if constexpr (decltype(narrow_c)::value) dot[u] += __mul24((int)v, (int)b[q]);
                     // (past the end of K nothing is multiplied: b may hold what is not finite)
                     else if (T::IS_INT || q * ES < keep) dot[u] = add_t(dot[u], mul_t(v, b[q]));
-                    if constexpr (T::IS_INT) col[q] = __builtin_amdgcn_sdot4(w[q >> 2], 1 << (8 * (q & 3)), col[q], false);
+                    if constexpr (!SUMS) {}
+                    else if constexpr (T::IS_INT) col[q] = __builtin_amdgcn_sdot4(w[q >> 2], 1 << (8 * (q & 3)), col[q], false);
                     else col[q] = add_t(col[q], v);
                     if constexpr (!T::IS_INT) top = fmaxf(top, fabsf((float)v));
                 }
@@ -73,7 +74,7 @@ template <int DT, int WAVES> __device__ __forceinline__ void group_pass(const Gr
         else add(std::false_type{});
     }
 #pragma unroll
-    for (int q4 = 0; q4 < CE / 4; ++q4)
+    for (int q4 = 0; q4 < CE / 4 && SUMS; ++q4)
         *reinterpret_cast<i32x4 *>(red + wave * COLS + lane * CE + 4 * q4) =
             i32x4{(int)as_word(col[4 * q4]), (int)as_word(col[4 * q4 + 1]), (int)as_word(col[4 * q4 + 2]), (int)as_word(col[4 * q4 + 3])};
     if constexpr (!T::IS_INT) {
@@ -89,7 +90,7 @@ template <int DT, int WAVES> __device__ __forceinline__ void group_pass(const Gr
     if (lane < PASS_ROWS && r0 + lane < rows) atomic_add_word(g.rc_pred + first + r0 + lane, mine);
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // (over LDS alone: not for the additions above)
 #pragma unroll
-    for (int c = tid; c < COLS; c += 64 * WAVES) {
+    for (int c = tid; c < COLS && SUMS; c += 64 * WAVES) {
         if (k0 + c < K) {
             acc_t s = red[c];
 #pragma unroll
