@@ -63,6 +63,7 @@ __device__ __forceinline__ void fast_tile(const GemmArgs &g, SRC source, uint8_t
     constexpr int MI = L::MI, NI = L::NI, NMF = MI * NI, NFR = MI + NI;
     constexpr int NF = L::NF, NR = L::NR, NLD = L::NLD;
     constexpr bool PROT = MODE != FAST_PLAIN, OWN = MODE == FAST_OWN;
+    static_assert(!AT || BT, "A's rows of k come with B's");
     static_assert(!(AT || BT) || (ES == 2 && !OWN), "rows of k are turned 16 bits at a time, and not reduced");
 
     const int tid = tile_thread_index(), lane = tid & 63;
@@ -156,27 +157,43 @@ __device__ __forceinline__ void fast_tile(const GemmArgs &g, SRC source, uint8_t
         constexpr int t = decltype(t_c)::value, set = t & 1, HALF = 4 * SLAB_BYTES, STEP = 16 * SLAB_BYTES * t;
         [[maybe_unused]] const uint32_t base = (uint32_t)(uintptr_t)lds + turn_at;
         auto put = [&](i32x4 &f, const i32x2 &x, const i32x2 &y) __attribute__((always_inline)) { f = i32x4{x[0], x[1], y[0], y[1]}; };
-        if constexpr (BT) {
-            const uint32_t p = base + (L::ring3(L::load_of_b(0)) ? b.f : b.r) + L::at(L::load_of_b(0)) + wn * L::UNIT, p1 = p ^ 64u;
+        const uint32_t pb = base + (L::ring3(L::load_of_b(0)) ? b.f : b.r) + L::at(L::load_of_b(0)) + wn * L::UNIT;
+        const uint32_t pa = base + (L::ring3(L::load_of_a(0)) ? b.f : b.r) + L::at(L::load_of_a(0)) + wm * (MI / 2) * L::UNIT;
+#define FAST_TURN(O, P) "ds_read_b64_tr_b16 %" O ", %" P
+        if constexpr (AT && MI == 4) {
+            i32x2 h[12];
+            asm volatile(FAST_TURN("0", "12") " offset:%18\n\t" FAST_TURN("1", "12") " offset:%19\n\t" FAST_TURN("2", "13") " offset:%18\n\t" FAST_TURN("3", "13") " offset:%19\n\t"
+                         FAST_TURN("4", "14") " offset:%18\n\t" FAST_TURN("5", "14") " offset:%19\n\t" FAST_TURN("6", "15") " offset:%18\n\t" FAST_TURN("7", "15") " offset:%19\n\t"
+                         FAST_TURN("8", "16") " offset:%18\n\t" FAST_TURN("9", "16") " offset:%19\n\t" FAST_TURN("10", "17") " offset:%18\n\t" FAST_TURN("11", "17") " offset:%19\n\t"
+                         "s_waitcnt lgkmcnt(0)"
+                         : "=&v"(h[0]), "=&v"(h[1]), "=&v"(h[2]), "=&v"(h[3]), "=&v"(h[4]), "=&v"(h[5]), "=&v"(h[6]), "=&v"(h[7]), "=&v"(h[8]), "=&v"(h[9]), "=&v"(h[10]),
+                           "=&v"(h[11])
+                         : "v"(pb), "v"(pb ^ 64u), "v"(pa), "v"(pa ^ 64u), "v"(pa + L::UNIT), "v"((pa ^ 64u) + L::UNIT), "n"(STEP), "n"(STEP + HALF) : "memory");
+            put(fb[set][0], h[0], h[1]);
+            put(fb[set][1], h[2], h[3]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) put(fa[set][i], h[4 + 2 * i], h[5 + 2 * i]);
+        } else if constexpr (AT) {
+            static_assert(MI == 2);
+            i32x2 h[8];
+            asm volatile(FAST_TURN("0", "8") " offset:%12\n\t" FAST_TURN("1", "8") " offset:%13\n\t" FAST_TURN("2", "9") " offset:%12\n\t" FAST_TURN("3", "9") " offset:%13\n\t"
+                         FAST_TURN("4", "10") " offset:%12\n\t" FAST_TURN("5", "10") " offset:%13\n\t" FAST_TURN("6", "11") " offset:%12\n\t" FAST_TURN("7", "11") " offset:%13\n\t"
+                         "s_waitcnt lgkmcnt(0)"
+                         : "=&v"(h[0]), "=&v"(h[1]), "=&v"(h[2]), "=&v"(h[3]), "=&v"(h[4]), "=&v"(h[5]), "=&v"(h[6]), "=&v"(h[7])
+                         : "v"(pb), "v"(pb ^ 64u), "v"(pa), "v"(pa ^ 64u), "n"(STEP), "n"(STEP + HALF) : "memory");
+            put(fb[set][0], h[0], h[1]);
+            put(fb[set][1], h[2], h[3]);
+            put(fa[set][0], h[4], h[5]);
+            put(fa[set][1], h[6], h[7]);
+        } else {
             i32x2 h[4];
-            asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
-                         "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\ts_waitcnt lgkmcnt(0)"
-                         : "=&v"(h[0]), "=&v"(h[1]), "=&v"(h[2]), "=&v"(h[3]) : "v"(p), "v"(p1), "n"(STEP), "n"(STEP + HALF) : "memory");
+            asm volatile(FAST_TURN("0", "4") " offset:%6\n\t" FAST_TURN("1", "4") " offset:%7\n\t" FAST_TURN("2", "5") " offset:%6\n\t" FAST_TURN("3", "5") " offset:%7\n\t"
+                         "s_waitcnt lgkmcnt(0)"
+                         : "=&v"(h[0]), "=&v"(h[1]), "=&v"(h[2]), "=&v"(h[3]) : "v"(pb), "v"(pb ^ 64u), "n"(STEP), "n"(STEP + HALF) : "memory");
             put(fb[set][0], h[0], h[1]);
             put(fb[set][1], h[2], h[3]);
         }
-        if constexpr (AT) {
-            static_for<0, MI / 2>([&](auto u_c) {
-                constexpr int u = decltype(u_c)::value;
-                const uint32_t p = base + (L::ring3(L::load_of_a(0)) ? b.f : b.r) + L::at(L::load_of_a(0)) + (wm * (MI / 2) + u) * L::UNIT, p1 = p ^ 64u;
-                i32x2 h[4];
-                asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
-                             "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\ts_waitcnt lgkmcnt(0)"
-                             : "=&v"(h[0]), "=&v"(h[1]), "=&v"(h[2]), "=&v"(h[3]) : "v"(p), "v"(p1), "n"(STEP), "n"(STEP + HALF) : "memory");
-                put(fa[set][2 * u], h[0], h[1]);
-                put(fa[set][2 * u + 1], h[2], h[3]);
-            });
-        }
+#undef FAST_TURN
     };
     // MFMA j of step t (set t & 1)
     auto mfma = [&](auto first_c, auto t_c, auto j_c) __attribute__((always_inline)) {
