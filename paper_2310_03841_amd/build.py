@@ -10,8 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libabft.so")
-SOURCES = ["gemm_tile.hip", "gemm_fast.hip", "gemm_item_rows.hip", "gemm_item_cols.hip", "gemm_item.hip", "gemm_group.hip", "gemm_group_few.hip", "gemm_group_big_i8.hip", "gemm_group_big_bf16.hip", "gemm_group_big_f16.hip", "gemm_group_big_wgrad.hip", "group_check.hip", "quantize.hip", "aux_kernels.hip", "abft_api.hip"]
-HEADERS = ["abft_internal.h", "abft_device.h", "gemm_args.h", "gemm_epilogue.h", "gemm_apass.h", "gemm_item.h", "block_out.h", "encode_pass.h", "predict_pass.h", "check_dots.h", "gemm_fast_tile.h", "group_args.h", "gemm_group_big.h", "group_passes.h", os.path.join("..", "..", "include", "abft.h")]
+SOURCES = ["gemm_tile.hip", "gemm_fast.hip", "gemm_item_rows.hip", "gemm_item_cols.hip", "gemm_item.hip", "gemm_group.hip", "gemm_group_i8.hip", "gemm_group_bf16.hip", "gemm_group_f16.hip", "gemm_group_few.hip", "gemm_group_big_i8.hip", "gemm_group_big_bf16.hip", "gemm_group_big_f16.hip", "gemm_group_big_wgrad.hip", "group_check.hip", "quantize.hip", "aux_kernels.hip", "abft_api.hip"]
+HEADERS = ["abft_internal.h", "abft_device.h", "gemm_args.h", "gemm_epilogue.h", "gemm_apass.h", "gemm_item.h", "block_out.h", "encode_pass.h", "predict_pass.h", "check_dots.h", "gemm_fast_tile.h", "group_args.h", "gemm_group.h", "gemm_group_big.h", "group_passes.h", os.path.join("..", "..", "include", "abft.h")]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-munsafe-fp-atomics",

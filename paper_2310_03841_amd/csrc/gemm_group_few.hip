@@ -320,9 +320,9 @@ __global__ __launch_bounds__(256) void gemm_group_few_kernel(FewArgs f)
 // ------------------------------------------------------------------------------------------
 constexpr int FEW_MAX_SUMS = 64 * 1024;      // bytes of LDS for the column sums of A
 
-bool group_takes_few(int dt, bool transB, const GroupArgs &g)
+bool group_few_fits(int dt, bool protect, const GroupArgs &g)
 {
-    return transB && (long)g.M <= 16L * g.groups && ((long)g.K * elem_size(dt) + 15) / 16 * 32 <= FEW_MAX_SUMS;
+    return !protect || (g.M <= 32L * g.groups && ((long)g.K * elem_size(dt) + 15) / 16 * 32 <= FEW_MAX_SUMS);
 }
 
 template <int DT, int OT, bool PROT, int NB> static hipError_t launch_few_one(FewArgs &f, hipStream_t st)
@@ -346,7 +346,7 @@ template <int DT, int OT, bool PROT, int NB> static hipError_t launch_few_one(Fe
 // 32 columns to a workgroup, which reads its rows of A once for both halves, unless that leaves compute units without one.
 template <int DT, int OT> static hipError_t launch_few_type(bool protect, FewArgs &f, hipStream_t st)
 {
-    const bool wide = (long)std::min(f.g.M, f.g.groups) * ((f.g.N + 31) / 32) >= 512;
+    const bool wide = (long)std::min(f.g.M, f.g.groups) * ((f.g.M / f.g.groups + 15) / 16) * ((f.g.N + 31) / 32) >= 512;
     if (protect) return wide ? launch_few_one<DT, OT, true, 2>(f, st) : launch_few_one<DT, OT, true, 1>(f, st);
     return wide ? launch_few_one<DT, OT, false, 2>(f, st) : launch_few_one<DT, OT, false, 1>(f, st);
 }

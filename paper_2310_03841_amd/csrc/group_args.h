@@ -130,10 +130,15 @@ template <int BM> __device__ __forceinline__ bool find_tile(const GroupArgs &g, 
     return true;
 }
 
-// Groups of few rows (gemm_group_few.hip), whose kernel checks the columns itself: cc_obs then holds a mark for each that disagrees.
-bool group_takes_few(int dt, bool transB, const GroupArgs &g);
-// Its shares of the observed sums of rows, for every sixteen columns one after the other, [M] words each: they take the place of the sums in doubles, of which it
-// keeps none: 16 rows to a group make at most M (N / 16 + 1) <= groups N + M words.
+// The kernel that a product takes: tiles by four waves (gemm_group.h, of the shape `tiles`), of the fast kernel (gemm_group_big.h), or few rows
+// (gemm_group_few.hip), whose kernel checks the columns itself: cc_obs then holds a mark for each that disagrees.
+enum { GROUP_KERNEL_TILE, GROUP_KERNEL_BIG, GROUP_KERNEL_FEW };
+struct GroupKernel { int kind, tiles; };
+GroupKernel group_kernel(int dt, bool transB, bool protect, const GroupArgs &g);
+// Whether the kernel of few rows has room for what it keeps.
+bool group_few_fits(int dt, bool protect, const GroupArgs &g);
+// Its shares of the observed sums of rows, for every sixteen columns one after the other, [M] words each: they take the place of the sums in doubles (2 (groups N +
+// M) words), of which it keeps none.
 inline uint32_t *group_few_shares(const GroupArgs &g) { return reinterpret_cast<uint32_t *>(g.cc_acc); }
 hipError_t launch_group_few(int dt, int ot, bool protect, GroupArgs &g, const uint32_t *b_max, float tau_cols, hipStream_t st);
 

@@ -182,7 +182,7 @@ hipError_t launch_group_check(int dt, const GroupArgs &g, bool transB, const Wor
     f.row_flag = v.row_flag; f.col_flag = v.col_flag; f.counts = v.counts;
     f.zero_ptr = end.zero_ptr; f.zero_words = end.zero_ptr ? end.zero_words : 0;
     f.zero2_ptr = end.zero2_ptr; f.zero2_words = end.zero2_ptr ? end.zero2_words : 0;
-    const bool marked = group_takes_few(dt, transB, g);
+    const bool marked = group_kernel(dt, transB, true, g).kind == GROUP_KERNEL_FEW;
     const int per = transB ? 4 * RW : GCHK_KN_LANES * (16 / elem_size(dt));
     f.row_units = marked ? (g.M + 3) / 4 : (g.M + 255) / 256;
     f.col_units = (g.N + per - 1) / per;
