@@ -246,7 +246,10 @@ typedef struct {
  * be OR-ed with ABFT_B_CHECKSUM_CACHED (others: ABFT_EINVAL).  What is checked are the int32 sums ahead of the scales, by
  * equality as in abft_gemm, so every single fault of the product shows whatever the scales are; faults behind the sums (scales, rounding,
  * C in memory) do not.  batch must be 1 (ABFT_ESHAPE); K may exceed 4096, K * 2^14 < 2^31.
- * abft_verify, abft_correct and abft_discrepancy have nothing to go by behind this call (ABFT_ESTATE). */
+ * abft_verify, abft_correct and abft_discrepancy have nothing to go by behind this call (ABFT_ESTATE), and abft_workspace has no vectors
+ * of it.  An armed accumulator flip (abft_inject) and the event of abft_gemm_done_event are honoured as by abft_gemm.
+ * Enqueues, protected: the pass over B, unless its checksum is cached; the product, whose launch also passes over A; the check
+ * kernel. */
 int abft_gemm_scaled(abft_ctx *ctx, const void *A, const void *B, const abft_scales *scales, void *C, int mode,
                      const abft_shape *s, const abft_result *r, void *stream);
 
@@ -258,8 +261,9 @@ int abft_gemm_scaled(abft_ctx *ctx, const void *A, const void *B, const abft_sca
  * of C, and flagged, is unspecified.)
  * scales: NULL: C as in abft_gemm (int32 for ABFT_I8); ABFT_I8 with scales: as in abft_gemm_scaled.
  * mode, K and what may follow the call: as in abft_gemm_scaled.  ABFT_DETECT: row_flag [M] (0 for rows of no group), col_flag [batch][N]; the
- * checksums, max|A|, max|B| and with them the tolerance are a group's own.  abft_encode_b with this shape encodes the B of all groups.
- * abft_workspace has no vectors of this call.  The context serves s->M <= max_rows, batch * N <= max_cols,
+ * checksums, max|A|, max|B| and with them the tolerance are a group's own (where groups have few rows, a column's check and its max|A| are those of sixteen rows at
+ * a time).  abft_encode_b with this shape encodes the B of all groups (it does not look at M).  An armed accumulator flip counts batch_idx in groups and
+ * the row from its group's first.  The context serves s->M <= max_rows, batch * N <= max_cols,
  * batch * (K rounded up to 128) <= max_depth, batch <= max_batch.
  * The backward pass with respect to A is this call again: dA = dC B^T, that is, A := dC, B as it lies with transB
  * inverted, and N and K exchanged. */

@@ -152,6 +152,8 @@ SHAPES = [
     ([0] * 66 + [7, 7, 40], 64, 96, True),              # more groups than lanes, nearly all empty
     (list(range(0, 130 * 3, 3)), 72, 200, False),
 ]
+# Tiles of every shape in both layouts of B
+SHAPES += [([0, 1000, 1700, 3000], 2000, 136, True), ([0, 9000, 17000], 60, 72, False)]
 # Enough for tiles of 256: left-over rows of every kind, a group without rows, columns that end inside a tile, K of the fewest slabs and of many, rows of no
 # group; more than 64 groups; fewer tiles than compute units, and some rounds of them
 BIG = [
@@ -162,6 +164,7 @@ BIG = [
     (list(range(0, 131 * 130, 130)), 264, 384, True),
     ([0, 8192], 512, 384, True),
     ([0, 4000, 12600], 2056, 384, True),
+    ([0, 5000, 5000, 12000], 1024, 448, False),
 ]
 # Few rows to a group: one and sixteen and seventeen of them, groups of many among them, one piece of K and many, parts of a piece, and both widths of tiles
 FEW = [
@@ -171,6 +174,7 @@ FEW = [
     (list(range(0, 71)), 264, 136, True),
     ([0] * 40 + [170] + [171] * 23, 264, 200, True),
     ([0, 13], 1000, 713, True),
+    (list(range(0, 65)), 264, 2000, True),
 ]
 TYPES = [("i8", None), ("i8", "bf16"), ("i8", "f16"), ("bf16", None), ("f16", None)]
 
@@ -308,6 +312,98 @@ def test_values_that_are_not_finite_stay_in_their_rows_and_columns(dtype, value,
         p.close()
 
 
+@pytest.mark.gpu
+def test_tolerances_of_the_caller():
+    """tau for both checks, tau_cols for the columns alone, in each kernel: a flip that the default tolerance finds and a wide one does not."""
+    for ends, N, K in (([0, 3, 8], 70, 96), ([0, 100, 330], 200, 136), ([0, 1300, 4200], 1024, 384)):
+        p = Group("bf16", ends, N, K, seed=8)
+        try:
+            for tau, tau_cols, want in ((0.0, 0.0, (1, 1)), (1e30, 0.0, (0, 0)), (1e30, 1e-3, (0, 1)), (1e-3, 1e30, (1, 0))):
+                s = ab.make_shape(1, N, K, batch=p.groups, lda=p.A.shape[-1], ldb=p.B.shape[-1], ldc=p.ldc, strideA=0, strideC=p.M * p.ldc)
+                assert ab.abft_inject(p.ctx, None, p.code, s, 1, 0, 5, 29, ab.ABFT_INJECT_ACCUMULATOR) == ab.ABFT_OK
+                p.run(ab.ABFT_DETECT, tau=tau, tau_cols=tau_cols)
+                flip = p.ends[1]
+                assert (p.row_flag[flip].item(), p.col_flag[N + 5].item()) == want, (ends, tau, tau_cols)
+                if tau != 1e-3 and tau_cols != 1e-3:
+                    assert p.counts[:2].tolist() == list(want)
+        finally:
+            p.close()
+
+
+# ------------------------------------------------------------------------------------------ layouts
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,out", [("i8", "bf16"), ("i8", None), ("bf16", None)])
+@pytest.mark.parametrize("ends,N,K,trans_b", [([0, 2, 7], 50, 70, True), ([0, 80, 200], 130, 200, True), ([0, 80, 200], 130, 200, False),
+                                              ([0, 1300, 4200], 1024, 384, True), ([0, 5000, 9000], 1024, 448, False)])
+def test_wide_rows_and_matrices_far_apart(dtype, out, ends, N, K, trans_b):
+    p = Group(dtype, ends, N, K, trans_b, out=out, seed=9)
+    try:
+        q = 16 if dtype == "i8" else 8
+        wide = lambda x, more, pre: torch.nn.functional.pad(x, (0, more) + pre).cuda()
+        p.dA = wide(p.A, 3 * q, ())
+        whole = wide(p.B, 5 * q, (0, 3))
+        p.dB = whole
+        p.C = torch.full((p.M, p.ldc + 24), p.fill, dtype=p.c_type, device="cuda")
+        p.shape = ab.make_shape(p.M, N, K, batch=p.groups, lda=p.dA.shape[1], ldb=whole.shape[2], ldc=p.C.shape[1], strideB=whole.stride(0), transB=trans_b)
+        p.run(ab.ABFT_DETECT)
+        p.check()
+        p.clean()
+    finally:
+        p.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ends,N,K", [([40000, 40003, 69999], 24, 96), ([10, 30000, 69990], 256, 384)])
+def test_places_past_32_bits(ends, N, K):
+    """Rows of A and C, and matrices, more than 2^31 and 2^32 bytes from the first: those of the last group are compared."""
+    M, lda, ldc = 70000, 65536, 40960
+    A = torch.empty((M, lda), dtype=torch.int8, device="cuda")
+    A[:, :K].random_(-128, 128)
+    B = torch.empty((2, 1 << 32), dtype=torch.int8, device="cuda")
+    C = torch.empty((M, ldc), dtype=torch.bfloat16, device="cuda")
+    C[:, :N].fill_(7)
+    W = torch.randint(-128, 128, (2, N, 384), dtype=torch.int8, device="cuda")
+    for g in range(2):
+        B[g, :N * 384] = W[g].flatten()
+    ctx = ab.abft_create(M, 2 * N, 2 * 384, 2)
+    try:
+        off = torch.tensor(ends, dtype=torch.int32, device="cuda")
+        rf, cf, cnt = (torch.full((n,), 3, dtype=t, device="cuda") for n, t in ((M, torch.uint8), (2 * N, torch.uint8), (8, torch.int32)))
+        s = ab.make_shape(M, N, K, batch=2, lda=lda, ldb=384, ldc=ldc, strideB=1 << 32)
+        row = torch.rand(M, device="cuda") * 1e-3
+        sc = ab.make_scales(row, None, None, out=ab.ABFT_BF16)
+        assert ab.abft_gemm_grouped(ctx, A, B, off, sc, C, ab.ABFT_I8, ab.ABFT_DETECT, s, ab.make_result(rf, cf, cnt)) == ab.ABFT_OK
+        torch.cuda.synchronize()
+        assert cnt[:3].tolist() == [0, 0, 0] and not rf.any() and not cf.any()
+        for g in range(2):
+            for a, b in ((ends[g], min(ends[g] + 100, ends[g + 1])), (max(ends[g + 1] - 100, ends[g]), ends[g + 1])):
+                want = (A[a:b, :K].double() @ W[g, :, :K].double().t()) * row[a:b, None].double()
+                got = C[a:b, :N].double()
+                assert ((got - want).abs() <= half_step(torch.bfloat16) * want.abs() + 4 * U32 * want.abs()).all()
+        assert (C[:ends[0], :N] == 7).all() and (C[ends[2]:, :N] == 7).all()
+    finally:
+        ab.abft_destroy(ctx)
+
+
+@pytest.mark.gpu
+def test_two_contexts_on_two_streams_at_once():
+    a, b = Group("bf16", [0, 900, 2500], 520, 384, seed=61), Group("i8", [0, 5, 9, 40], 300, 512, out="f16", seed=62)
+    try:
+        streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+        torch.cuda.synchronize()
+        for _ in range(5):
+            for p, st in zip((a, b), streams):
+                with torch.cuda.stream(st):
+                    assert p.call(ab.ABFT_DETECT) == ab.ABFT_OK
+        torch.cuda.synchronize()
+        for p in (a, b):
+            p.check()
+            p.clean()
+    finally:
+        a.close()
+        b.close()
+
+
 # ------------------------------------------------------------------------------------------ gradients
 def wgrad(dtype, ends, N, K, trans_b, M=None, seed=0, guard=0):
     gen = torch.Generator().manual_seed(seed)
@@ -338,7 +434,7 @@ def wgrad(dtype, ends, N, K, trans_b, M=None, seed=0, guard=0):
 
 
 WGRAD = [([0, 1], 1, 1), ([0, 0, 5, 5], 40, 72), ([3, 60, 61, 189], 130, 100), ([0, 64, 192, 200], 128, 128), ([0, 700, 701, 1500], 257, 136),
-         ([0, 500, 1300], 520, 264), (list(range(0, 72)), 33, 40), ([5, 5], 16, 24),
+         ([0, 500, 1300], 520, 264), (list(range(0, 72)), 33, 40), ([5, 5], 16, 24), (list(range(0, 602, 2)), 60, 56),
          # enough for tiles of 256: depths of no, one and some slabs and a part of one
          ([2, 2, 3, 66, 131, 300, 1000], 1030, 520), ([0, 64, 128, 320, 1345], 1024, 1001), ([0, 700, 4001], 2056, 1024)]
 
@@ -428,7 +524,7 @@ def check_quantize(x, cols):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (5, 8), (197, 768), (9, 513), (4, 1000), (6, 2047), (7, 4096), (3, 4097), (2, 9001)])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (5, 8), (197, 768), (9, 513), (4, 1000), (3, 1200), (6, 2047), (5, 2500), (7, 4096), (3, 4097), (2, 9001)])
 def test_rows_to_int8(dtype, rows, cols):
     gen = torch.Generator().manual_seed(rows)
     x = rand(gen, dtype, rows, cols)
