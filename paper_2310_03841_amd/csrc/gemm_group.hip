@@ -34,12 +34,13 @@ static double big_us(const GroupProblem &p)
 }
 
 // Sixteen rows and 32 columns to a workgroup, which reads both over all of K: the L2 caches, or the matrices from memory, and its start and end.  Protected,
-// the sums of its rows of A, and, floating point, the vector instructions of the columns' check.
+// the sums of its rows of A, and, floating point, the vector instructions of the columns' check: 3.2 TB/s of the matrices.
 static double few_us(const GroupProblem &p)
 {
-    const double tiles = (double)p.groups * (ceil_div(p.rows, 16) + (p.groups > 1 && p.rows > 4 ? 0.3 : 0.0)) * ceil_div(p.N, 32);
-    const double read = tiles * 48 * p.K * p.es / 8e6 * (p.protect && p.es == 2 ? 2.2 : 1.0);
-    return (p.protect ? p.es == 2 ? 3.0 : 1.0 : 0.5) + tiles * 2e-3 + std::max(read, (double)p.groups * p.N * p.K * p.es / 5e6);
+    const double tiles = (double)p.groups * (ceil_div(p.rows, 16) + (p.groups > 1 && p.rows > 4 ? 0.3 : 0.0)) * ceil_div(p.N, 32), row = (double)p.K * p.es;
+    const bool slow = p.protect && p.es == 2;
+    const double read = std::max(tiles * 48 * row / 8e6, slow ? tiles * 32 * row / 3.2e6 : 0.0);
+    return (slow ? 3.0 : p.protect ? 1.0 : 0.5) + tiles * (slow ? 1e-3 : 2e-3) + std::max(read, (double)p.groups * p.N * row / 5e6);
 }
 
 GroupKernel group_kernel(int dt, bool transB, bool protect, const GroupArgs &g)

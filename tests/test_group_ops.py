@@ -175,6 +175,7 @@ FEW = [
     ([0] * 40 + [170] + [171] * 23, 264, 200, True),
     ([0, 13], 1000, 713, True),
     (list(range(0, 65)), 264, 2000, True),
+    (list(range(0, 33)), 2048, 1024, True),
 ]
 TYPES = [("i8", None), ("i8", "bf16"), ("i8", "f16"), ("bf16", None), ("f16", None)]
 
