@@ -36,7 +36,8 @@
  *     item: the library may read (never use) the pad between K and lda.
  *   - The caller owns A, B, C, the flag / count buffers and the stream.  The
  *     context owns its workspace (checksum vectors, tile lists).
- *   - abft_gemm / abft_verify / abft_correct / abft_correct_checksum / abft_inject /
+ *   - abft_gemm / abft_gemm_scaled / abft_gemm_grouped / abft_gemm_grouped_wgrad / abft_quantize_rows /
+ *     abft_verify / abft_correct / abft_correct_checksum / abft_inject /
  *     abft_encode_b / abft_discrepancy only enqueue work on `stream` (a hipStream_t
  *     passed as void*): they allocate nothing, copy nothing to the host and never
  *     synchronise.  Results are valid once the stream has reached that point.
@@ -264,7 +265,7 @@ int abft_gemm_scaled(abft_ctx *ctx, const void *A, const void *B, const abft_sca
  * checksums, max|A|, max|B| and with them the tolerance are a group's own (where groups have few rows, a column's check and its max|A| are those of sixteen rows at
  * a time).  abft_encode_b with this shape encodes the B of all groups (it does not look at M).  An armed accumulator flip counts batch_idx in groups and
  * the row from its group's first.  The context serves s->M <= max_rows, batch * N <= max_cols,
- * batch * (K rounded up to 128) <= max_depth, batch <= max_batch.
+ * batch * (K rounded up to 128) <= max_depth, batch <= max_batch; M <= 2^30, K <= 2^29, batch * N <= 2^27 (ABFT_ESHAPE).
  * The backward pass with respect to A is this call again: dA = dC B^T, that is, A := dC, B as it lies with transB
  * inverted, and N and K exchanged. */
 int abft_gemm_grouped(abft_ctx *ctx, const void *A, const void *B, const int32_t *offsets, const abft_scales *scales,

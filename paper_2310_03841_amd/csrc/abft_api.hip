@@ -677,7 +677,8 @@ static int check_group_shape(const abft_ctx *c, int dt, int os, const abft_shape
 {
     if (!c || !s) return ABFT_EINVAL;
     if (s->M < 1 || s->N < 1 || s->K < 1 || s->batch < 1) return ABFT_ESHAPE;
-    if (s->M > (1 << 30) || s->N > (1 << 30) || s->K > (1 << 30) || s->batch > 65535) return ABFT_ESHAPE;
+    // (bytes of a row of A, B and C, and of a tile behind its end, are counted in 32 bits; columns of all groups, by the check kernel's workgroups)
+    if (s->M > (1 << 30) || s->N > (1 << 29) || s->K > (1 << 29) || s->batch > 65535 || s->batch * s->N > (1 << 27)) return ABFT_ESHAPE;
     if (s->transB != 0 && s->transB != 1) return ABFT_EINVAL;
     const int es = elem_size(dt);
     if (dt == ABFT_I8 && s->K >= (1 << 17)) return ABFT_ESHAPE;       // K * 2^14 must stay below 2^31

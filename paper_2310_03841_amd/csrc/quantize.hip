@@ -30,7 +30,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a)
     constexpr uint32_t INF_BITS = DT == DT_BF16 ? 0x7F80u : 0x7C00u;
     typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
     const int lane = threadIdx.x & 63;
-    const int nch = (a.cols + 7) / 8, tail = a.cols * 2;
+    const int nch = (a.cols + 7) / 8;
     for (long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6); r < a.rows; r += (long)gridDim.x * 4) {
         const uint8_t *src = a.X + r * a.ldx * 2;
         uint8_t *dst = a.Q + r * a.ldq;
@@ -45,7 +45,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a)
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
                 const int c = c0 + 64 * i + lane;
-                if (c >= nch - 1) x[i] = mask_chunk(x[i], c < nch ? tail - c * 16 : 0);
+                if (c >= nch - 1) x[i] = mask_chunk(x[i], c < nch ? (a.cols - c * 8) * 2 : 0);
             }
         };
         auto largest = [&]() __attribute__((always_inline)) {

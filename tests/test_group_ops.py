@@ -743,5 +743,7 @@ def test_refusals():
         assert w(shape(), offsets=None) == ab.ABFT_EINVAL
         assert w(shape(), dW=P + 8) == ab.ABFT_EALIGN
         assert w(shape(M=65)) == ab.ABFT_EWORKSPACE
+        for s in (shape(K=(1 << 29) + 8), shape(N=(1 << 25) + 8), shape(M=(1 << 30) + 8), shape(batch=1, N=(1 << 27) + 8)):
+            assert g(s) == ab.ABFT_ESHAPE and w(s) == ab.ABFT_ESHAPE
     finally:
         ab.abft_destroy(ctx)
