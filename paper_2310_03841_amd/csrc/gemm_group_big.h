@@ -16,6 +16,16 @@ namespace abft {
 
 enum { BIG_ROWS, BIG_DEPTH };
 
+// A gradient's tiles take as long as their group is deep.  Up to 64 groups are put in the order of their depth, what is cut in halves the least deep, and
+// the rounds are dealt out one way and the other, so that every compute unit has about as much to do.  Worth it from two rounds on, of groups of 512 rows on
+// average: with fewer the stores of C count for more, and the tiles of a round are no longer neighbours of those of the one behind it.  (bf16 2048 x 1024, group
+// by group / so, us: 13 groups of 64 rows on average 20.0 / 22.6, of 512 37.9 / 37.8, of 1024 74.6 / 62.6; 34 groups of 256 58.8 / 62.2, of 512 87.3 / 85.9;
+// 6 groups of 512, one round, 21.7 / 22.0; 16 groups of 3072 x 768 and 0 to 1377 rows 83.5 / 70.)
+inline bool big_deep_first(const GroupArgs &g, int tiles_n, int cus)
+{
+    return g.groups > 1 && g.groups <= 64 && g.M / g.groups >= 512 && (g.K + 255L) / 256 * tiles_n * g.groups > cus;
+}
+
 // The arguments of one tile, formed where they are used: behind the main loop they are read again rather than held across it.
 template <int OT, int GROUP> struct GroupSource {
     static constexpr bool LAYER_BIAS = false;            // (a bias of scaled products is outside the checked sums)
@@ -49,8 +59,20 @@ template <int OT, int GROUP> struct GroupSource {
 
 struct BigTile { int e, first, rows, m0, tn; bool tall; };
 
+// The place of a lane's group among up to 64 by their depth, the deepest first.
+__device__ __forceinline__ int depth_rank(const GroupArgs &g)
+{
+    const int lane = threadIdx.x & 63, groups = g.groups;
+    // (the order of groups deeper than 2^24 is of no account)
+    const int key = lane < groups ? min(group_lane(g, lane).rows, (1 << 24) - 1) * 64 + 63 - lane : -1;
+    int rank = 0;
+#pragma unroll 8
+    for (int e = 0; e < groups; ++e) rank += __builtin_amdgcn_readlane(key, e) > key ? 1 : 0;
+    return lane < groups ? rank : 64;
+}
+
 // Tile t of the list: false, there is none, and *tiles are all.
-template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const GroupArgs &g, const GroupLane &kept, int t, int wgs, BigTile *o, int *tiles)
+template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const GroupArgs &g, const GroupLane &kept, int rank, int t, int wgs, BigTile *o, int *tiles)
 {
     const int lane = threadIdx.x & 63, tiles_n = g.tiles_n;
     // rows of tiles of 256, of 128, of a product of so many rows
@@ -85,7 +107,22 @@ template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const G
     bool left_over = false;
     o->tall = false;
     *tiles = halves + ns + whole;
-    if (t < halves) {
+    if (GROUP == BIG_DEPTH && g.deep_first) {
+        // by falling depth, a round at a time, each the other way round than the one ahead of it, and the last round first
+        const int k = t / wgs, last = rounds(*tiles) - 1, slot = deal(t - k * wgs, wgs);
+        auto place = [&](int r) __attribute__((always_inline)) { return r * wgs + (r & 1 ? wgs - 1 - slot : slot); };
+        const int r = last - k - (place(last) < *tiles ? 0 : 1);
+        if (r < 0) return false;
+        L = place(r);
+        if (L < whole) {
+            o->tall = true;
+        } else if ((L -= whole) < ns) {
+            left_over = true;
+        } else {
+            half = (L -= ns) & 1;
+            L = whole + (L >> 1);
+        }
+    } else if (t < halves) {
         const int h = deal(t, halves);
         L = whole + (h >> 1);
         half = h & 1;
@@ -99,9 +136,9 @@ template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const G
         return false;
     }
     if constexpr (GROUP == BIG_DEPTH) {
-        const int per = (left_over ? small_of(g.K) : tall_of(g.K)) * tiles_n;
-        o->e = L / per;
-        L -= o->e * per;
+        const int per = (left_over ? small_of(g.K) : tall_of(g.K)) * tiles_n, nth = L / per;
+        L -= nth * per;
+        o->e = g.deep_first ? __builtin_ctzll(__ballot(rank == nth)) : nth;
         group_rows(g.offsets, g.M, o->e, &o->first, &o->rows);
     } else {
         const bool found = find_group(g, kept, [&](int rows) { return (left_over ? small_of(rows) : tall_of(rows)) * tiles_n; }, &L, &o->e, &o->first, &o->rows);
@@ -123,13 +160,15 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void gemm_group_big_kernel(GroupAr
     constexpr int MODE = PROT ? FAST_BESIDE : FAST_PLAIN, ES = Traits<DT>::ES;
     fetch_args<GroupArgs>();
     GroupLane kept = {0, 0};
+    int rank = 0;
     if constexpr (!DEPTH) kept = group_lane(kernel_args<GroupArgs>(), threadIdx.x & 63);
+    else if (kernel_args<GroupArgs>().deep_first) rank = depth_rank(kernel_args<GroupArgs>());
     int tiles;
     for (int t = blockIdx.x;; t += gridDim.x) {
         const GroupArgs &a = kernel_args<GroupArgs>();
         if (PROT && t == 0 && threadIdx.x < 5) a.counts[threadIdx.x] = 0u;       // completed by the check kernel
         BigTile b;
-        if (!big_tile<GROUP, PROT>(a, kept, t, (int)gridDim.x, &b, &tiles)) break;
+        if (!big_tile<GROUP, PROT>(a, kept, rank, t, (int)gridDim.x, &b, &tiles)) break;
         // the epilogue's last reads of LDS precede the next tile's first writes
         if (t != (int)blockIdx.x) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         GemmArgs g = {};
@@ -178,6 +217,7 @@ template <int DT, int OT, bool PROT, int GROUP, bool BT> static hipError_t launc
     if (e != hipSuccess) return e;
     g.tiles_n = (g.N + 255) / 256;
     g.group_inv = map_inverse(g.tiles_n);
+    g.deep_first = GROUP == BIG_DEPTH && big_deep_first(g, g.tiles_n, cus);
     hipLaunchKernelGGL(kern, dim3((unsigned)cus), dim3(64 * FAST_WAVES), smem, st, g);
     return hipGetLastError();
 }

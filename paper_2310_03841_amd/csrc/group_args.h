@@ -25,6 +25,7 @@ struct GroupArgs {
     uint32_t *a_sum, *a_max;              // e^T A and max|A| of a group's rows  [groups][K], [groups]
     const uint32_t *b_sum;                // B e of each group  [groups][K]
     uint32_t *counts;                     // cleared for the check kernel
+    int deep_first;                       // tiles of a gradient go by the depth of their groups (big_deep_first)
     int n_pass, pass_win;                 // workgroups that pass over A, ahead of those that take tiles; windows along K
     uint32_t pass_inv;                    // map_inverse(pass_win)
 };

@@ -451,6 +451,35 @@ def test_gradient_of_the_weights_matches_plain(dtype, trans_b, ends, N, K):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("ends,N,K", [
+    # two rounds of tiles and a part of one, groups of very different depth, of the same, of none; more than three rounds
+    ([0, 0, 1100, 1164, 1165, 1500, 1900, 2300, 2364, 2999, 3200], 1536, 1280), ([0, 300, 600, 900, 1200, 1500], 2568, 1928),
+    ([7, 7, 7, 2500, 2500], 4096, 1288), ([0, 129, 1600, 1601, 4200], 4224, 3200), ([0] + [620 * i + 37 * (i % 7) for i in range(1, 64)] + [40000], 512, 768)])
+def test_gradients_of_unequal_depths(dtype, ends, N, K):
+    """Whole numbers of at most 3: a sum of 20000 products stays below 2^24, so fp32 holds it exactly and one rounding is left."""
+    print(f"case {dtype} {ends[:8]} {N} {K}", flush=True)
+    gen = torch.Generator().manual_seed(N + K)
+    M, groups, t = ends[-1] + 5, len(ends) - 1, TORCH[dtype]
+    X = torch.randint(-3, 4, (M, K), generator=gen, dtype=torch.int8).cuda().to(t)
+    dY = torch.randint(-3, 4, (M, N), generator=gen, dtype=torch.int8).cuda().to(t)
+    dW = torch.full((groups, N + 1, K), 77.0, dtype=t, device="cuda")
+    off = torch.tensor(ends, dtype=torch.int32).cuda()
+    ctx = ab.abft_create(M, groups * N, groups * ((K + 127) // 128 * 128), groups)
+    try:
+        s = ab.make_shape(M, N, K, batch=groups, strideB=(N + 1) * K)
+        assert ab.abft_gemm_grouped_wgrad(ctx, X, dY, off, dW, ab.DTYPE_CODE[dtype], s) == ab.ABFT_OK
+        torch.cuda.synchronize()
+        assert bool((dW[:, N] == 77).all()), "written between the gradients"
+        for g in range(groups):
+            a, b = ends[g], ends[g + 1]
+            want = torch.mm(dY[a:b].float().t().contiguous(), X[a:b].float()).to(t)
+            assert torch.equal(dW[g, :N], want), g
+    finally:
+        ab.abft_destroy(ctx)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_gradients_agree_with_differences(dtype):
     """A layer's loss sum(C * G) against its differences when an element of A or of B moves by a step that the type holds exactly: the
     loss is linear in each, so a difference is the gradient up to the rounding of C."""
