@@ -672,6 +672,59 @@ def test_grouped_calls_can_be_captured_in_a_graph(dtype, out, ends, N, K, trans_
 
 
 @pytest.mark.gpu
+def test_two_graphs_of_a_context_with_offsets_that_change():
+    """Two captured calls take turns on one context, and between their replays the rows are dealt out anew where the offsets lie, as a router's kernel does."""
+    splits = [[0, 0, 1300, 1301, 1700, 2600], [5, 600, 600, 600, 2590, 2595], [0, 520, 1040, 1560, 2080, 2600], [0, 0, 0, 0, 0, 0]]
+    small = [[0, 3, 9, 9], [0, 0, 0, 20], [1, 17, 18, 19], [20, 20, 20, 20]]
+    ctx = ab.abft_create(4096, 16384, 8192, 16)
+    p = Group("bf16", splits[0], 2056, 1288, M=2600, seed=51, ctx=ctx)
+    q = Group("i8", small[0], 264, 208, out="bf16", M=20, seed=52, ctx=ctx)
+    whole = lambda *shape: torch.randint(-3, 4, shape, generator=torch.Generator().manual_seed(53), dtype=torch.int8).cuda().to(torch.bfloat16)
+    X, dY, dW = whole(2600, 1288), whole(2600, 2056), torch.zeros(5, 2056, 1288, dtype=torch.bfloat16, device="cuda")
+    s = ab.make_shape(2600, 2056, 1288, batch=5)
+
+    def first():
+        assert p.call(ab.ABFT_DETECT) == ab.ABFT_OK
+        assert ab.abft_gemm_grouped_wgrad(ctx, X, dY, p.offsets, dW, ab.ABFT_BF16, s) == ab.ABFT_OK
+
+    def second():
+        assert q.call(ab.ABFT_DETECT) == ab.ABFT_OK
+
+    try:
+        graphs = []
+        for f in (first, second):
+            f()
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                f()
+            graphs.append(graph)
+        for k in (0, 1, 2, 3, 1):
+            for x, ends in ((p, splits[k]), (q, small[k])):
+                x.ends = ends
+                x.offsets.copy_(torch.tensor(ends, dtype=torch.int32))
+                x.C.fill_(x.fill)
+                for y in (x.row_flag, x.col_flag, x.counts):
+                    y.fill_(3)
+            dW.fill_(5.0)
+            for graph in graphs:
+                graph.replay()
+            torch.cuda.synchronize()
+            for x in (p, q):
+                x.check()
+                x.clean()
+            for g in range(5):
+                a, b = splits[k][g], splits[k][g + 1]
+                assert torch.equal(dW[g], torch.mm(dY[a:b].float().t().contiguous(), X[a:b].float()).to(torch.bfloat16)), (k, g)
+            second()
+            torch.cuda.synchronize()
+            q.check()
+            q.clean()
+    finally:
+        ab.abft_destroy(ctx)
+
+
+@pytest.mark.gpu
 def test_grouped_and_other_calls_share_a_context():
     """Calls of other kinds between grouped ones: the regions they accumulate into are clean for each."""
     ctx = ab.abft_create(4096, 8192, 8192, 16)
