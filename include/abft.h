@@ -274,7 +274,8 @@ int abft_gemm_grouped(abft_ctx *ctx, const void *A, const void *B, const int32_t
 /* Its backward pass with respect to B: for each group the sum over its rows of the products of dY and X,
  * dW[e] = dY_e^T X_e (N x K, transB = 1) or X_e^T dY_e (K x N, transB = 0), as B lies in memory.  s: the shape of the
  * forward call: X is its A (lda), dY has the layout of its C (ldc, elements of dtype), dW that of its B (ldb, strideB, which must keep the
- * groups apart: ABFT_ESHAPE).  ABFT_BF16 or ABFT_F16, sums in fp32, rounded once.  A group without rows gets zeros.  Unprotected. */
+ * groups apart: ABFT_ESHAPE).  ABFT_BF16 or ABFT_F16, sums in fp32, rounded once.  A group without rows gets zeros.  Unprotected.  The
+ * context serves the shapes it serves the forward call for, and keeps nothing of this one. */
 int abft_gemm_grouped_wgrad(abft_ctx *ctx, const void *X, const void *dY, const int32_t *offsets, void *dW,
                             abft_dtype dtype, const abft_shape *s, void *stream);
 
