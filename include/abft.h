@@ -264,7 +264,7 @@ int abft_gemm_scaled(abft_ctx *ctx, const void *A, const void *B, const abft_sca
  * mode, K and what may follow the call: as in abft_gemm_scaled.  ABFT_DETECT: row_flag [M] (0 for rows of no group), col_flag [batch][N]; the
  * checksums, max|A|, max|B| and with them the tolerance are a group's own (where groups have few rows, a column's check and its max|A| are those of sixteen rows at
  * a time).  abft_encode_b with this shape encodes the B of all groups (it does not look at M).  An armed accumulator flip counts batch_idx in groups and
- * the row from its group's first.  The context serves s->M <= max_rows, batch * N <= max_cols,
+ * the row from its group's first (abft_inject with this shape; nothing is flipped in a row that the group turns out not to have).  The context serves s->M <= max_rows, batch * N <= max_cols,
  * batch * (K rounded up to 128) <= max_depth, batch <= max_batch; M <= 2^30, K <= 2^29, batch * N <= 2^27 (ABFT_ESHAPE).
  * The backward pass with respect to A is this call again: dA = dC B^T, that is, A := dC, B as it lies with transB
  * inverted, and N and K exchanged. */
@@ -367,7 +367,9 @@ int abft_discrepancy(abft_ctx *ctx, abft_dtype dtype, const abft_shape *s, int s
  * transB, else K x N); bit 0..7 for ABFT_I8, 0..15 otherwise.  What the checks see of such a flip
  * depends on when the checksums were taken: a flip before abft_gemm is part of the operands the
  * call encodes (consistent, hence silent); a weight flipped after abft_encode_b and used with
- * ABFT_B_CHECKSUM_CACHED shows as row flags in every row i with A[i,k] != 0. */
+ * ABFT_B_CHECKSUM_CACHED shows as row flags in every row i with A[i,k] != 0.
+ * Shapes of abft_gemm_grouped, whose M counts the rows of all groups, serve ABFT_INJECT_ACCUMULATOR and ABFT_INJECT_OPERAND_B
+ * as they are (neither holds batch * M against the context's max_rows); for A and the stored C, where (row, col) index all groups' rows, batch is 1. */
 int abft_inject(abft_ctx *ctx, void *C, abft_dtype dtype, const abft_shape *s, int64_t batch_idx,
                 int64_t row, int64_t col, int bit, int where, void *stream);
 

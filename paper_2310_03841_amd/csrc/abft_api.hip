@@ -181,7 +181,8 @@ extern "C" int abft_destroy(abft_ctx *c)
 static bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 
 // need: 1 = A, 2 = B, 4 = C
-static int check_shape(const abft_ctx *c, int dt, const abft_shape *s, int need, Shape *o, bool protect = true)
+// rows: something is kept for each row of every batch item.  Without, M may count the rows of all of them together, as it does for groups of rows.
+static int check_shape(const abft_ctx *c, int dt, const abft_shape *s, int need, Shape *o, bool protect = true, bool rows = true)
 {
     if (!c || !s) return ABFT_EINVAL;
     if (dt != ABFT_I8 && dt != ABFT_BF16 && dt != ABFT_F16) return ABFT_EINVAL;
@@ -203,8 +204,7 @@ static int check_shape(const abft_ctx *c, int dt, const abft_shape *s, int need,
         if ((need & 4) && (s->strideC < s->M * s->ldc || (s->strideC * os) % 16)) return ABFT_EALIGN;
     }
     const int64_t Kp = round_up(s->K, SLAB_BYTES / es);
-    // (a call on B alone keeps nothing for the rows of A, which groups share out among them)
-    if ((need != 2 && s->batch * s->M > c->cfg.max_rows) || s->batch * s->N > c->cfg.max_cols ||
+    if ((rows && s->batch * s->M > c->cfg.max_rows) || s->batch * s->N > c->cfg.max_cols ||
         s->batch * Kp > c->cfg.max_depth || s->batch > c->cfg.max_batch)
         return ABFT_EWORKSPACE;
     o->M = (int)s->M; o->N = (int)s->N; o->K = (int)s->K; o->batch = (int)s->batch; o->transB = s->transB;
@@ -362,7 +362,7 @@ static int begin_b_pass(abft_ctx *ctx, hipStream_t st)
 extern "C" int abft_encode_b(abft_ctx *ctx, const void *B, abft_dtype dtype, const abft_shape *s, void *stream)
 {
     Shape sh;
-    int rc = check_shape(ctx, dtype, s, 2, &sh);
+    int rc = check_shape(ctx, dtype, s, 2, &sh, true, false);
     if (rc) return rc;
     if (!B) return ABFT_EINVAL;
     if (!aligned16(B)) return ABFT_EALIGN;
@@ -975,7 +975,7 @@ extern "C" int abft_inject(abft_ctx *ctx, void *C, abft_dtype dtype, const abft_
     if (where == ABFT_INJECT_OPERAND_A || where == ABFT_INJECT_OPERAND_B) {
         // a bit of an element of the stored operand array: A is M x K; B is N x K or K x N as stored
         const bool isA = where == ABFT_INJECT_OPERAND_A;
-        int rc = check_shape(ctx, dtype, s, isA ? 1 : 2, &sh, false);
+        int rc = check_shape(ctx, dtype, s, isA ? 1 : 2, &sh, false, isA);
         if (rc) return rc;
         if (!C) return ABFT_EINVAL;
         const int64_t rows = isA ? sh.M : (sh.transB ? sh.N : sh.K), cols = isA ? sh.K : (sh.transB ? sh.K : sh.N);
@@ -985,7 +985,8 @@ extern "C" int abft_inject(abft_ctx *ctx, void *C, abft_dtype dtype, const abft_
         HIP_TRY(launch_flip_at(C, idx, elem_size(dtype), bit, (hipStream_t)stream));
         return ABFT_OK;
     }
-    int rc = check_shape(ctx, dtype, s, where == ABFT_INJECT_STORED_C ? 4 : 0, &sh);
+    // (a flip is armed for a call that checks its own shape, and the place against it)
+    int rc = check_shape(ctx, dtype, s, where == ABFT_INJECT_STORED_C ? 4 : 0, &sh, true, where != ABFT_INJECT_ACCUMULATOR);
     if (rc) return rc;
     if (batch_idx < 0 || batch_idx >= sh.batch || row < 0 || row >= sh.M || col < 0 || col >= sh.N)
         return ABFT_EINVAL;

@@ -269,6 +269,53 @@ def test_a_flip_in_an_accumulator_is_found(dtype, out, ends, N, K, trans_b):
         p.close()
 
 
+def one_flip(p, clean, g, i, j, bit, mode):
+    """A flip armed with the call's own shape: what differs in C, and what is flagged, is its element."""
+    rc = ab.abft_inject(p.ctx, None, p.code, p.shape, g, i, j, bit, ab.ABFT_INJECT_ACCUMULATOR)
+    assert rc == ab.ABFT_OK, (g, i, j, ab.abft_strerror(rc))
+    p.run(mode)
+    at = p.ends[g] + i
+    differs = (p.C.view(torch.int16 if p.C.element_size() == 2 else torch.int32) != clean).nonzero().tolist()
+    assert differs == [[at, j]], (g, i, j, bit, differs[:5])
+    if mode != ab.ABFT_OFF:
+        rf, cf = p.row_flag.nonzero().flatten().tolist(), p.col_flag.nonzero().flatten().tolist()
+        assert rf == [at] and cf == [g * p.N + j], (g, i, j, bit, rf[:5], cf[:5])
+        assert p.counts[:5].tolist() == [1, 1, ab.ABFT_LOCALISED, 0, ab.ABFT_LOCALISED]
+
+
+def stored_bits(p):
+    return p.C.clone().view(torch.int16 if p.C.element_size() == 2 else torch.int32)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,out", TYPES)
+@pytest.mark.parametrize("ends,N,K,trans_b", [([0, 0, 7], 70, 96, True), ([2, 5, 290], 200, 136, False), ([0, 20, 1500, 1500], 520, 384, True)])
+def test_a_flip_is_armed_with_the_shape_of_the_call(dtype, out, ends, N, K, trans_b):
+    """M of a grouped call counts the rows of all groups; a context of its size takes a flip in any of a group's rows.  Bit 30 moves a floating-point sum by 2 at
+    least; the tolerance is 1e-3 K max|A| max|B| < 1e-3 384 5.2 0.52 = 1.04."""
+    p = Group(dtype, ends, N, K, trans_b, M=ends[-1] + 3, out=out, seed=13)
+    try:
+        p.run(ab.ABFT_DETECT)
+        p.check()
+        clean = stored_bits(p)
+        g = max(range(p.groups), key=lambda e: p.ends[e + 1] - p.ends[e])
+        rows = p.ends[g + 1] - p.ends[g]
+        for i, j in ((0, 0), (rows - 1, N - 1), (rows // 2, N // 3)):
+            for mode in (ab.ABFT_OFF, ab.ABFT_DETECT):
+                one_flip(p, clean, g, i, j, 30, mode)
+        # a row that the group does not have: armed, and gone with the next call
+        assert ab.abft_inject(p.ctx, None, p.code, p.shape, g, rows, 0, 30, ab.ABFT_INJECT_ACCUMULATOR) == ab.ABFT_OK
+        for _ in range(2):
+            p.run(ab.ABFT_DETECT)
+            p.clean()
+            assert torch.equal(stored_bits(p), clean)
+        inject = lambda *at: ab.abft_inject(p.ctx, None, p.code, p.shape, *at, 30, ab.ABFT_INJECT_ACCUMULATOR)
+        for at in ((p.groups, 0, 0), (-1, 0, 0), (0, p.M, 0), (0, -1, 0), (0, 0, N), (0, 0, -1)):
+            assert inject(*at) == ab.ABFT_EINVAL, at
+    finally:
+        p.close()
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype,out", [("i8", "bf16"), ("i8", None), ("bf16", None)])
 def test_a_weight_that_changed_behind_its_encoding_shows_in_rows(dtype, out):
