@@ -247,8 +247,8 @@ typedef struct {
  * be OR-ed with ABFT_B_CHECKSUM_CACHED (others: ABFT_EINVAL).  What is checked are the int32 sums ahead of the scales, by
  * equality as in abft_gemm, so every single fault of the product shows whatever the scales are; faults behind the sums (scales, rounding,
  * C in memory) do not.  batch must be 1 (ABFT_ESHAPE); K may exceed 4096, K * 2^14 < 2^31.
- * abft_verify, abft_correct and abft_discrepancy have nothing to go by behind this call (ABFT_ESTATE), and abft_workspace has no vectors
- * of it.  An armed accumulator flip (abft_inject) and the event of abft_gemm_done_event are honoured as by abft_gemm.
+ * abft_verify, abft_correct, abft_correct_checksum and abft_discrepancy have nothing to go by behind this call in either mode (ABFT_ESTATE: what an earlier
+ * abft_gemm had left is given up), and abft_workspace has no vectors of it.  An armed accumulator flip (abft_inject) and the event of abft_gemm_done_event are honoured as by abft_gemm.
  * Enqueues, protected: the pass over B, unless its checksum is cached; the product, whose launch also passes over A; the check
  * kernel. */
 int abft_gemm_scaled(abft_ctx *ctx, const void *A, const void *B, const abft_scales *scales, void *C, int mode,

@@ -781,6 +781,9 @@ static int group_impl(abft_ctx *ctx, const void *A, const void *B, const int32_t
     g.inj_b = arm.batch; g.inj_row = arm.row; g.inj_col = arm.col; g.inj_bit = arm.bit;
     if (q) { g.row_scale = q->row; g.col_scale = q->col; g.bias = q->bias; }
     if (base == ABFT_OFF) {
+        // (predictions of an earlier product of the same sizes are not this one's)
+        ctx->pred_valid = false;
+        ctx->vobs_valid = false;
         ctx->arm.batch = -1;
         HIP_TRY(launch_group(dtype, ot, false, sh.transB != 0, g, nullptr, nullptr, st));
         if (ctx->done_event && !capturing(st)) HIP_TRY(hipEventRecord(ctx->done_event, st));

@@ -799,6 +799,31 @@ def test_grouped_and_other_calls_share_a_context():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("mode", [ab.ABFT_OFF, ab.ABFT_DETECT])
+@pytest.mark.parametrize("scaled", [False, True])
+def test_nothing_to_verify_by_behind_a_grouped_call_of_either_mode(mode, scaled):
+    """The predictions of an earlier product of the same sizes are not another's: a C that no protected product made is refused, not judged by them."""
+    M, N, K = 64, 128, 64
+    ctx = ab.abft_create(M, N, K, 1)
+    p = Group("i8", [0, M], N, K, out="f16" if scaled else None, seed=14, ctx=ctx, dense=scaled)
+    A, B = rand(torch.Generator().manual_seed(15), "i8", M, K).cuda(), rand(torch.Generator().manual_seed(16), "i8", N, K).cuda()
+    C = torch.zeros(M, N, dtype=torch.int32, device="cuda")
+    s = ab.make_shape(M, N, K)
+    res = ab.make_result(p.row_flag, p.col_flag, p.counts)
+    try:
+        assert ab.abft_gemm(ctx, A, B, C, ab.ABFT_I8, ab.ABFT_DETECT, s, res) == ab.ABFT_OK
+        assert ab.abft_verify(ctx, C, ab.ABFT_I8, s, res) == ab.ABFT_OK
+        p.run(mode)
+        assert ab.abft_verify(ctx, C, ab.ABFT_I8, s, res) == ab.ABFT_ESTATE
+        assert ab.abft_correct(ctx, A, B, C, ab.ABFT_I8, s, res) == ab.ABFT_ESTATE
+        assert ab.abft_correct_checksum(ctx, C, ab.ABFT_I8, s, res) == ab.ABFT_ESTATE
+        p.check()
+    finally:
+        torch.cuda.synchronize()
+        ab.abft_destroy(ctx)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("bad", [[0, 50, 20, 64], [-5, 10, 30, 400], [2 ** 31 - 1, -2 ** 31, 64, 64], [64, 0, 0, 64]])
 def test_bad_offsets_address_nothing_outside(bad):
     """Offsets that fall or point outside: A and C lie inside larger buffers, whose other rows stay as they are."""
