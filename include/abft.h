@@ -265,7 +265,9 @@ int abft_gemm_scaled(abft_ctx *ctx, const void *A, const void *B, const abft_sca
  * checksums, max|A|, max|B| and with them the tolerance are a group's own (where groups have few rows, a column's check and its max|A| are those of sixteen rows at
  * a time).  abft_encode_b with this shape encodes the B of all groups (it does not look at M).  An armed accumulator flip counts batch_idx in groups and
  * the row from its group's first (abft_inject with this shape; nothing is flipped in a row that the group turns out not to have).  The context serves s->M <= max_rows, batch * N <= max_cols,
- * batch * (K rounded up to 128) <= max_depth, batch <= max_batch; M <= 2^30, K <= 2^29, batch * N <= 2^27 (ABFT_ESHAPE).
+ * batch * (K rounded up to 128) <= max_depth, batch <= max_batch; M <= 2^30, K <= 2^29, batch * N <= 2^27 (ABFT_ESHAPE).  Products whose
+ * tiles outnumber the workgroups of a launch (2^24; from some 2^36 elements of C on, or, protected, M * ceil(bytes of a row of A / 1024) above 2^29) are
+ * ABFT_ESHAPE too, like every refusal before the context or the stream has changed.
  * The backward pass with respect to A is this call again: dA = dC B^T, that is, A := dC, B as it lies with transB
  * inverted, and N and K exchanged. */
 int abft_gemm_grouped(abft_ctx *ctx, const void *A, const void *B, const int32_t *offsets, const abft_scales *scales,
@@ -275,7 +277,8 @@ int abft_gemm_grouped(abft_ctx *ctx, const void *A, const void *B, const int32_t
  * dW[e] = dY_e^T X_e (N x K, transB = 1) or X_e^T dY_e (K x N, transB = 0), as B lies in memory.  s: the shape of the
  * forward call: X is its A (lda), dY has the layout of its C (ldc, elements of dtype), dW that of its B (ldb, strideB, which must keep the
  * groups apart: ABFT_ESHAPE).  ABFT_BF16 or ABFT_F16, sums in fp32, rounded once.  A group without rows gets zeros.  Unprotected.  The
- * context serves the shapes it serves the forward call for, and keeps nothing of this one. */
+ * context serves the shapes it serves the forward call for, and keeps nothing of this one.  Gradients of more tiles than a launch has workgroups (from some 2^36
+ * elements on): ABFT_ESHAPE. */
 int abft_gemm_grouped_wgrad(abft_ctx *ctx, const void *X, const void *dY, const int32_t *offsets, void *dW,
                             abft_dtype dtype, const abft_shape *s, void *stream);
 

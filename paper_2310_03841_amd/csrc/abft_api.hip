@@ -711,8 +711,8 @@ static GroupArgs group_args(const void *A, const void *B, void *C, const int32_t
 
 // The kernels of a protected call: the pass over the matrices (unless their encoding is cached), the product, whose launch also passes
 // over A, and the check.  The regions it accumulates into alternate as those of enqueue_tiled.
-static int enqueue_group(abft_ctx *ctx, int dtype, int ot, bool cached, GroupArgs &g, const void *B, const Shape &sh, const Verdict &v,
-                         hipStream_t st)
+static int enqueue_group(abft_ctx *ctx, int dtype, int ot, bool cached, const GroupKernel &k, GroupArgs &g, const void *B, const Shape &sh,
+                         const Verdict &v, hipStream_t st)
 {
     const bool gm = in_graph_mode(ctx, st);
     const int prev = ctx->cur;
@@ -745,9 +745,9 @@ static int enqueue_group(abft_ctx *ctx, int dtype, int ot, bool cached, GroupArg
     if (!cached) HIP_TRY(launch_encode_b(dtype, B, sh, w, w.cc_obs, stale, st));
     else if (stale) HIP_TRY(launch_zero(w.cc_obs, stale, st));
     ctx->sto_valid = false;
-    HIP_TRY(launch_group(dtype, ot, true, sh.transB != 0, g, w.b_max, &v, st));
+    HIP_TRY(launch_group(dtype, ot, true, sh.transB != 0, k, g, w.b_max, &v, st));
     if (ctx->done_event && !gm) HIP_TRY(hipEventRecord(ctx->done_event, st));
-    HIP_TRY(launch_group_check(dtype, g, sh.transB != 0, w, v, end, st));
+    HIP_TRY(launch_group_check(dtype, k, g, sh.transB != 0, w, v, end, st));
     if (!gm) {
         ctx->bclean[ctx->bslot ^ 1] = true;
         ctx->dirty[prev] = 0;
@@ -780,12 +780,14 @@ static int group_impl(abft_ctx *ctx, const void *A, const void *B, const int32_t
     GroupArgs g = group_args(A, B, C, offsets, sh);
     g.inj_b = arm.batch; g.inj_row = arm.row; g.inj_col = arm.col; g.inj_bit = arm.bit;
     if (q) { g.row_scale = q->row; g.col_scale = q->col; g.bias = q->bias; }
+    GroupKernel k;
+    if (!group_plan(dtype, sh.transB != 0, base != ABFT_OFF, g, &k)) return ABFT_ESHAPE;
     if (base == ABFT_OFF) {
         // (predictions of an earlier product of the same sizes are not this one's)
         ctx->pred_valid = false;
         ctx->vobs_valid = false;
         ctx->arm.batch = -1;
-        HIP_TRY(launch_group(dtype, ot, false, sh.transB != 0, g, nullptr, nullptr, st));
+        HIP_TRY(launch_group(dtype, ot, false, sh.transB != 0, k, g, nullptr, nullptr, st));
         if (ctx->done_event && !capturing(st)) HIP_TRY(hipEventRecord(ctx->done_event, st));
         return ABFT_OK;
     }
@@ -798,7 +800,7 @@ static int group_impl(abft_ctx *ctx, const void *A, const void *B, const int32_t
     ctx->vobs_valid = false;
     if (!cached) ctx->b_valid = false;
     ctx->arm.batch = -1;
-    rc = enqueue_group(ctx, dtype, ot, cached, g, B, sh, v, st);
+    rc = enqueue_group(ctx, dtype, ot, cached, k, g, B, sh, v, st);
     if (rc) return rc;
     ctx->b_valid = true;
     ctx->b_dt = dtype;
@@ -838,7 +840,9 @@ extern "C" int abft_gemm_grouped_wgrad(abft_ctx *ctx, const void *X, const void 
     g.ldc = sh.ldb;
     g.K = sh.transB ? sh.N : sh.K;
     g.N = sh.transB ? sh.K : sh.N;
-    HIP_TRY(launch_group_wgrad(dtype, g, (hipStream_t)stream));
+    GroupKernel k;
+    if (!group_plan_wgrad(g, &k)) return ABFT_ESHAPE;
+    HIP_TRY(launch_group_wgrad(dtype, k, g, (hipStream_t)stream));
     return ABFT_OK;
 }
 

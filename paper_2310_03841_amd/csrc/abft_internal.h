@@ -177,11 +177,13 @@ hipError_t launch_mfma_peak(int dt, int blocks, int iters, unsigned long long *c
 
 // Products over groups of rows (gemm_group.hip, group_check.hip); what a launch takes is in group_args.h.
 struct GroupArgs;
+struct GroupKernel;
 // dt: of the operands, ot: of C (int8 operands: DT_I8 for the int32 sums, or the type of the scaled values)
 // b_max, v: protected
-hipError_t launch_group(int dt, int ot, bool protect, bool transB, GroupArgs &g, const uint32_t *b_max, const Verdict *v, hipStream_t st);
-hipError_t launch_group_check(int dt, const GroupArgs &g, bool transB, const Workspace &w, const Verdict &v, const OneLaunch &end, hipStream_t st);
-hipError_t launch_group_wgrad(int dt, GroupArgs &g, hipStream_t st);
+// k: group_plan's, group_plan_wgrad's
+hipError_t launch_group(int dt, int ot, bool protect, bool transB, const GroupKernel &k, GroupArgs &g, const uint32_t *b_max, const Verdict *v, hipStream_t st);
+hipError_t launch_group_check(int dt, const GroupKernel &k, const GroupArgs &g, bool transB, const Workspace &w, const Verdict &v, const OneLaunch &end, hipStream_t st);
+hipError_t launch_group_wgrad(int dt, const GroupKernel &k, GroupArgs &g, hipStream_t st);
 hipError_t launch_quantize_rows(int dt, const void *X, int rows, int cols, long ldx, void *Q, long ldq, float *scale, hipStream_t st);
 
 }  // namespace abft

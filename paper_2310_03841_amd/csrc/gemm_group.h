@@ -430,7 +430,6 @@ static hipError_t launch_one(GroupArgs &g, hipStream_t st)
     g.group_inv = map_inverse(g.tiles_n);
     const long tiles_m = GROUP == GROUP_DEPTH ? ceil_div(g.K, BM) * g.groups : row_tiles(g.M, g.groups, BM);
     const long wgs = (PROT ? g.n_pass : 0) + ceil_div(tiles_m * g.tiles_n, 8) * 8;
-    if (wgs > MAX_GRID_X) return hipErrorInvalidValue;
     hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), smem, st, g);
     return hipGetLastError();
 }

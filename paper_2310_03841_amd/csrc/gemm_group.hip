@@ -47,7 +47,7 @@ static double few_us(const GroupProblem &p)
     return (slow ? 3.0 : p.protect ? 1.0 : 0.5) + tiles * (slow ? 1e-3 : 2e-3) + std::max(read, (double)p.groups * p.N * row / 5e6);
 }
 
-GroupKernel group_kernel(int dt, bool transB, bool protect, const GroupArgs &g)
+static GroupKernel group_kernel(int dt, bool transB, bool protect, const GroupArgs &g)
 {
     const int es = elem_size(dt), ke = SLAB_BYTES / es;
     const GroupProblem p = {(int)ceil_div(g.M, g.groups), g.N, g.K, g.groups, es, protect, false};
@@ -64,16 +64,31 @@ GroupKernel group_kernel(int dt, bool transB, bool protect, const GroupArgs &g)
     return best;
 }
 
-hipError_t launch_group(int dt, int ot, bool protect, bool transB, GroupArgs &g, const uint32_t *b_max, const Verdict *v, hipStream_t st)
+// Workgroups of a kernel's launch that take tiles (launch_one, launch_few_one), or tiles of the list that a launch of one to a compute unit walks; tall: rows of
+// tiles by their height.
+template <typename F> static bool tiles_fit(const GroupKernel &k, const GroupArgs &g, long n_pass, const F &tall)
 {
+    if (k.kind == GROUP_KERNEL_BIG) return tall(128) * ceil_div(g.N, 256) < 1L << 31;
+    const long wgs = k.kind == GROUP_KERNEL_FEW ? group_few_workgroups(g) : ceil_div(tall(64) * ceil_div(g.N, k.tiles == TILE_64_128 ? 128 : 64), 8) * 8;
+    return n_pass + wgs <= MAX_GRID_X;
+}
+
+bool group_plan(int dt, bool transB, bool protect, GroupArgs &g, GroupKernel *k)
+{
+    long n_pass = 0;
     if (protect) {
         g.pass_win = (int)ceil_div((long)g.K * elem_size(dt), PASS_BYTES);
         g.pass_inv = map_inverse(g.pass_win);
-        const long units = row_tiles(g.M, g.groups, 4 * PASS_ROWS) * g.pass_win;
-        if (units > MAX_GRID_X) return hipErrorInvalidValue;
-        g.n_pass = (int)ceil_div(units, 8) * 8;
+        n_pass = ceil_div(row_tiles(g.M, g.groups, 4 * PASS_ROWS) * g.pass_win, 8) * 8;
+        if (n_pass > MAX_GRID_X) return false;
+        g.n_pass = (int)n_pass;
     }
-    const GroupKernel k = group_kernel(dt, transB, protect, g);
+    *k = group_kernel(dt, transB, protect, g);
+    return tiles_fit(*k, g, n_pass, [&](int bm) { return row_tiles(g.M, g.groups, bm); });
+}
+
+hipError_t launch_group(int dt, int ot, bool protect, bool transB, const GroupKernel &k, GroupArgs &g, const uint32_t *b_max, const Verdict *v, hipStream_t st)
+{
     switch (k.kind) {
     case GROUP_KERNEL_FEW: {
         const float tau = !v ? 0.f : v->tau_override_cols > 0.f ? v->tau_override_cols : v->tau_override;
@@ -95,16 +110,22 @@ hipError_t launch_group(int dt, int ot, bool protect, bool transB, GroupArgs &g,
     }
 }
 
-hipError_t launch_group_wgrad(int dt, GroupArgs &g, hipStream_t st)
+bool group_plan_wgrad(const GroupArgs &g, GroupKernel *k)
 {
     const GroupProblem p = {g.K, g.N, (int)ceil_div(g.M, g.groups), g.groups, 2, false, true};
     constexpr long ALL = 1L << 31;
     // (a group's depth may be nearly all rows; of a slab more than there are, three at least, is asked for)
     const long most = ((long)g.M + 4 * 64) * 2;
     const double wide = tile_us(p, TILE_64_128), square = tile_us(p, TILE_64);
-    if (most * g.lda < ALL && most * g.ldb < ALL && g.groups <= 4096 && big_us(p) < std::min(wide, square)) return launch_group_big_wgrad(dt, g, st);
-    const int tiles = wide < square ? TILE_64_128 : ceil_div(p.rows, 64) * ceil_div(p.N, 64) * p.groups <= 256 ? TILE_64_4 : TILE_64;
-    return dt == DT_BF16 ? launch_group_depth_bf16(tiles, g, st) : launch_group_depth_f16(tiles, g, st);
+    k->kind = most * g.lda < ALL && most * g.ldb < ALL && g.groups <= 4096 && big_us(p) < std::min(wide, square) ? GROUP_KERNEL_BIG : GROUP_KERNEL_TILE;
+    k->tiles = wide < square ? TILE_64_128 : ceil_div(p.rows, 64) * ceil_div(p.N, 64) * p.groups <= 256 ? TILE_64_4 : TILE_64;
+    return tiles_fit(*k, g, 0, [&](int bm) { return ceil_div(g.K, bm) * g.groups; });
+}
+
+hipError_t launch_group_wgrad(int dt, const GroupKernel &k, GroupArgs &g, hipStream_t st)
+{
+    if (k.kind == GROUP_KERNEL_BIG) return launch_group_big_wgrad(dt, g, st);
+    return dt == DT_BF16 ? launch_group_depth_bf16(k.tiles, g, st) : launch_group_depth_f16(k.tiles, g, st);
 }
 
 }  // namespace abft

@@ -325,6 +325,18 @@ bool group_few_fits(int dt, bool protect, const GroupArgs &g)
     return !protect || (g.M <= 32L * g.groups && ((long)g.K * elem_size(dt) + 15) / 16 * 32 <= FEW_MAX_SUMS);
 }
 
+// 32 columns to a workgroup, which reads its rows of A once for both halves, unless that leaves compute units without one.
+int group_few_columns(const GroupArgs &g)
+{
+    return (long)std::min(g.M, g.groups) * ((g.M / g.groups + 15) / 16) * ((g.N + 31) / 32) >= 512 ? 32 : 16;
+}
+
+long group_few_workgroups(const GroupArgs &g)
+{
+    const int bn = group_few_columns(g);
+    return ((g.groups == 1 ? (g.M + 15) / 16 : g.M / 16 + std::min(g.M, g.groups)) * (long)((g.N + bn - 1) / bn) + 7) / 8 * 8;
+}
+
 template <int DT, int OT, bool PROT, int NB> static hipError_t launch_few_one(FewArgs &f, hipStream_t st)
 {
     GroupArgs &g = f.g;
@@ -336,17 +348,14 @@ template <int DT, int OT, bool PROT, int NB> static hipError_t launch_few_one(Fe
     if (e != hipSuccess) return e;
     g.tiles_n = (g.N + 16 * NB - 1) / (16 * NB);
     g.group_inv = map_inverse(g.tiles_n);
-    const long tiles = (g.groups == 1 ? (g.M + 15) / 16 : g.M / 16 + std::min(g.M, g.groups)) * (long)g.tiles_n;
-    const long wgs = (PROT ? g.n_pass : 0) + (tiles + 7) / 8 * 8;
-    if (wgs > MAX_GRID_X) return hipErrorInvalidValue;
+    const long wgs = (PROT ? g.n_pass : 0) + group_few_workgroups(g);
     hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), smem, st, f);
     return hipGetLastError();
 }
 
-// 32 columns to a workgroup, which reads its rows of A once for both halves, unless that leaves compute units without one.
 template <int DT, int OT> static hipError_t launch_few_type(bool protect, FewArgs &f, hipStream_t st)
 {
-    const bool wide = (long)std::min(f.g.M, f.g.groups) * ((f.g.M / f.g.groups + 15) / 16) * ((f.g.N + 31) / 32) >= 512;
+    const bool wide = group_few_columns(f.g) == 32;
     if (protect) return wide ? launch_few_one<DT, OT, true, 2>(f, st) : launch_few_one<DT, OT, true, 1>(f, st);
     return wide ? launch_few_one<DT, OT, false, 2>(f, st) : launch_few_one<DT, OT, false, 1>(f, st);
 }

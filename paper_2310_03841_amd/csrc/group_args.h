@@ -135,9 +135,14 @@ template <int BM> __device__ __forceinline__ bool find_tile(const GroupArgs &g, 
 // (gemm_group_few.hip), whose kernel checks the columns itself: cc_obs then holds a mark for each that disagrees.
 enum { GROUP_KERNEL_TILE, GROUP_KERNEL_BIG, GROUP_KERNEL_FEW };
 struct GroupKernel { int kind, tiles; };
-GroupKernel group_kernel(int dt, bool transB, bool protect, const GroupArgs &g);
-// Whether the kernel of few rows has room for what it keeps.
+// Of a product, and of a gradient of weights; what g says of the pass over A.  False: more workgroups, or tiles in its list, than a launch or an int counts.
+// Asked once to a call, ahead of all that changes anything.
+bool group_plan(int dt, bool transB, bool protect, GroupArgs &g, GroupKernel *k);
+bool group_plan_wgrad(const GroupArgs &g, GroupKernel *k);
+// Whether the kernel of few rows has room for what it keeps; its columns to a workgroup; workgroups with tiles.
 bool group_few_fits(int dt, bool protect, const GroupArgs &g);
+int group_few_columns(const GroupArgs &g);
+long group_few_workgroups(const GroupArgs &g);
 // Its shares of the observed sums of rows, for every sixteen columns one after the other, [M] words each: they take the place of the sums in doubles (2 (groups N +
 // M) words), of which it keeps none.
 inline uint32_t *group_few_shares(const GroupArgs &g) { return reinterpret_cast<uint32_t *>(g.cc_acc); }

@@ -169,7 +169,7 @@ __global__ __launch_bounds__(256) void group_check_kernel(GroupCheckArgs f)
     if (nf && lane == 0) report_flags(f.counts, 1, nf);
 }
 
-hipError_t launch_group_check(int dt, const GroupArgs &g, bool transB, const Workspace &w, const Verdict &v, const OneLaunch &end, hipStream_t st)
+hipError_t launch_group_check(int dt, const GroupKernel &k, const GroupArgs &g, bool transB, const Workspace &w, const Verdict &v, const OneLaunch &end, hipStream_t st)
 {
     constexpr int RW = 4;
     GroupCheckArgs f;
@@ -182,12 +182,12 @@ hipError_t launch_group_check(int dt, const GroupArgs &g, bool transB, const Wor
     f.row_flag = v.row_flag; f.col_flag = v.col_flag; f.counts = v.counts;
     f.zero_ptr = end.zero_ptr; f.zero_words = end.zero_ptr ? end.zero_words : 0;
     f.zero2_ptr = end.zero2_ptr; f.zero2_words = end.zero2_ptr ? end.zero2_words : 0;
-    const bool marked = group_kernel(dt, transB, true, g).kind == GROUP_KERNEL_FEW;
+    const bool marked = k.kind == GROUP_KERNEL_FEW;
     const int per = transB ? 4 * RW : GCHK_KN_LANES * (16 / elem_size(dt));
     f.row_units = marked ? (g.M + 3) / 4 : (g.M + 255) / 256;
     f.col_units = (g.N + per - 1) / per;
+    // at most 2^22 units of rows (marked: of at most 2^21 rows) and 2^23 + 2^16 of columns, for up to 2^30 rows and 2^27 columns over all groups
     const long cols = (long)g.N * g.groups, units = f.row_units + (marked ? (cols + 255) / 256 : (long)f.col_units * g.groups);
-    if (units > MAX_GRID_X || cols > 0x7FFFFFFFL) return hipErrorInvalidValue;
     const dim3 grid((unsigned)units);
 #define GROUP_CHECK(DT) \
     if (marked)      hipLaunchKernelGGL((group_check_kernel<DT, RW, COLS_MARKED>), grid, dim3(256), 0, st, f); \

@@ -901,3 +901,29 @@ def test_refusals():
             assert g(s) == ab.ABFT_ESHAPE and w(s) == ab.ABFT_ESHAPE
     finally:
         ab.abft_destroy(ctx)
+
+
+@pytest.mark.gpu
+def test_products_of_more_tiles_than_a_launch_are_refused_by_their_shape():
+    """2^24 tiles of 64 x 128, one more than a launch has workgroups.  Nothing is launched: the pointers are never followed, and the context is as it was."""
+    P = 0x1000
+    ctx = ab.abft_create(1 << 19, 1 << 19, 1 << 18, 1)
+    try:
+        B = torch.zeros(1 << 18, 8, dtype=torch.bfloat16, device="cuda")
+        s = ab.make_shape(1 << 19, 1 << 18, 8)
+        assert ab.abft_encode_b(ctx, B, ab.ABFT_BF16, s) == ab.ABFT_OK
+        torch.cuda.synchronize()
+        for mode in (ab.ABFT_OFF, ab.ABFT_DETECT, ab.ABFT_DETECT | ab.ABFT_B_CHECKSUM_CACHED):
+            assert ab.abft_gemm_grouped(ctx, P, P, P, None, P, ab.ABFT_BF16, mode, s, ab.make_result(P, P, P)) == ab.ABFT_ESHAPE
+        # (the encoding is still there: of a product of few rows it is asked for and found)
+        small = ab.make_shape(1, 1 << 18, 8)
+        A, C, off = torch.ones(1, 8, dtype=torch.bfloat16, device="cuda"), torch.ones(1, 1 << 18, dtype=torch.bfloat16, device="cuda"), torch.tensor([0, 1], dtype=torch.int32).cuda()
+        rf, cf, cnt = (torch.zeros(n, dtype=t, device="cuda") for n, t in ((1, torch.uint8), (1 << 18, torch.uint8), (8, torch.int32)))
+        rc = ab.abft_gemm_grouped(ctx, A, B, off, None, C, ab.ABFT_BF16, ab.ABFT_DETECT | ab.ABFT_B_CHECKSUM_CACHED, small, ab.make_result(rf, cf, cnt))
+        assert rc == ab.ABFT_OK, ab.abft_strerror(rc)
+        torch.cuda.synchronize()
+        assert not C.any() and cnt[:3].tolist() == [0, 0, 0]
+        # gradients of 2^37 elements whose rows lie too far apart for the tiles that a launch's workgroups walk
+        assert ab.abft_gemm_grouped_wgrad(ctx, P, P, P, P, ab.ABFT_BF16, ab.make_shape(8192, 1 << 19, 1 << 18)) == ab.ABFT_ESHAPE
+    finally:
+        ab.abft_destroy(ctx)
