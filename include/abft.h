@@ -265,9 +265,9 @@ int abft_gemm_scaled(abft_ctx *ctx, const void *A, const void *B, const abft_sca
  * checksums, max|A|, max|B| and with them the tolerance are a group's own (where groups have few rows, a column's check and its max|A| are those of sixteen rows at
  * a time).  abft_encode_b with this shape encodes the B of all groups (it does not look at M).  An armed accumulator flip counts batch_idx in groups and
  * the row from its group's first (abft_inject with this shape; nothing is flipped in a row that the group turns out not to have).  The context serves s->M <= max_rows, batch * N <= max_cols,
- * batch * (K rounded up to 128) <= max_depth, batch <= max_batch; M <= 2^30, K <= 2^29, batch * N <= 2^27 (ABFT_ESHAPE).  Products whose
- * tiles outnumber the workgroups of a launch (2^24; from some 2^36 elements of C on, or, protected, M * ceil(bytes of a row of A / 1024) above 2^29) are
- * ABFT_ESHAPE too, like every refusal before the context or the stream has changed.
+ * batch * (K rounded up to 128) <= max_depth, batch <= max_batch; M <= 2^30, K <= 2^29, batch * N <= 2^27 (ABFT_ESHAPE).  Products of more
+ * workgroups than a launch has, 2^24 - 1, are ABFT_ESHAPE too, like every refusal before the context or the stream has changed: there may be one to 64 x 64
+ * elements of C (fewer by other tiles), and, protected, there is one to 32 rows and 1024 bytes of each row of A.
  * The backward pass with respect to A is this call again: dA = dC B^T, that is, A := dC, B as it lies with transB
  * inverted, and N and K exchanged. */
 int abft_gemm_grouped(abft_ctx *ctx, const void *A, const void *B, const int32_t *offsets, const abft_scales *scales,
@@ -382,6 +382,10 @@ int abft_workspace(abft_ctx *ctx, int which, const abft_shape *s, void **ptr, in
 /* Tile the GEMM kernel uses for a protected call of this problem (rows, cols of C per workgroup; M, N where
  * a workgroup takes a whole batch item). */
 int abft_tile_shape(abft_dtype dtype, const abft_shape *s, int *tile_m, int *tile_n);
+/* The same for abft_gemm_grouped and abft_gemm_scaled, in the mode of the call (ABFT_OFF or ABFT_DETECT), counted from the first row of a group and the first
+ * column: 16 x 16 or 32, 64 x 64 or 128, or 256 x 256 (where the last rows of a group, and tiles of the last round, are 128 high).  It needs no context and no
+ * GPU, and refuses a shape as the calls do; a C of 16-bit values is taken for one of int32 in its alignment. */
+int abft_group_tile_shape(abft_dtype dtype, int mode, const abft_shape *s, int *tile_m, int *tile_n);
 
 /* Kernel timing for reports (not a hot call: creates HIP events).  Between begin and end every
  * abft_gemm records events on the caller's stream around its kernels; up to max_calls calls are

@@ -672,10 +672,9 @@ extern "C" int abft_gemm_static(const void *A, const void *B, void *C, abft_dtyp
 // ------------------------------------------------------------------------------------------
 // Products over groups of rows, with scales or without.
 
-// M: rows over all groups; batch: groups.  os: bytes of an element of C.
+// M: rows over all groups; batch: groups.  os: bytes of an element of C.  c: the context that is to hold the call, or null: the shape alone.
 static int check_group_shape(const abft_ctx *c, int dt, int os, const abft_shape *s, Shape *o)
 {
-    if (!c || !s) return ABFT_EINVAL;
     if (s->M < 1 || s->N < 1 || s->K < 1 || s->batch < 1) return ABFT_ESHAPE;
     // (bytes of a row of A, B and C, and of a tile behind its end, are counted in 32 bits; columns of all groups, by the check kernel's workgroups)
     if (s->M > (1 << 30) || s->N > (1 << 29) || s->K > (1 << 29) || s->batch > 65535 || s->batch * s->N > (1 << 27)) return ABFT_ESHAPE;
@@ -686,8 +685,8 @@ static int check_group_shape(const abft_ctx *c, int dt, int os, const abft_shape
     if ((s->lda * es) % 16 || (s->ldb * es) % 16 || (s->ldc * os) % 16) return ABFT_EALIGN;
     if (s->batch > 1 && (s->strideB < 0 || (s->strideB * es) % 16)) return ABFT_EALIGN;
     const int64_t Kp = round_up(s->K, SLAB_BYTES / es);
-    if (s->M > c->cfg.max_rows || s->batch * s->N > c->cfg.max_cols || s->batch * Kp > c->cfg.max_depth ||
-        s->batch > c->cfg.max_batch)
+    if (c && (s->M > c->cfg.max_rows || s->batch * s->N > c->cfg.max_cols || s->batch * Kp > c->cfg.max_depth ||
+              s->batch > c->cfg.max_batch))
         return ABFT_EWORKSPACE;
     o->M = (int)s->M; o->N = (int)s->N; o->K = (int)s->K; o->batch = (int)s->batch; o->transB = s->transB;
     o->lda = s->lda; o->ldb = s->ldb; o->ldc = s->ldc;
@@ -770,6 +769,7 @@ static int group_impl(abft_ctx *ctx, const void *A, const void *B, const int32_t
         if (((uintptr_t)q->row & 3u) || ((uintptr_t)q->col & 3u) || ((uintptr_t)q->bias & 3u)) return ABFT_EALIGN;
         ot = q->out;
     }
+    if (!ctx || !s) return ABFT_EINVAL;
     Shape sh;
     int rc = check_group_shape(ctx, dtype, out_size(ot), s, &sh);
     if (rc) return rc;
@@ -827,6 +827,7 @@ extern "C" int abft_gemm_grouped_wgrad(abft_ctx *ctx, const void *X, const void 
                                        const abft_shape *s, void *stream)
 {
     if (dtype != ABFT_BF16 && dtype != ABFT_F16) return ABFT_EINVAL;
+    if (!ctx || !s) return ABFT_EINVAL;
     Shape sh;
     int rc = check_group_shape(ctx, dtype, elem_size(dtype), s, &sh);
     if (rc) return rc;
@@ -843,6 +844,21 @@ extern "C" int abft_gemm_grouped_wgrad(abft_ctx *ctx, const void *X, const void 
     GroupKernel k;
     if (!group_plan_wgrad(g, &k)) return ABFT_ESHAPE;
     HIP_TRY(launch_group_wgrad(dtype, k, g, (hipStream_t)stream));
+    return ABFT_OK;
+}
+
+extern "C" int abft_group_tile_shape(abft_dtype dtype, int mode, const abft_shape *s, int *tile_m, int *tile_n)
+{
+    if (!s || !tile_m || !tile_n) return ABFT_EINVAL;
+    if (dtype != ABFT_I8 && dtype != ABFT_BF16 && dtype != ABFT_F16) return ABFT_EINVAL;
+    if (mode != ABFT_OFF && mode != ABFT_DETECT) return ABFT_EINVAL;
+    Shape sh;
+    const int rc = check_group_shape(nullptr, dtype, out_size(dtype), s, &sh);
+    if (rc) return rc;
+    GroupArgs g = group_args(nullptr, nullptr, nullptr, nullptr, sh);
+    GroupKernel k;
+    if (!group_plan(dtype, sh.transB != 0, mode != ABFT_OFF, g, &k)) return ABFT_ESHAPE;
+    group_tile_shape(k, g, tile_m, tile_n);
     return ABFT_OK;
 }
 

@@ -64,12 +64,20 @@ static GroupKernel group_kernel(int dt, bool transB, bool protect, const GroupAr
     return best;
 }
 
+void group_tile_shape(const GroupKernel &k, const GroupArgs &g, int *rows, int *columns)
+{
+    *rows = k.kind == GROUP_KERNEL_BIG ? 256 : k.kind == GROUP_KERNEL_FEW ? 16 : 64;
+    *columns = k.kind == GROUP_KERNEL_BIG ? 256 : k.kind == GROUP_KERNEL_FEW ? group_few_columns(g) : k.tiles == TILE_64_128 ? 128 : 64;
+}
+
 // Workgroups of a kernel's launch that take tiles (launch_one, launch_few_one), or tiles of the list that a launch of one to a compute unit walks; tall: rows of
 // tiles by their height.
 template <typename F> static bool tiles_fit(const GroupKernel &k, const GroupArgs &g, long n_pass, const F &tall)
 {
     if (k.kind == GROUP_KERNEL_BIG) return tall(128) * ceil_div(g.N, 256) < 1L << 31;
-    const long wgs = k.kind == GROUP_KERNEL_FEW ? group_few_workgroups(g) : ceil_div(tall(64) * ceil_div(g.N, k.tiles == TILE_64_128 ? 128 : 64), 8) * 8;
+    int rows, columns;
+    group_tile_shape(k, g, &rows, &columns);
+    const long wgs = k.kind == GROUP_KERNEL_FEW ? group_few_workgroups(g) : ceil_div(tall(rows) * ceil_div(g.N, columns), 8) * 8;
     return n_pass + wgs <= MAX_GRID_X;
 }
 

@@ -139,6 +139,8 @@ struct GroupKernel { int kind, tiles; };
 // Asked once to a call, ahead of all that changes anything.
 bool group_plan(int dt, bool transB, bool protect, GroupArgs &g, GroupKernel *k);
 bool group_plan_wgrad(const GroupArgs &g, GroupKernel *k);
+// Rows and columns of C that a workgroup of a product's kernel takes at a time.
+void group_tile_shape(const GroupKernel &k, const GroupArgs &g, int *rows, int *columns);
 // Whether the kernel of few rows has room for what it keeps; its columns to a workgroup; workgroups with tiles.
 bool group_few_fits(int dt, bool protect, const GroupArgs &g);
 int group_few_columns(const GroupArgs &g);
