@@ -508,9 +508,12 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, SRC sou
             for (int r = 0; r < nrow && gc < N; ++r) {
                 acc_t v = from_word<acc_t>(*reinterpret_cast<const uint32_t *>(wbuf + r * SROW + lane * 4));
                 if (has_bias) v = add_t(v, bias_lds[wn * TN + lane]);
-                if constexpr (SCALED)
-                    Traits<OT>::store_c(Cb, (long)(br + r) * g.ldc + gc, scaled(v, srow[wm * TM + mi * 32 + r], scol[wn * TN + lane], sbias[wn * TN + lane]));
-                else T::store_c(Cb, (long)(br + r) * g.ldc + gc, v);
+                if constexpr (SCALED) {
+                    float x = scaled(v, srow[wm * TM + mi * 32 + r], scol[wn * TN + lane], sbias[wn * TN + lane]);
+                    // (the compiler makes product, sum and fp16 value one instruction with one rounding, where the register path has two)
+                    asm("" : "+v"(x));
+                    Traits<OT>::store_c(Cb, (long)(br + r) * g.ldc + gc, x);
+                } else T::store_c(Cb, (long)(br + r) * g.ldc + gc, v);
                 if (PROT) colacc = add_t(colacc, v);
                 if constexpr (STO) {
                     const float sv = stored_value<DT>((float)v);

@@ -237,6 +237,34 @@ def test_scales_left_out_are_ones():
         p.close()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("out", ["bf16", "f16"])
+@pytest.mark.parametrize("ends,N,K", [([0, 7, 30], 70, 96), ([0, 100, 1124, 1124, 2500, 6100], 2043, 384), ([0, 130, 1000], 1030, 136), ([0, 8000], 520, 384)])
+def test_scaled_results_are_rounded_step_by_step(out, ends, N, K):
+    """fp32 behind the row's scale, fp32 behind the column's and the bias together, then C's type, in tiles inside C, at its edges, and where a flip is armed: what
+    a product gives does not depend on which kernel or part of one makes it.  (Sums are below 2^24, so each is its own fp32 value; product and bias in 64 bits, 48 of
+    which the product takes, are rounded to fp32 as one rounding does.)"""
+    p = Group("i8", ends, N, K, M=ends[-1], out=out, bias=True, seed=17)
+    try:
+        group = torch.repeat_interleave(torch.arange(p.groups), torch.tensor(ends).diff())
+        acc = torch.zeros(p.M, N)
+        for g in range(p.groups):
+            acc[ends[g]:ends[g + 1]] = (p.A[ends[g]:ends[g + 1], :K].double() @ p.weights(g)).float()
+        assert acc.abs().max() < 2 ** 24
+        want = ((acc * p.row[:, None]).double() * p.col[group].double() + p.bias.double()).float().to(TORCH[out])
+        for mode in (ab.ABFT_OFF, ab.ABFT_DETECT):
+            p.run(mode)
+            assert torch.equal(p.C.cpu()[:, :N], want), mode
+        # a flip in an element whose neighbours are then made by what serves tiles at an edge
+        g = max(range(p.groups), key=lambda e: ends[e + 1] - ends[e])
+        s = ab.make_shape(1, N, K, batch=p.groups, lda=p.A.shape[-1], ldb=p.B.shape[-1], ldc=p.ldc, strideC=p.M * p.ldc)
+        assert ab.abft_inject(p.ctx, None, p.code, s, g, 0, 1, 30, ab.ABFT_INJECT_ACCUMULATOR) == ab.ABFT_OK
+        p.run()
+        assert (p.C.cpu()[:, :N] != want).nonzero().tolist() == [[ends[g], 1]]
+    finally:
+        p.close()
+
+
 # ------------------------------------------------------------------------------------------ faults
 def flips(p, g, i, j, bit, mode):
     s = ab.make_shape(1 if p.M < p.groups else p.M // p.groups, p.N, p.K, batch=p.groups, lda=p.A.shape[-1], ldb=p.B.shape[-1], ldc=p.ldc,
