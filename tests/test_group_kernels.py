@@ -41,6 +41,15 @@ def test_the_cases_reach_their_kernel(tile, dtypes, ends, N, K, trans_b):
             assert ab.abft_group_tile_shape(ab.DTYPE_CODE[dtype], mode, shape_of(dtype, ends, N, K, trans_b)) == tile, (dtype, mode)
 
 
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("rows,groups,N,K", [(31, 32, 4096, 1024), (15, 16, 4096, 1024), (48, 64, 2048, 768), (40, 48, 1536, 1024)])
+def test_fewer_rows_than_groups_fill_the_chip_too(dtype, rows, groups, N, K):
+    """A group has one row on average, rounded up as tiles are: 32 columns to a workgroup as soon as those are 512, as with a row to each group."""
+    ask = lambda M: ab.abft_group_tile_shape(ab.DTYPE_CODE[dtype], ab.ABFT_DETECT, ab.make_shape(M, N, K, batch=groups))
+    assert ask(rows) == ask(groups) == FEW_WIDE
+    assert ask(max(1, 400 * 32 // N)) in (FEW, SQUARE)
+
+
 def test_tile_shape_refuses_what_the_calls_refuse():
     ask = lambda dtype=ab.ABFT_BF16, mode=ab.ABFT_OFF, **k: ab.abft_group_tile_shape(dtype, mode, ab.make_shape(**{**dict(M=64, N=64, K=64, batch=4), **k}))
     assert ask() == FEW and ask(transB=False) == SQUARE
