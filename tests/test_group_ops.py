@@ -800,6 +800,44 @@ def test_two_graphs_of_a_context_with_offsets_that_change():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("mode", [ab.ABFT_OFF, ab.ABFT_DETECT])
+def test_the_event_of_a_context_is_recorded_behind_the_product(mode):
+    p = Group("bf16", [0, 900, 2500], 520, 384, seed=63)
+    try:
+        begin, event, end = (torch.cuda.Event(enable_timing=True) for _ in range(3))
+        event.record()
+        torch.cuda.synchronize()
+        assert ab.abft_gemm_done_event(p.ctx, event.cuda_event) == ab.ABFT_OK
+        begin.record()
+        p.run(mode)
+        end.record()
+        torch.cuda.synchronize()
+        assert 0 < begin.elapsed_time(event) <= begin.elapsed_time(end)
+        assert ab.abft_gemm_done_event(p.ctx, None) == ab.ABFT_OK
+        p.check()
+    finally:
+        p.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("a,b", [(-128, -128), (-128, 127)])
+@pytest.mark.parametrize("ends,N,K,trans_b", [([0, 1, 5], 200, 131071, True), ([0, 150, 300], 200, 131071, False), ([0, 2000, 2600], 1024, 1024, True), ([0, 16], 200, 2040, True)])
+def test_largest_integers_at_the_greatest_depth(ends, N, K, trans_b, a, b):
+    """Every product the largest in magnitude, up to K 2^14 just below 2^31: C holds the sum, the sums of sums agree in Z/2^32, and a flip of the lowest bit shows."""
+    p = Group("i8", ends, N, K, trans_b, seed=64)
+    try:
+        p.dA.fill_(a)
+        p.dB.fill_(b)
+        for mode in (ab.ABFT_OFF, ab.ABFT_DETECT):
+            p.run(mode)
+            assert bool((p.C[:, :N] == a * b * K).all())
+        p.clean()
+        one_flip(p, stored_bits(p), p.groups - 1, ends[-1] - ends[-2] - 1, N - 1, 0, ab.ABFT_DETECT)
+    finally:
+        p.close()
+
+
+@pytest.mark.gpu
 def test_grouped_and_other_calls_share_a_context():
     """Calls of other kinds between grouped ones: the regions they accumulate into are clean for each."""
     ctx = ab.abft_create(4096, 8192, 8192, 16)
