@@ -36,7 +36,7 @@
  *     item: the library may read (never use) the pad between K and lda.
  *   - The caller owns A, B, C, the flag / count buffers and the stream.  The
  *     context owns its workspace (checksum vectors, tile lists).
- *   - abft_gemm / abft_gemm_scaled / abft_gemm_grouped / abft_gemm_grouped_wgrad / abft_quantize_rows /
+ *   - abft_gemm / abft_gemm_scaled / abft_gemm_grouped / abft_gemm_grouped_wgrad / abft_quantize_rows / the calls from abft_route to abft_encode_mx4 /
  *     abft_verify / abft_correct / abft_correct_checksum / abft_inject /
  *     abft_encode_b / abft_discrepancy only enqueue work on `stream` (a hipStream_t
  *     passed as void*): they allocate nothing, copy nothing to the host and never
@@ -62,7 +62,7 @@ extern "C" {
 
 typedef struct abft_ctx abft_ctx;
 
-typedef enum { ABFT_I8 = 0, ABFT_BF16 = 1, ABFT_F16 = 2 } abft_dtype;
+typedef enum { ABFT_I8 = 0, ABFT_BF16 = 1, ABFT_F16 = 2, ABFT_F32 = 3 /* logits of abft_route alone */ } abft_dtype;
 
 /* mode = one base value, optionally OR-ed with flag bits */
 enum {
@@ -281,6 +281,100 @@ int abft_gemm_grouped(abft_ctx *ctx, const void *A, const void *B, const int32_t
  * elements on): ABFT_ESHAPE. */
 int abft_gemm_grouped_wgrad(abft_ctx *ctx, const void *X, const void *dY, const int32_t *offsets, void *dW,
                             abft_dtype dtype, const abft_shape *s, void *stream);
+
+/* ---- From a router's logits to the rows of its experts, and back ---------------------------------------- */
+
+enum { ABFT_SOFTMAX = 0, ABFT_SIGMOID = 1 };
+
+/* How a router's logits (tokens x experts, rows ld apart) become choices.  score: softmax over all experts or each logit's sigmoid.
+ * Experts are chosen by key = score + bias, the largest first, equal ones by their index; the weights are scores without bias.  A logit of -Inf, or a bias of -Inf or
+ * NaN, masks its expert.  groups > 1: experts/groups neighbouring ones form a group, whose value is the sum of its group_best (1 or 2) largest
+ * keys (of those that are not masked), and only the experts of the top_groups groups of largest value (equal ones by index) are left to choose from.  normalise: weights are divided by their sum
+ * over the token's choices.  scale: a factor of all weights. */
+typedef struct {
+    int64_t tokens, experts, ld;      /* experts <= 1024 */
+    int32_t topk;                     /* choices of a token: <= 64, <= experts, <= those of top_groups groups */
+    int32_t score;                    /* ABFT_SOFTMAX, ABFT_SIGMOID */
+    int32_t normalise;                /* 0, 1 */
+    float scale;                      /* finite */
+    const float *bias;                /* DEVICE [experts], or NULL */
+    int32_t groups, top_groups;       /* groups <= 64, a divisor of experts; 1 and 1: none */
+    int32_t group_best;               /* 1 or 2 */
+    int32_t reserved;                 /* 0 */
+} abft_routing;
+
+/* The choices: expert and weight, DEVICE, [tokens][topk].  logits: ABFT_BF16, ABFT_F16 or ABFT_F32; pointer and rows as the matrices above (16 bytes).
+ * Choices are those of exact arithmetic (two keys that differ by less than 2^-50 of the larger aside); weights are computed in fp32.  Where fewer
+ * than topk experts are left the rest is expert -1, weight 0, so a token whose logits are all -Inf goes to no expert.  A token with a logit that is NaN or +Inf
+ * has no scores: experts 0, 1, .. and weights NaN, so that nothing made of it looks sound.  Needs no context, nor do the
+ * other calls of this section but abft_group_rows; they run on the current device.  Sizes beyond those above, or tokens > 2^24: ABFT_ESHAPE. */
+int abft_route(const void *logits, abft_dtype dtype, const abft_routing *q, int32_t *expert, float *weight, void *stream);
+
+/* Its backward pass: dlogits (type of logits, rows ldd apart) from dweight [tokens][topk], for the choices expert as abft_route wrote them (entries outside
+ * [0, experts), and of masked logits, have no part; of an expert named twice by a token one counts).  Choices are constants, as is the bias.  All of a token's row is
+ * written, zeros included; what lies between experts and ldd stays.  A token with a logit that is NaN or +Inf gets NaN. */
+int abft_route_grad(const void *logits, abft_dtype dtype, const abft_routing *q, const int32_t *expert, const float *dweight, void *dlogits,
+                    int64_t ldd, void *stream);
+
+/* Sorts n entries (a token's choice each: entry t * topk + j) by group, keeping the order of those of a group.  group: [n], entries outside [0, groups)
+ * belong to none.  Writes offsets [groups + 1] as abft_gemm_grouped takes them; order [n]: the entry of each row, -1 behind the last group's; place [n]: the row of each
+ * entry, -1 of none.  All DEVICE, int32.  n <= max_rows of the context, groups <= max_batch, <= 1024.  Leaves what the context knows of products alone. */
+int abft_group_rows(abft_ctx *ctx, const int32_t *group, int64_t n, int64_t groups, int32_t *offsets, int32_t *order, int32_t *place, void *stream);
+
+/* Y[r] = X[order[r] / topk] for each row r < rows: the tokens' rows for their experts, of ABFT_I8, ABFT_BF16 or ABFT_F16.  Rows whose order is not in
+ * [0, tokens * topk) stay as they are, as does what lies between cols and ldy.  X and Y must not overlap.  Its backward pass is abft_combine_rows without
+ * weights. */
+int abft_gather_rows(const void *X, abft_dtype dtype, int64_t tokens, int64_t cols, int64_t ldx, const int32_t *order, int64_t rows, int32_t topk,
+                     void *Y, int64_t ldy, void *stream);
+
+/* out[t] = base[t] + the sum over j of weight[t][j] Y[place[t][j]], in fp32, j rising, rounded once; places outside [0, rows) have no part, whatever
+ * their weight.  base: NULL, or added first (may be out itself); weight: NULL, or [tokens][topk]: ones.  ABFT_BF16 or ABFT_F16.  What lies
+ * between cols and ldo stays.  tokens * topk <= 2^30. */
+int abft_combine_rows(const void *Y, abft_dtype dtype, int64_t rows, int64_t cols, int64_t ldy, const int32_t *place, const float *weight,
+                      int64_t tokens, int32_t topk, const void *base, int64_t ldb, void *out, int64_t ldo, void *stream);
+
+/* Its backward pass: dY[place[t][j]] = weight[t][j] dout[t], rounded once, and dweight[t][j] = the dot of dout[t] and Y[place[t][j]], in fp32, 0 where the place is
+ * outside [0, rows).  Rows of dY that no place names stay as they are; a row named twice holds one of the two.  dY or dweight (then Y too) may be NULL.  (base's
+ * gradient is dout.) */
+int abft_combine_rows_grad(const void *dout, abft_dtype dtype, int64_t tokens, int64_t cols, int64_t ldd, const int32_t *place, const float *weight,
+                           int32_t topk, const void *Y, int64_t rows, int64_t ldy, void *dY, int64_t lddy, float *dweight, void *stream);
+
+/* ---- 4-bit floating point in blocks with a power of two each -------------------------------------------- */
+
+/* Rows of 4-bit elements (sign, 2 bits of exponent, 1 of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6), two to a byte, the first in the low half, in blocks of 32 along the row.
+ * A block's elements are multiplied by 2^(scale - 127), scale a byte; 255: all NaN.  A last block of fewer elements is filled up with zeros, and products
+ * count on it.  Leading dimensions of the elements count elements (multiples of 32), those of the scales bytes (multiples of 16); pointers are multiples of 16 bytes.  (The
+ * library may read the pad behind a row's last block, and never uses it.)
+ *
+ * abft_quantize_mx4: row r of Q is row order[r] / topk of X (order NULL: row r, and rows = tokens), X: tokens x cols of ABFT_BF16 or ABFT_F16.  Rows whose order is not in
+ * [0, tokens * topk) stay as they are.  scale - 127 = floor(log2 max|x|) - 2, at least -127; x / 2^(scale - 127) is rounded to the nearest element, ties
+ * to the even code, magnitudes above 6 to 6, as exact arithmetic gives it.  A block of zeros: scale 0; with an Inf or a NaN: scale 255.
+ * abft_dequantize_mx4: the values, rounded once to dtype (they are exact but where that type's range ends). */
+int abft_quantize_mx4(const void *X, abft_dtype dtype, int64_t tokens, int64_t cols, int64_t ldx, const int32_t *order, int64_t rows, int32_t topk,
+                      void *Q, int64_t ldq, uint8_t *scale, int64_t lds, void *stream);
+int abft_dequantize_mx4(const void *Q, int64_t ldq, const uint8_t *scale, int64_t lds, int64_t rows, int64_t cols, void *X, abft_dtype dtype,
+                        int64_t ldx, void *stream);
+
+/* What a product of such rows takes besides the elements, all DEVICE. */
+typedef struct {
+    const uint8_t *a;                 /* scales of the rows of A, [M], lda bytes apart */
+    const uint8_t *b;                 /* of B, [batch][N], ldb bytes apart, groups strideB bytes apart (ignored if batch == 1) */
+    int64_t lda, ldb, strideB;
+    const float *bias;                /* [N], shared by all groups, or NULL */
+    int32_t out;                      /* type of C: ABFT_BF16 or ABFT_F16 */
+    int32_t reserved;                 /* 0 */
+} abft_mx4;
+
+/* C = A B + bias for such A (M x K) and B (N x K, transB = 1), sums in fp32, the bias added in fp32, rounded once.  lda, ldb and strideB of the shape count elements.  offsets: the
+ * rows of A and C sorted by group, exactly as in abft_gemm_grouped, or NULL with batch = 1.  mode: ABFT_OFF or ABFT_DETECT, which may be OR-ed with
+ * ABFT_B_CHECKSUM_CACHED (behind abft_encode_mx4 or an earlier protected call, with the same B and shape).  What is checked are the sums ahead of the bias, group by group,
+ * as in abft_gemm_grouped for floating point: tolerance 1e-3 K max|A| max|B| of the values (scales included), or abft_result's.  What may follow the
+ * call, the context's limits and those of the shape (K <= 2^29) are also as there; an accumulator flip is armed with the same shape as ABFT_BF16.
+ * Gradients: of A by abft_gemm_grouped on the dequantised B, of B by abft_gemm_grouped_wgrad. */
+int abft_gemm_mx4(abft_ctx *ctx, const void *A, const void *B, const int32_t *offsets, const abft_mx4 *q, void *C, int mode, const abft_shape *s,
+                  const abft_result *r, void *stream);
+/* abft_encode_b for such B (q: b, ldb and strideB are looked at, and out). */
+int abft_encode_mx4(abft_ctx *ctx, const void *B, const abft_mx4 *q, const abft_shape *s, void *stream);
 
 /* Producer-side input checksum for the next abft_gemm / abft_gemm_bias on this context called with
  * ABFT_A_CHECKSUM_GIVEN (Sec. V "Optimizations" (2): the checksum is generated while the tensor is

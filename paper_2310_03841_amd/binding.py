@@ -21,14 +21,17 @@ __all__ = [
     "ABFT_WS_A_SUM", "ABFT_WS_B_SUM", "ABFT_WS_CC_PRED", "ABFT_WS_RC_PRED", "ABFT_WS_CC_OBS",
     "ABFT_WS_RC_OBS", "ABFT_WS_CC_VOBS", "ABFT_WS_RC_VOBS", "ABFT_WS_TAU", "ABFT_WS_S_PRED", "ABFT_WS_MAXABS", "ABFT_WS_CC_STO", "ABFT_WS_RC_STO",
     "abft_shape", "abft_config", "abft_result", "abft_scales", "make_scales",
-    "abft_gemm_scaled", "abft_gemm_grouped", "abft_gemm_grouped_wgrad", "abft_quantize_rows", "AbftError", "lib", "lib_path", "exported_symbols",
+    "abft_gemm_scaled", "abft_gemm_grouped", "abft_gemm_grouped_wgrad", "abft_quantize_rows", "ABFT_F32", "ABFT_SOFTMAX", "ABFT_SIGMOID", "abft_routing", "make_routing", "abft_mx4", "make_mx4",
+    "abft_route", "abft_route_grad", "abft_group_rows", "abft_gather_rows", "abft_combine_rows", "abft_combine_rows_grad", "abft_quantize_mx4",
+    "abft_dequantize_mx4", "abft_gemm_mx4", "abft_encode_mx4", "AbftError", "lib", "lib_path", "exported_symbols",
     "abft_create", "abft_destroy", "abft_encode_b", "abft_gemm", "abft_gemm_bias", "abft_gemm_static", "abft_verify", "abft_correct",
     "abft_correct_checksum", "abft_inject", "abft_discrepancy", "abft_workspace", "abft_tile_shape", "abft_group_tile_shape", "abft_strerror", "abft_last_hip_error",
     "abft_version", "abft_mfma_peak", "abft_profile_begin", "abft_profile_end", "make_shape", "make_result", "DTYPE_CODE",
 ]
 
-ABFT_I8, ABFT_BF16, ABFT_F16 = 0, 1, 2
-DTYPE_CODE = {"i8": ABFT_I8, "bf16": ABFT_BF16, "f16": ABFT_F16}
+ABFT_I8, ABFT_BF16, ABFT_F16, ABFT_F32 = 0, 1, 2, 3
+ABFT_SOFTMAX, ABFT_SIGMOID = 0, 1
+DTYPE_CODE = {"i8": ABFT_I8, "bf16": ABFT_BF16, "f16": ABFT_F16, "f32": ABFT_F32}
 ABFT_OFF, ABFT_DETECT, ABFT_DETECT_CORRECT = 0, 1, 2
 ABFT_B_CHECKSUM_CACHED = 0x10
 ABFT_STORED_SUMS = 0x20
@@ -66,6 +69,18 @@ class abft_scales(ctypes.Structure):
                 ("out", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class abft_routing(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("experts", ctypes.c_int64), ("ld", ctypes.c_int64),
+                ("topk", ctypes.c_int32), ("score", ctypes.c_int32), ("normalise", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("bias", ctypes.c_void_p), ("groups", ctypes.c_int32), ("top_groups", ctypes.c_int32),
+                ("group_best", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class abft_mx4(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("lda", ctypes.c_int64), ("ldb", ctypes.c_int64),
+                ("strideB", ctypes.c_int64), ("bias", ctypes.c_void_p), ("out", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 class AbftError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -97,6 +112,30 @@ _SIGS = {
                                                ctypes.c_void_p]),
     "abft_quantize_rows": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64,
                                           ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p]),
+    "abft_route": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.POINTER(abft_routing), ctypes.c_void_p, ctypes.c_void_p,
+                                  ctypes.c_void_p]),
+    "abft_route_grad": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.POINTER(abft_routing), ctypes.c_void_p, ctypes.c_void_p,
+                                       ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
+    "abft_group_rows": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p,
+                                       ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
+    "abft_gather_rows": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p,
+                                        ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
+    "abft_combine_rows": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p,
+                                         ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64,
+                                         ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
+    "abft_combine_rows_grad": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64,
+                                              ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64,
+                                              ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p]),
+    "abft_quantize_mx4": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p,
+                                         ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                         ctypes.c_int64, ctypes.c_void_p]),
+    "abft_dequantize_mx4": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64,
+                                           ctypes.c_int64, ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_void_p]),
+    "abft_gemm_mx4": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(abft_mx4),
+                                     ctypes.c_void_p, ctypes.c_int, ctypes.POINTER(abft_shape), ctypes.POINTER(abft_result),
+                                     ctypes.c_void_p]),
+    "abft_encode_mx4": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(abft_mx4), ctypes.POINTER(abft_shape),
+                                       ctypes.c_void_p]),
     "abft_supply_a": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
     "abft_gemm_done_event": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
     "abft_verify": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.POINTER(abft_shape),
@@ -216,6 +255,16 @@ def make_scales(row=None, col=None, bias=None, out: int = ABFT_BF16) -> abft_sca
     return abft_scales(_ptr(row), _ptr(col), _ptr(bias), int(out), 0)
 
 
+def make_routing(tokens, experts, topk, ld=None, score=ABFT_SOFTMAX, normalise=True, scale=1.0, bias=None, groups=1, top_groups=1,
+                 group_best=1) -> abft_routing:
+    return abft_routing(tokens, experts, experts if ld is None else ld, topk, score, 1 if normalise else 0, float(scale), _ptr(bias),
+                        groups, top_groups, group_best, 0)
+
+
+def make_mx4(a, lda, b, ldb, strideB=0, bias=None, out: int = ABFT_BF16) -> abft_mx4:
+    return abft_mx4(_ptr(a), _ptr(b), lda, ldb, strideB, _ptr(bias), int(out), 0)
+
+
 def abft_strerror(code: int) -> str:
     return lib().abft_strerror(int(code)).decode()
 
@@ -288,6 +337,56 @@ def abft_gemm_grouped_wgrad(ctx, X, dY, offsets, dW, dtype: int, shape: abft_sha
 
 def abft_quantize_rows(X, dtype: int, rows: int, cols: int, ldx: int, Q, ldq: int, scale, stream=None) -> int:
     return int(lib().abft_quantize_rows(_ptr(X), dtype, rows, cols, ldx, _ptr(Q), ldq, _ptr(scale), _stream(stream)))
+
+
+def abft_route(logits, dtype: int, routing: abft_routing, expert, weight, stream=None) -> int:
+    return int(lib().abft_route(_ptr(logits), dtype, ctypes.byref(routing), _ptr(expert), _ptr(weight), _stream(stream)))
+
+
+def abft_route_grad(logits, dtype: int, routing: abft_routing, expert, dweight, dlogits, ldd: int, stream=None) -> int:
+    return int(lib().abft_route_grad(_ptr(logits), dtype, ctypes.byref(routing), _ptr(expert), _ptr(dweight), _ptr(dlogits), ldd,
+                                     _stream(stream)))
+
+
+def abft_group_rows(ctx, group, n: int, groups: int, offsets, order, place, stream=None) -> int:
+    return int(lib().abft_group_rows(ctx, _ptr(group), n, groups, _ptr(offsets), _ptr(order), _ptr(place), _stream(stream)))
+
+
+def abft_gather_rows(X, dtype: int, tokens: int, cols: int, ldx: int, order, rows: int, topk: int, Y, ldy: int, stream=None) -> int:
+    return int(lib().abft_gather_rows(_ptr(X), dtype, tokens, cols, ldx, _ptr(order), rows, topk, _ptr(Y), ldy, _stream(stream)))
+
+
+def abft_combine_rows(Y, dtype: int, rows: int, cols: int, ldy: int, place, weight, tokens: int, topk: int, base, ldb: int, out, ldo: int,
+                      stream=None) -> int:
+    return int(lib().abft_combine_rows(_ptr(Y), dtype, rows, cols, ldy, _ptr(place), _ptr(weight), tokens, topk, _ptr(base), ldb, _ptr(out),
+                                       ldo, _stream(stream)))
+
+
+def abft_combine_rows_grad(dout, dtype: int, tokens: int, cols: int, ldd: int, place, weight, topk: int, Y, rows: int, ldy: int, dY,
+                           lddy: int, dweight, stream=None) -> int:
+    return int(lib().abft_combine_rows_grad(_ptr(dout), dtype, tokens, cols, ldd, _ptr(place), _ptr(weight), topk, _ptr(Y), rows, ldy,
+                                            _ptr(dY), lddy, _ptr(dweight), _stream(stream)))
+
+
+def abft_quantize_mx4(X, dtype: int, tokens: int, cols: int, ldx: int, order, rows: int, topk: int, Q, ldq: int, scale, lds: int,
+                      stream=None) -> int:
+    return int(lib().abft_quantize_mx4(_ptr(X), dtype, tokens, cols, ldx, _ptr(order), rows, topk, _ptr(Q), ldq, _ptr(scale), lds,
+                                       _stream(stream)))
+
+
+def abft_dequantize_mx4(Q, ldq: int, scale, lds: int, rows: int, cols: int, X, dtype: int, ldx: int, stream=None) -> int:
+    return int(lib().abft_dequantize_mx4(_ptr(Q), ldq, _ptr(scale), lds, rows, cols, _ptr(X), dtype, ldx, _stream(stream)))
+
+
+def abft_gemm_mx4(ctx, A, B, offsets, mx4: abft_mx4, C, mode: int, shape: abft_shape, result: abft_result | None = None,
+                  stream=None) -> int:
+    r = ctypes.byref(result) if result is not None else None
+    q = ctypes.byref(mx4) if mx4 is not None else None
+    return int(lib().abft_gemm_mx4(ctx, _ptr(A), _ptr(B), _ptr(offsets), q, _ptr(C), mode, ctypes.byref(shape), r, _stream(stream)))
+
+
+def abft_encode_mx4(ctx, B, mx4: abft_mx4, shape: abft_shape, stream=None) -> int:
+    return int(lib().abft_encode_mx4(ctx, _ptr(B), ctypes.byref(mx4), ctypes.byref(shape), _stream(stream)))
 
 
 def abft_gemm_done_event(ctx, event) -> int:

@@ -8,7 +8,9 @@
 
 #include "../../include/abft.h"
 #include "abft_internal.h"
+#include "gemm_mx4.h"
 #include "group_args.h"
+#include "route_args.h"
 
 using namespace abft;
 
@@ -32,6 +34,7 @@ struct abft_ctx {
     size_t vdirty[2];
     int32_t  *fix_tiles;
     uint32_t *small;        // fix_count[4], cmp_ticket[4], group tickets of the item kernel [64], bias sum
+    uint32_t *pool_rows;    // counts of abft_group_rows (null: entries of one workgroup; none in a static context)
     uint32_t *pool_given;   // copy of a supplied e^T A, then of max|A| per batch item: see own_given
     InjectArm arm;
     int last_hip;
@@ -156,6 +159,13 @@ extern "C" int abft_create(abft_ctx **out, const abft_config *cfg)
             return r;
         }
     }
+    // (written before it is read by every call that uses it)
+    const size_t rows_words = group_rows_words(c->cfg.max_rows, (int)(c->cfg.max_batch < GROUP_ROWS_MAX ? c->cfg.max_batch : GROUP_ROWS_MAX));
+    if (rows_words && (e = hipMalloc((void **)&c->pool_rows, rows_words * 4)) != hipSuccess) {
+        int r = fail_hip(c, e);
+        abft_destroy(c);
+        return r;
+    }
     e = hipDeviceSynchronize();
     if (e != hipSuccess) { int r = fail_hip(c, e); abft_destroy(c); return r; }
     start_clean(c);
@@ -173,6 +183,7 @@ extern "C" int abft_destroy(abft_ctx *c)
     pool_slots(c, slot);
     for (void **p : slot)
         if (*p) (void)hipFree(*p);
+    if (c->pool_rows) (void)hipFree(c->pool_rows);
     delete c;
     return ABFT_OK;
 }
@@ -710,8 +721,10 @@ static GroupArgs group_args(const void *A, const void *B, void *C, const int32_t
 
 // The kernels of a protected call: the pass over the matrices (unless their encoding is cached), the product, whose launch also passes
 // over A, and the check.  The regions it accumulates into alternate as those of enqueue_tiled.
-static int enqueue_group(abft_ctx *ctx, int dtype, int ot, bool cached, const GroupKernel &k, GroupArgs &g, const void *B, const Shape &sh,
-                         const Verdict &v, hipStream_t st)
+// encode(workspace, zero, words): the first, which clears those words besides; product(workspace); check(workspace, what to clear for calls to come).
+template <typename ENCODE, typename PRODUCT, typename CHECK>
+static int enqueue_group(abft_ctx *ctx, int dtype, bool cached, GroupArgs &g, const Shape &sh, const Verdict &v, hipStream_t st, const ENCODE &encode,
+                         const PRODUCT &product, const CHECK &check)
 {
     const bool gm = in_graph_mode(ctx, st);
     const int prev = ctx->cur;
@@ -741,12 +754,12 @@ static int enqueue_group(abft_ctx *ctx, int dtype, int ot, bool cached, const Gr
             end.zero2_words = ctx->bslot_words;
         }
     }
-    if (!cached) HIP_TRY(launch_encode_b(dtype, B, sh, w, w.cc_obs, stale, st));
+    if (!cached) HIP_TRY(encode(w, w.cc_obs, stale));
     else if (stale) HIP_TRY(launch_zero(w.cc_obs, stale, st));
     ctx->sto_valid = false;
-    HIP_TRY(launch_group(dtype, ot, true, sh.transB != 0, k, g, w.b_max, &v, st));
+    HIP_TRY(product(w));
     if (ctx->done_event && !gm) HIP_TRY(hipEventRecord(ctx->done_event, st));
-    HIP_TRY(launch_group_check(dtype, k, g, sh.transB != 0, w, v, end, st));
+    HIP_TRY(check(w, end));
     if (!gm) {
         ctx->bclean[ctx->bslot ^ 1] = true;
         ctx->dirty[prev] = 0;
@@ -800,7 +813,10 @@ static int group_impl(abft_ctx *ctx, const void *A, const void *B, const int32_t
     ctx->vobs_valid = false;
     if (!cached) ctx->b_valid = false;
     ctx->arm.batch = -1;
-    rc = enqueue_group(ctx, dtype, ot, cached, k, g, B, sh, v, st);
+    rc = enqueue_group(ctx, dtype, cached, g, sh, v, st,
+                       [&](const Workspace &w, uint32_t *zero, size_t words) { return launch_encode_b(dtype, B, sh, w, zero, words, st); },
+                       [&](const Workspace &w) { return launch_group(dtype, ot, true, sh.transB != 0, k, g, w.b_max, &v, st); },
+                       [&](const Workspace &w, const OneLaunch &end) { return launch_group_check(dtype, k, g, sh.transB != 0, w, v, end, st); });
     if (rc) return rc;
     ctx->b_valid = true;
     ctx->b_dt = dtype;
@@ -870,6 +886,267 @@ extern "C" int abft_quantize_rows(const void *X, abft_dtype dtype, int64_t rows,
     if (!X || !Q || !scale) return ABFT_EINVAL;
     if (!aligned16(X) || !aligned16(Q) || (ldx * 2) % 16 || ldq % 16 || ((uintptr_t)scale & 3u)) return ABFT_EALIGN;
     return launch_quantize_rows(dtype, X, (int)rows, (int)cols, ldx, Q, ldq, scale, (hipStream_t)stream) == hipSuccess ? ABFT_OK : ABFT_EHIP;
+}
+
+// ------------------------------------------------------------------------------------------
+// 4-bit operands.
+
+// A shape of 4-bit operands, and the scales that go with it; sh: K of whole blocks.  a: A is there too; c: the context, or null.
+static int check_mx4(const abft_ctx *c, const abft_mx4 *q, const abft_shape *s, bool a, Shape *sh)
+{
+    if (!q || !s || q->reserved || (q->out != ABFT_BF16 && q->out != ABFT_F16) || s->transB != 1) return ABFT_EINVAL;
+    if (s->M < 1 || s->N < 1 || s->K < 1 || s->batch < 1) return ABFT_ESHAPE;
+    if (s->M > (1 << 30) || s->N > (1 << 29) || s->K > (1 << 29) || s->batch > 65535 || s->batch * s->N > (1 << 27)) return ABFT_ESHAPE;
+    const int64_t K = round_up(s->K, 32);
+    if ((a && (s->lda < K || s->ldc < s->N || q->lda < K / 32)) || s->ldb < K || q->ldb < K / 32) return ABFT_ESHAPE;
+    if ((a && (s->lda % 32 || (s->ldc * 2) % 16 || q->lda % 16)) || s->ldb % 32 || q->ldb % 16) return ABFT_EALIGN;
+    if (s->batch > 1 && (s->strideB < 0 || s->strideB % 32 || q->strideB < 0 || q->strideB % 16)) return ABFT_EALIGN;
+    if (c && ((a && s->M > c->cfg.max_rows) || s->batch * s->N > c->cfg.max_cols || s->batch * round_up(K, 128) > c->cfg.max_depth || s->batch > c->cfg.max_batch))
+        return ABFT_EWORKSPACE;
+    if ((a && !q->a) || !q->b) return ABFT_EINVAL;
+    if ((a && !aligned16(q->a)) || !aligned16(q->b) || ((uintptr_t)q->bias & 3u)) return ABFT_EALIGN;
+    sh->M = (int)s->M; sh->N = (int)s->N; sh->K = (int)K; sh->batch = (int)s->batch; sh->transB = 1;
+    sh->lda = s->lda / 2; sh->ldb = s->ldb / 2; sh->ldc = s->ldc;
+    sh->sA = sh->sC = 0;
+    sh->sB = s->batch > 1 ? s->strideB / 2 : 0;
+    sh->Kp = (int)round_up(K, 128);
+    return ABFT_OK;
+}
+
+static Mx4Args mx4_args(const void *A, const void *B, void *C, const int32_t *offsets, const abft_mx4 *q, const Shape &sh)
+{
+    Mx4Args g;
+    memset(&g, 0, sizeof(g));
+    static_cast<GroupArgs &>(g) = group_args(A, B, C, offsets, sh);
+    g.K = sh.K / 2;                                      // bytes
+    g.sa = q->a; g.sb = q->b;
+    g.ld_sa = q->lda; g.ld_sb = q->ldb; g.stride_sb = sh.batch > 1 ? q->strideB : 0;
+    g.bias = q->bias;
+    return g;
+}
+
+extern "C" int abft_encode_mx4(abft_ctx *ctx, const void *B, const abft_mx4 *q, const abft_shape *s, void *stream)
+{
+    Shape sh;
+    int rc = check_mx4(ctx, q, s, false, &sh);
+    if (rc) return rc;
+    if (!ctx || !B) return ABFT_EINVAL;
+    if (!aligned16(B)) return ABFT_EALIGN;
+    ctx->b_valid = false;
+    rc = begin_b_pass(ctx, (hipStream_t)stream);
+    if (rc) return rc;
+    Workspace w;
+    carve_rows(ctx, DT_BF16, sh, 0, &w);                 // (of which b and max|B| are used)
+    HIP_TRY(launch_mx4_encode(mx4_args(nullptr, B, nullptr, nullptr, q, sh), w, nullptr, 0, (hipStream_t)stream));
+    ctx->b_valid = true;
+    ctx->b_dt = DT_MX4;
+    ctx->b_shape = *s;
+    return ABFT_OK;
+}
+
+extern "C" int abft_gemm_mx4(abft_ctx *ctx, const void *A, const void *B, const int32_t *offsets, const abft_mx4 *q, void *C, int mode, const abft_shape *s,
+                             const abft_result *r, void *stream)
+{
+    hipStream_t st = (hipStream_t)stream;
+    const int base = mode & ABFT_MODE_MASK;
+    if (base != ABFT_OFF && base != ABFT_DETECT) return ABFT_EINVAL;
+    if (mode & ~(ABFT_MODE_MASK | ABFT_B_CHECKSUM_CACHED)) return ABFT_EINVAL;
+    Shape sh;
+    int rc = check_mx4(ctx, q, s, true, &sh);
+    if (rc) return rc;
+    if (!ctx || !A || !B || !C || (!offsets && sh.batch != 1)) return ABFT_EINVAL;
+    if (!aligned16(A) || !aligned16(B) || !aligned16(C) || ((uintptr_t)offsets & 3u)) return ABFT_EALIGN;
+    const InjectArm arm = ctx->arm;
+    if (arm.batch >= 0 && (arm.batch >= sh.batch || arm.row >= sh.M || arm.col >= sh.N)) return ABFT_EINVAL;
+    Mx4Args g = mx4_args(A, B, C, offsets, q, sh);
+    g.inj_b = arm.batch; g.inj_row = arm.row; g.inj_col = arm.col; g.inj_bit = arm.bit;
+    GroupKernel k;
+    if (!mx4_plan(base != ABFT_OFF, g, &k)) return ABFT_ESHAPE;
+    const float tau_k = 1e-3f * (float)s->K;
+    if (base == ABFT_OFF) {
+        ctx->pred_valid = false;
+        ctx->vobs_valid = false;
+        ctx->arm.batch = -1;
+        HIP_TRY(k.kind == GROUP_KERNEL_FEW ? launch_mx4_few(q->out, false, g, nullptr, tau_k, 0.f, st) : launch_mx4_rows(q->out, k.tiles, false, g, st));
+        if (ctx->done_event && !capturing(st)) HIP_TRY(hipEventRecord(ctx->done_event, st));
+        return ABFT_OK;
+    }
+    Verdict v;
+    rc = check_verdict(r, &v);
+    if (rc) return rc;
+    const bool cached = (mode & ABFT_B_CHECKSUM_CACHED) != 0;
+    if (cached && !(ctx->b_valid && ctx->b_dt == DT_MX4 && same_b(ctx->b_shape, *s))) return ABFT_ESTATE;
+    ctx->pred_valid = false;
+    ctx->vobs_valid = false;
+    if (!cached) ctx->b_valid = false;
+    ctx->arm.batch = -1;
+    const float tau_cols = v.tau_override_cols > 0.f ? v.tau_override_cols : v.tau_override;
+    rc = enqueue_group(ctx, DT_BF16, cached, g, sh, v, st,
+                       [&](const Workspace &w, uint32_t *zero, size_t words) { return launch_mx4_encode(g, w, zero, words, st); },
+                       [&](const Workspace &w) {
+                           return k.kind == GROUP_KERNEL_FEW ? launch_mx4_few(q->out, true, g, w.b_max, tau_k, tau_cols, st) : launch_mx4_rows(q->out, k.tiles, true, g, st);
+                       },
+                       [&](const Workspace &w, const OneLaunch &end) { return launch_mx4_check(k, g, (int)s->K, w, v, end, st); });
+    if (rc) return rc;
+    ctx->b_valid = true;
+    ctx->b_dt = DT_MX4;
+    ctx->b_shape = *s;
+    return ABFT_OK;
+}
+
+// What the rows of a dispatch ask of their sizes; es: bytes of an element.
+static int check_rows(int64_t rows, int64_t cols, int64_t ld, int es)
+{
+    if (rows < 1 || cols < 1 || rows > (1 << 30) || cols > (1 << 28) || ld < cols) return ABFT_ESHAPE;
+    return (ld * es) % 16 ? ABFT_EALIGN : ABFT_OK;
+}
+static bool is_half(int dtype) { return dtype == ABFT_BF16 || dtype == ABFT_F16; }
+static int from_hip(hipError_t e) { return e == hipSuccess ? ABFT_OK : ABFT_EHIP; }
+
+extern "C" int abft_quantize_mx4(const void *X, abft_dtype dtype, int64_t tokens, int64_t cols, int64_t ldx, const int32_t *order, int64_t rows, int32_t topk,
+                                 void *Q, int64_t ldq, uint8_t *scale, int64_t lds, void *stream)
+{
+    if (!is_half(dtype) || topk < 1) return ABFT_EINVAL;
+    int rc = check_rows(tokens, cols, ldx, 2);
+    if (rc == ABFT_ESHAPE) return rc;
+    if (rows < 1 || rows > (1 << 30) || (!order && rows != tokens) || ldq < round_up(cols, 32) || lds < (cols + 31) / 32) return ABFT_ESHAPE;
+    if (!X || !Q || !scale) return ABFT_EINVAL;
+    if (rc || !aligned16(X) || !aligned16(Q) || !aligned16(scale) || ldq % 32 || lds % 16 || ((uintptr_t)order & 3u)) return ABFT_EALIGN;
+    return from_hip(launch_quantize_mx4(dtype, X, (int)tokens, (int)cols, ldx * 2, order, (int)rows, topk, Q, ldq / 2, scale, lds, (hipStream_t)stream));
+}
+
+extern "C" int abft_dequantize_mx4(const void *Q, int64_t ldq, const uint8_t *scale, int64_t lds, int64_t rows, int64_t cols, void *X, abft_dtype dtype,
+                                   int64_t ldx, void *stream)
+{
+    if (!is_half(dtype)) return ABFT_EINVAL;
+    int rc = check_rows(rows, cols, ldx, 2);
+    if (rc == ABFT_ESHAPE || ldq < round_up(cols, 32) || lds < (cols + 31) / 32) return ABFT_ESHAPE;
+    if (!X || !Q || !scale) return ABFT_EINVAL;
+    if (rc || !aligned16(X) || !aligned16(Q) || !aligned16(scale) || ldq % 32 || lds % 16) return ABFT_EALIGN;
+    return from_hip(launch_dequantize_mx4(dtype, Q, ldq / 2, scale, lds, (int)rows, (int)cols, X, ldx * 2, (hipStream_t)stream));
+}
+
+// ------------------------------------------------------------------------------------------
+// From a router's logits to the rows of its experts, and back.
+
+static int route_args(const void *logits, int dtype, const abft_routing *q, RouteArgs *a)
+{
+    if ((dtype != ABFT_BF16 && dtype != ABFT_F16 && dtype != ABFT_F32) || !q) return ABFT_EINVAL;
+    if ((q->score != ABFT_SOFTMAX && q->score != ABFT_SIGMOID) || (q->normalise != 0 && q->normalise != 1) || q->reserved) return ABFT_EINVAL;
+    if (q->group_best != 1 && q->group_best != 2) return ABFT_EINVAL;
+    if (!(q->scale > -__builtin_inff() && q->scale < __builtin_inff())) return ABFT_EINVAL;
+    if (q->tokens < 1 || q->experts < 1 || q->tokens > (1 << 24) || q->experts > ROUTE_MAX_EXPERTS || q->ld < q->experts || q->ld > (1 << 28)) return ABFT_ESHAPE;
+    if (q->topk < 1 || q->topk > ROUTE_MAX_TOPK || q->topk > q->experts) return ABFT_ESHAPE;
+    if (q->groups < 1 || q->groups > ROUTE_MAX_GROUPS || q->experts % q->groups || q->top_groups < 1 || q->top_groups > q->groups ||
+        q->topk > q->top_groups * (q->experts / q->groups))
+        return ABFT_ESHAPE;
+    if (!logits) return ABFT_EINVAL;
+    const int es = dtype == ABFT_F32 ? 4 : 2;
+    if (!aligned16(logits) || (q->ld * es) % 16 || ((uintptr_t)q->bias & 3u)) return ABFT_EALIGN;
+    memset(a, 0, sizeof(*a));
+    a->logits = (const uint8_t *)logits;
+    a->ld = q->ld * es;
+    a->tokens = (int)q->tokens; a->experts = (int)q->experts; a->topk = q->topk;
+    a->sigmoid = q->score == ABFT_SIGMOID; a->normalise = q->normalise;
+    // all groups: every expert stays
+    a->groups = q->top_groups < q->groups ? q->groups : 1; a->top_groups = q->top_groups; a->group_best = q->group_best;
+    a->by_logit = !q->bias && (a->groups == 1 || q->group_best == 1);
+    a->scale = q->scale;
+    a->bias = q->bias;
+    return ABFT_OK;
+}
+
+extern "C" int abft_route(const void *logits, abft_dtype dtype, const abft_routing *q, int32_t *expert, float *weight, void *stream)
+{
+    RouteArgs a;
+    const int rc = route_args(logits, dtype, q, &a);
+    if (rc) return rc;
+    if (!expert || !weight) return ABFT_EINVAL;
+    if (((uintptr_t)expert & 3u) || ((uintptr_t)weight & 3u)) return ABFT_EALIGN;
+    a.expert = expert; a.weight = weight;
+    return from_hip(launch_route(dtype, false, a, (hipStream_t)stream));
+}
+
+extern "C" int abft_route_grad(const void *logits, abft_dtype dtype, const abft_routing *q, const int32_t *expert, const float *dweight, void *dlogits,
+                               int64_t ldd, void *stream)
+{
+    RouteArgs a;
+    const int rc = route_args(logits, dtype, q, &a);
+    if (rc) return rc;
+    if (ldd < q->experts) return ABFT_ESHAPE;
+    if (!expert || !dweight || !dlogits) return ABFT_EINVAL;
+    const int es = dtype == ABFT_F32 ? 4 : 2;
+    if (((uintptr_t)expert & 3u) || ((uintptr_t)dweight & 3u) || !aligned16(dlogits) || (ldd * es) % 16) return ABFT_EALIGN;
+    a.expert = const_cast<int32_t *>(expert); a.dweight = dweight;
+    a.dlogits = (uint8_t *)dlogits; a.ldd = ldd * es;
+    return from_hip(launch_route(dtype, true, a, (hipStream_t)stream));
+}
+
+extern "C" int abft_group_rows(abft_ctx *ctx, const int32_t *group, int64_t n, int64_t groups, int32_t *offsets, int32_t *order, int32_t *place, void *stream)
+{
+    if (n < 1 || groups < 1 || n > (1 << 30) || groups > GROUP_ROWS_MAX) return ABFT_ESHAPE;
+    if (!ctx) return ABFT_EINVAL;
+    if (n > ctx->cfg.max_rows || groups > ctx->cfg.max_batch) return ABFT_EWORKSPACE;
+    if (!group || !offsets || !order || !place) return ABFT_EINVAL;
+    if (((uintptr_t)group | (uintptr_t)offsets | (uintptr_t)order | (uintptr_t)place) & 3u) return ABFT_EALIGN;
+    HIP_TRY(launch_group_rows(group, (int)n, (int)groups, offsets, order, place, ctx->pool_rows, (hipStream_t)stream));
+    return ABFT_OK;
+}
+
+extern "C" int abft_gather_rows(const void *X, abft_dtype dtype, int64_t tokens, int64_t cols, int64_t ldx, const int32_t *order, int64_t rows, int32_t topk,
+                                void *Y, int64_t ldy, void *stream)
+{
+    if ((dtype != ABFT_I8 && !is_half(dtype)) || topk < 1) return ABFT_EINVAL;
+    const int es = elem_size(dtype), rx = check_rows(tokens, cols, ldx, es), ry = check_rows(rows, cols, ldy, es);
+    if (rx == ABFT_ESHAPE || ry == ABFT_ESHAPE) return ABFT_ESHAPE;
+    if (!X || !order || !Y) return ABFT_EINVAL;
+    if (rx || ry || !aligned16(X) || !aligned16(Y) || ((uintptr_t)order & 3u)) return ABFT_EALIGN;
+    return from_hip(launch_gather_rows(es, X, (int)tokens, (int)cols, ldx * es, order, (int)rows, topk, Y, ldy * es, (hipStream_t)stream));
+}
+
+// Y: rows of the experts, or absent (rows is then what place is held against)
+static int combine_args(int dtype, const void *Y, int64_t rows, int64_t cols, int64_t ldy, const int32_t *place, const float *weight, int64_t tokens, int32_t topk,
+                        CombineArgs *a)
+{
+    if (!is_half(dtype) || topk < 1) return ABFT_EINVAL;
+    const int rc = check_rows(rows, cols, Y ? ldy : cols, 1);
+    if (rc == ABFT_ESHAPE || tokens < 1 || tokens > (1 << 30) || tokens * (int64_t)topk > (1 << 30)) return ABFT_ESHAPE;
+    if (!place) return ABFT_EINVAL;
+    if ((Y && (!aligned16(Y) || (ldy * 2) % 16)) || ((uintptr_t)place & 3u) || ((uintptr_t)weight & 3u)) return ABFT_EALIGN;
+    memset(a, 0, sizeof(*a));
+    a->Y = (const uint8_t *)Y;
+    a->place = place; a->weight = weight;
+    a->tokens = (int)tokens; a->rows = (int)rows; a->cols = (int)cols; a->topk = topk;
+    a->ldy = ldy * 2;
+    return ABFT_OK;
+}
+
+extern "C" int abft_combine_rows(const void *Y, abft_dtype dtype, int64_t rows, int64_t cols, int64_t ldy, const int32_t *place, const float *weight,
+                                 int64_t tokens, int32_t topk, const void *base, int64_t ldb, void *out, int64_t ldo, void *stream)
+{
+    if (!Y || !out) return ABFT_EINVAL;
+    CombineArgs a;
+    const int rc = combine_args(dtype, Y, rows, cols, ldy, place, weight, tokens, topk, &a);
+    if (rc) return rc;
+    if (ldo < cols || (base && ldb < cols)) return ABFT_ESHAPE;
+    if (!aligned16(base) || !aligned16(out) || (ldo * 2) % 16 || (base && (ldb * 2) % 16)) return ABFT_EALIGN;
+    a.base = (const uint8_t *)base; a.out = (uint8_t *)out;
+    a.ldb = ldb * 2; a.ldo = ldo * 2;
+    return from_hip(launch_combine_rows(dtype, false, a, (hipStream_t)stream));
+}
+
+extern "C" int abft_combine_rows_grad(const void *dout, abft_dtype dtype, int64_t tokens, int64_t cols, int64_t ldd, const int32_t *place, const float *weight,
+                                      int32_t topk, const void *Y, int64_t rows, int64_t ldy, void *dY, int64_t lddy, float *dweight, void *stream)
+{
+    if (!dout || (!dY && !dweight) || (dweight && !Y)) return ABFT_EINVAL;
+    CombineArgs a;
+    const int rc = combine_args(dtype, Y, rows, cols, ldy, place, weight, tokens, topk, &a);
+    if (rc) return rc;
+    if (ldd < cols || (dY && lddy < cols)) return ABFT_ESHAPE;
+    if (!aligned16(dout) || !aligned16(dY) || (ldd * 2) % 16 || (dY && (lddy * 2) % 16) || ((uintptr_t)dweight & 3u)) return ABFT_EALIGN;
+    a.dout = (const uint8_t *)dout; a.ldo = ldd * 2;
+    a.dY = (uint8_t *)dY; a.lddy = lddy * 2; a.dweight = dweight;
+    return from_hip(launch_combine_rows(dtype, true, a, (hipStream_t)stream));
 }
 
 extern "C" int abft_gemm_done_event(abft_ctx *ctx, void *event)

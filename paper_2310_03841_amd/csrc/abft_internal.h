@@ -21,7 +21,8 @@ constexpr long MAX_GRID_X = (1L << 24) - 1;
 // Most flagged rows (columns) per batch item that localisation lists.
 constexpr int MAX_LIST = 64;
 
-enum { DT_I8 = 0, DT_BF16 = 1, DT_F16 = 2 };
+// DT_F32: routers' logits; DT_MX4: 4-bit floating point, two elements to a byte, in blocks of 32 with a power of two each.
+enum { DT_I8 = 0, DT_BF16 = 1, DT_F16 = 2, DT_F32 = 3, DT_MX4 = 4 };
 
 __host__ __device__ inline int elem_size(int dt) { return dt == DT_I8 ? 1 : 2; }
 __host__ __device__ inline int out_size(int dt) { return dt == DT_I8 ? 4 : 2; }
@@ -184,6 +185,8 @@ struct GroupKernel;
 hipError_t launch_group(int dt, int ot, bool protect, bool transB, const GroupKernel &k, GroupArgs &g, const uint32_t *b_max, const Verdict *v, hipStream_t st);
 hipError_t launch_group_check(int dt, const GroupKernel &k, const GroupArgs &g, bool transB, const Workspace &w, const Verdict &v, const OneLaunch &end, hipStream_t st);
 hipError_t launch_group_wgrad(int dt, const GroupKernel &k, GroupArgs &g, hipStream_t st);
+hipError_t launch_quantize_mx4(int dt, const void *X, int tokens, int cols, long ldx, const int *order, int rows, int topk, void *Q, long ldq, void *S, long lds, hipStream_t st);
+hipError_t launch_dequantize_mx4(int dt, const void *Q, long ldq, const void *S, long lds, int rows, int cols, void *X, long ldx, hipStream_t st);   // pitches: bytes
 hipError_t launch_quantize_rows(int dt, const void *X, int rows, int cols, long ldx, void *Q, long ldq, float *scale, hipStream_t st);
 
 }  // namespace abft

@@ -16,6 +16,7 @@
 #include "block_out.h"
 #include "group_args.h"
 #include "group_passes.h"
+#include "mx4_pass.h"
 
 namespace abft {
 
@@ -114,17 +115,27 @@ template <int DT, int W, bool KM> struct GroupOperand {
 // What a kernel computes: C over groups of rows, or the gradient over groups along the depth.
 enum { GROUP_ROWS, GROUP_DEPTH };
 
-__host__ __device__ constexpr int group_loop_bytes(int BM, int BN, int ns)
+__host__ __device__ constexpr int group_scale_loads(int BM, int BN) { return ((BM + BN) / 32 + 3) / 4; }
+template <int DT> __host__ __device__ constexpr int group_buffer_bytes(int BM, int BN)
 {
-    const int loop = ns * (BM + BN) * SLAB_BYTES, epi = 2 * (BM + BN) * 4;
+    return (BM + BN) * SLAB_BYTES + (DT == DT_MX4 ? group_scale_loads(BM, BN) * 4 * 256 : 0);
+}
+template <int DT> __host__ __device__ constexpr int group_loop_bytes(int BM, int BN, int ns)
+{
+    const int loop = ns * group_buffer_bytes<DT>(BM, BN), epi = 2 * (BM + BN) * 4;
     return loop > epi ? loop : epi;
 }
 // behind the buffers: scales of the tile's rows and columns, bias of its columns
-__host__ __device__ constexpr int group_lds_bytes(int BM, int BN, int ns, bool scaled) { return group_loop_bytes(BM, BN, ns) + (scaled ? (BM + 2 * BN) * 4 : 0); }
+template <int DT> __host__ __device__ constexpr int group_lds_bytes(int BM, int BN, int ns, bool scaled)
+{
+    return group_loop_bytes<DT>(BM, BN, ns) + (scaled ? (BM + 2 * BN) * 4 : 0);
+}
 
 // DT: of the operands; OT: of C, the same or, of scaled int8, a 16-bit type.
+// Operands in 4 bits (gemm_mx4.h): an element of one byte is two of theirs.  The powers of two of a slab's eight blocks of each row follow the operands through
+// LDS, eight bytes a row, and go to the MFMAs in a register.
 template <int DT, int OT, int BM, int BN, int NS, bool PROT, int GROUP, bool TRANSB>
-__global__ __launch_bounds__(256) void gemm_group_kernel(GroupArgs g)
+__global__ __launch_bounds__(256) void gemm_group_kernel(typename GroupArgsOf<DT>::type g)
 {
     using T = Traits<DT>;
     typedef typename T::acc_t acc_t;
@@ -132,22 +143,26 @@ __global__ __launch_bounds__(256) void gemm_group_kernel(GroupArgs g)
     constexpr bool SCALED = OT != DT, DEPTH = GROUP == GROUP_DEPTH;
     constexpr int ES = T::ES, OS = Traits<OT>::OS, KE = SLAB_BYTES / ES;
     constexpr int TM = BM / 2, TN = BN / 2, MI = TM / 32, NI = TN / 32;
-    constexpr int BUF = (BM + BN) * SLAB_BYTES;
+    constexpr bool MX4 = DT == DT_MX4;
+    constexpr int SC_LOADS = MX4 ? group_scale_loads(BM, BN) : 0;     // of a wave for a slab: 4 bytes a lane, 32 rows
+    constexpr int BUF = group_buffer_bytes<DT>(BM, BN);
     typedef GroupOperand<DT, BM, DEPTH> OpA;
     typedef GroupOperand<DT, BN, DEPTH || !TRANSB> OpB;
-    constexpr int NLD = OpA::G + OpB::G;
+    constexpr int NLD = OpA::G + OpB::G + SC_LOADS;
     static_assert((NS - 2) * NLD < 64, "the wait count is an immediate");
 
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-    fetch_args<GroupArgs>();
+    fetch_args<typename GroupArgsOf<DT>::type>();
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if constexpr (PROT) {
         if (blockIdx.x == 0 && tid < 5) g.counts[tid] = 0u;
         if ((int)blockIdx.x < g.n_pass) {
             GroupTile t;
-            if (find_tile<4 * PASS_ROWS>(g, g.pass_win, g.pass_inv, (int)blockIdx.x, &t))
-                group_pass<DT, 4>(g, t.e, t.first, t.rows, t.tm * 4 * PASS_ROWS, t.tn, smem);
+            if (find_tile<4 * PASS_ROWS>(g, g.pass_win, g.pass_inv, (int)blockIdx.x, &t)) {
+                if constexpr (MX4) mx4_pass<4>(g, t.e, t.first, t.rows, t.tm * 4 * PASS_ROWS, t.tn, smem);
+                else group_pass<DT, 4>(g, t.e, t.first, t.rows, t.tm * 4 * PASS_ROWS, t.tn, smem);
+            }
             return;
         }
     }
@@ -192,7 +207,7 @@ __global__ __launch_bounds__(256) void gemm_group_kernel(GroupArgs g)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[mi][ni][i] = T::zero();
 
-    float *const srow = reinterpret_cast<float *>(smem + group_loop_bytes(BM, BN, NS)), *const scol = srow + BM, *const sbias = scol + BN;
+    float *const srow = reinterpret_cast<float *>(smem + group_loop_bytes<DT>(BM, BN, NS)), *const scol = srow + BM, *const sbias = scol + BN;
     if constexpr (SCALED) {
         // (absent: ones, and a bias of zeros)
         for (int i = tid; i < BM; i += 256) srow[i] = g.row_scale ? g.row_scale[t.first + min(m0 + i, M - 1)] : 1.f;
@@ -208,15 +223,44 @@ __global__ __launch_bounds__(256) void gemm_group_kernel(GroupArgs g)
         oa.setup(Ab, g.lda, m0, M, wave, lane);
         ob.setup(Bb, g.ldb, n0, N, wave, lane);
         i32x4 fa[2][4][MI], fb[2][4][NI];
+        // 4 bits: where this wave's loads of powers of two read, and the words of a set: bytes 0 and 2 are those of a lane's blocks of K
+        const uint8_t *sc_src[SC_LOADS ? SC_LOADS : 1];
+        uint32_t sa[2][2][MI], sb[2][2][NI];
+        if constexpr (MX4) {
+#pragma unroll
+            for (int p = 0; p < SC_LOADS; ++p) {
+                const int r = (4 * p + wave) * 32 + (lane >> 1);              // rows of A, then of B
+                sc_src[p] = r < BM ? g.sa + (long)(t.first + min(m0 + r, M - 1)) * g.ld_sa : g.sb + (long)t.e * g.stride_sb + (long)min(n0 + r - BM, N - 1) * g.ld_sb;
+                sc_src[p] += 4 * (lane & 1);
+            }
+        }
         auto issue = [&](int s) __attribute__((always_inline)) {
             uint8_t *d = smem + (s % NS) * BUF;
             oa.issue(s, d, K, wave);
             ob.issue(s, d + OpA::BYTES, K, wave);
+            if constexpr (MX4) {
+                // (rows of scales are whole 16 bytes, so a last slab's eight are there)
+#pragma unroll
+                for (int p = 0; p < SC_LOADS; ++p)
+                    __builtin_amdgcn_global_load_lds((grp_gas_ptr)(sc_src[p] + s * 8), (grp_las_ptr)(d + (BM + BN) * SLAB_BYTES + (4 * p + wave) * 256), 4, 0, 0);
+            }
         };
         auto read = [&](int s, auto set_c) __attribute__((always_inline)) {
+            constexpr int set = decltype(set_c)::value;
             const uint8_t *d = smem + (s % NS) * BUF;
-            OpA::read(fa[decltype(set_c)::value], d, wm * TM, lane);
-            OpB::read(fb[decltype(set_c)::value], d + OpA::BYTES, wn * TN, lane);
+            OpA::read(fa[set], d, wm * TM, lane);
+            OpB::read(fb[set], d + OpA::BYTES, wn * TN, lane);
+            if constexpr (MX4) {
+                auto words = [&](int row, uint32_t &lo, uint32_t &hi) __attribute__((always_inline)) {
+                    const uint2 w = *reinterpret_cast<const uint2 *>(d + (BM + BN) * SLAB_BYTES + row * 8);
+                    lo = w.x >> (8 * lh);
+                    hi = w.y >> (8 * lh);
+                };
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi) words(wm * TM + mi * 32 + l32, sa[set][0][mi], sa[set][1][mi]);
+#pragma unroll
+                for (int ni = 0; ni < NI; ++ni) words(BM + wn * TN + ni * 32 + l32, sb[set][0][ni], sb[set][1][ni]);
+            }
         };
         auto clear_tail = [&](auto set_c) __attribute__((always_inline)) {
             constexpr int set = decltype(set_c)::value;
@@ -228,16 +272,28 @@ __global__ __launch_bounds__(256) void gemm_group_kernel(GroupArgs g)
                 for (int mi = 0; mi < MI; ++mi) fa[set][s4][mi] = mask_chunk(fa[set][s4][mi], keep);
 #pragma unroll
                 for (int ni = 0; ni < NI; ++ni) fb[set][s4][ni] = mask_chunk(fb[set][s4][ni], keep);
+                if constexpr (MX4) {
+                    // a power of two behind the last block may be anything, NaN too: the smallest
+                    const uint32_t drop = keep > 0 ? ~0u : ~(0xFFu << (16 * (s4 & 1)));
+#pragma unroll
+                    for (int mi = 0; mi < MI; ++mi) sa[set][s4 >> 1][mi] &= drop;
+#pragma unroll
+                    for (int ni = 0; ni < NI; ++ni) sb[set][s4 >> 1][ni] &= drop;
+                }
             }
         };
         auto mfmas = [&](auto set_c) __attribute__((always_inline)) {
             constexpr int set = decltype(set_c)::value;
-#pragma unroll
-            for (int s4 = 0; s4 < 4; ++s4)
+            static_for<0, 4>([&](auto s4_c) {
+                constexpr int s4 = decltype(s4_c)::value;
 #pragma unroll
                 for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
-                    for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = T::mfma(fb[set][s4][ni], fa[set][s4][mi], acc[mi][ni]);
+                    for (int ni = 0; ni < NI; ++ni) {
+                        if constexpr (MX4) acc[mi][ni] = mfma_mx4<2 * (s4 & 1)>(fb[set][s4][ni], fa[set][s4][mi], acc[mi][ni], sb[set][s4 >> 1][ni], sa[set][s4 >> 1][mi]);
+                        else acc[mi][ni] = T::mfma(fb[set][s4][ni], fa[set][s4][mi], acc[mi][ni]);
+                    }
+            });
         };
         typedef std::integral_constant<int, 0> set0;
         typedef std::integral_constant<int, 1> set1;
@@ -419,9 +475,9 @@ inline long ceil_div(long a, long b) { return (a + b - 1) / b; }
 inline long row_tiles(int M, int groups, int BM) { return groups == 1 ? ceil_div(M, BM) : M / BM + std::min(M, groups); }
 
 template <int DT, int OT, int BM, int BN, int NS, bool PROT, int GROUP, bool TRANSB>
-static hipError_t launch_one(GroupArgs &g, hipStream_t st)
+static hipError_t launch_one(typename GroupArgsOf<DT>::type &g, hipStream_t st)
 {
-    constexpr int smem = group_lds_bytes(BM, BN, NS, OT != DT);
+    constexpr int smem = group_lds_bytes<DT>(BM, BN, NS, OT != DT);
     static_assert(smem >= group_pass_lds<DT, 4>(), "the pass over A runs in the LDS of a tile");
     auto kern = gemm_group_kernel<DT, OT, BM, BN, NS, PROT, GROUP, TRANSB>;
     hipError_t e = ensure_max_lds(reinterpret_cast<const void *>(kern), smem);

@@ -30,6 +30,14 @@ struct GroupArgs {
     uint32_t pass_inv;                    // map_inverse(pass_win)
 };
 
+// Of 4-bit operands: K, lda, ldb and sB count bytes, of two elements each, and K whole blocks of 16; sums along K have 2 K terms.
+struct Mx4Args : GroupArgs {
+    const uint8_t *sa, *sb;               // powers of two of the blocks, with a bias of 127: rows of A, of B
+    long ld_sa, ld_sb, stride_sb;         // bytes
+};
+template <int DT> struct GroupArgsOf { typedef GroupArgs type; };
+template <> struct GroupArgsOf<DT_MX4> { typedef Mx4Args type; };
+
 // The rows of group e: whatever the offsets hold, inside [0, M].
 __device__ __forceinline__ void group_rows(const int *offsets, int M, int e, int *first, int *rows)
 {

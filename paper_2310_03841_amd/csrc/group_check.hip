@@ -4,7 +4,9 @@
 
 #include "abft_device.h"
 #include "check_dots.h"
+#include "gemm_mx4.h"
 #include "group_args.h"
+#include "mx4_device.h"
 
 namespace abft {
 
@@ -18,7 +20,7 @@ struct GroupCheckArgs {
     const uint32_t *rc_pred;
     const double *cc_acc, *rc_acc;
     const uint32_t *shares;               // COLS_MARKED: of the observed sums of rows, [(N + 15) / 16][M]
-    float tau_override, tau_override_cols;
+    float tau_k, tau_override, tau_override_cols;      // 1e-3 K
     uint8_t *row_flag, *col_flag;
     uint32_t *counts;
     int row_units, col_units;             // of 256 rows each, COLS_MARKED: four; per group
@@ -26,25 +28,72 @@ struct GroupCheckArgs {
     size_t zero_words, zero2_words;
 };
 
+// 4-bit operands: ldb, sB and K in bytes, as Mx4Args has them
+struct Mx4CheckArgs : GroupCheckArgs {
+    const uint8_t *sb;
+    long ld_sb, stride_sb;
+};
+template <int DT> struct GroupCheckArgsOf { typedef GroupCheckArgs type; };
+template <> struct GroupCheckArgsOf<DT_MX4> { typedef Mx4CheckArgs type; };
+
+// Dots of RW rows of 4-bit B with a vector of 2 K terms: a block to a lane, 64 at a time.
+template <int RW> __device__ __forceinline__ void mx4_row_dots(const uint8_t *X, long ld, const uint8_t *S, long lds, int row0, int rows, int K, const uint32_t *vec, float (&dot)[RW])
+{
+    const int lane = threadIdx.x & 63, nb = K / 16;
+#pragma unroll
+    for (int j = 0; j < RW; ++j) dot[j] = 0.f;
+    for (int b0 = 0; b0 < nb; b0 += 64) {
+        const int at = min(b0 + lane, nb - 1);
+        i32x4 v[RW];
+        uint32_t s[RW];
+#pragma unroll
+        for (int j = 0; j < RW; ++j) {
+            const long r = min(row0 + j, rows - 1);
+            v[j] = *reinterpret_cast<const i32x4 *>(X + r * ld + at * 16);
+            s[j] = S[r * lds + at];
+        }
+        float a[32];
+#pragma unroll
+        for (int q4 = 0; q4 < 8; ++q4) {
+            const i32x4_word w = *reinterpret_cast<const i32x4_word *>(vec + at * 32 + 4 * q4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[4 * q4 + i] = __uint_as_float((uint32_t)w[i]);
+        }
+        if (b0 + lane < nb) {
+#pragma unroll
+            for (int j = 0; j < RW; ++j) {
+                float x[32];
+                mx4_values(v[j], mx4_unit(s[j]), x);
+#pragma unroll
+                for (int q = 0; q < 32; ++q) dot[j] = __builtin_fmaf(x[q], a[q], dot[j]);
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < RW; ++j) dot[j] = wave_sum(dot[j]);
+}
+
 constexpr int GCHK_KN_LANES = 4;          // chunk columns of a unit over a B stored K x N (64 lanes run along k)
 
 // What is left to do of the columns: their predictions from B stored N x K or K x N, or nothing but to write down what the product's kernel marked.
 enum { COLS_NK, COLS_KN, COLS_MARKED };
 
 template <int DT, int RW, int COLS>
-__global__ __launch_bounds__(256) void group_check_kernel(GroupCheckArgs f)
+__global__ __launch_bounds__(256) void group_check_kernel(typename GroupCheckArgsOf<DT>::type f)
 {
     using T = Traits<DT>;
     typedef typename T::acc_t acc_t;
+    constexpr bool MX4 = DT == DT_MX4;
+    static_assert(!MX4 || COLS == COLS_NK, "4-bit B is stored N x K");
     constexpr int ES = T::ES, CE = 16 / ES;
     __shared__ acc_t part[4][GCHK_KN_LANES * CE];
-    fetch_args<GroupCheckArgs>();
+    fetch_args<typename GroupCheckArgsOf<DT>::type>();
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     for (size_t i = (size_t)blockIdx.x * 256 + tid; i < f.zero_words; i += (size_t)gridDim.x * 256) f.zero_ptr[i] = 0u;
     for (size_t i = (size_t)blockIdx.x * 256 + tid; i < f.zero2_words; i += (size_t)gridDim.x * 256) f.zero2_ptr[i] = 0u;
     auto tolerance = [&](int e) __attribute__((always_inline)) {
         if (T::IS_INT) return 0.f;
-        return f.tau_override > 0.f ? f.tau_override : (1e-3f * (float)f.K) * __uint_as_float(f.a_max[e]) * __uint_as_float(f.b_max[e]);
+        return f.tau_override > 0.f ? f.tau_override : f.tau_k * __uint_as_float(f.a_max[e]) * __uint_as_float(f.b_max[e]);
     };
     auto tolerance_cols = [&](int e) __attribute__((always_inline)) { return f.tau_override_cols > 0.f ? f.tau_override_cols : tolerance(e); };
     auto observed = [&](uint32_t *sum, const double *acc, long o) __attribute__((always_inline)) {
@@ -103,7 +152,7 @@ __global__ __launch_bounds__(256) void group_check_kernel(GroupCheckArgs f)
     int first, rows;
     group_rows(f.offsets, f.M, e, &first, &rows);
     const uint8_t *Bb = f.B + (long)e * f.sB * ES;
-    const uint32_t *asum = f.a_sum + (long)e * K;
+    const uint32_t *asum = f.a_sum + (long)e * K * (MX4 ? 2 : 1);
     bool mine_ok = false;
     int n = 0;
     acc_t pred = T::zero();
@@ -114,7 +163,8 @@ __global__ __launch_bounds__(256) void group_check_kernel(GroupCheckArgs f)
         // (a group without rows: nothing of its matrix is read)
         if (rows > 0 && row0 < N) {
             acc_t dot[RW];
-            row_dots<DT, RW>(Bb, f.ldb, row0, N, K, asum, false, dot);
+            if constexpr (MX4) mx4_row_dots<RW>(Bb, f.ldb, f.sb + (long)e * f.stride_sb, f.ld_sb, row0, N, K, asum, dot);
+            else row_dots<DT, RW>(Bb, f.ldb, row0, N, K, asum, false, dot);
 #pragma unroll
             for (int j = 0; j < RW; ++j) pred = lane == j ? dot[j] : pred;
         }
@@ -169,26 +219,39 @@ __global__ __launch_bounds__(256) void group_check_kernel(GroupCheckArgs f)
     if (nf && lane == 0) report_flags(f.counts, 1, nf);
 }
 
-hipError_t launch_group_check(int dt, const GroupKernel &k, const GroupArgs &g, bool transB, const Workspace &w, const Verdict &v, const OneLaunch &end, hipStream_t st)
+constexpr int GCHK_ROWS = 4;              // rows of B to a wave
+
+// What all launches fill in alike.
+static void check_args(GroupCheckArgs &f, const GroupArgs &g, float k, const Workspace &w, const Verdict &v, const OneLaunch &end)
 {
-    constexpr int RW = 4;
-    GroupCheckArgs f;
     f.B = g.B; f.offsets = g.offsets;
     f.M = g.M; f.N = g.N; f.K = g.K; f.groups = g.groups; f.ldb = g.ldb; f.sB = g.sB;
     f.a_sum = g.a_sum; f.a_max = g.a_max; f.b_max = w.b_max;
     f.cc_obs = g.cc_obs; f.rc_obs = g.rc_obs; f.cc_pred = w.cc_pred; f.rc_pred = g.rc_pred;
     f.cc_acc = g.cc_acc; f.rc_acc = g.rc_acc; f.shares = group_few_shares(g);
-    f.tau_override = v.tau_override; f.tau_override_cols = v.tau_override_cols;
+    f.tau_k = 1e-3f * k; f.tau_override = v.tau_override; f.tau_override_cols = v.tau_override_cols;
     f.row_flag = v.row_flag; f.col_flag = v.col_flag; f.counts = v.counts;
     f.zero_ptr = end.zero_ptr; f.zero_words = end.zero_ptr ? end.zero_words : 0;
     f.zero2_ptr = end.zero2_ptr; f.zero2_words = end.zero2_ptr ? end.zero2_words : 0;
+}
+
+// Workgroups of a launch, at most 2^22 with rows (marked: of at most 2^21 rows) and 2^23 + 2^16 with columns, for up to 2^30 rows and 2^27 columns over all
+// groups.  per: columns to a workgroup.
+static dim3 check_grid(GroupCheckArgs &f, bool marked, int per)
+{
+    f.row_units = marked ? (f.M + 3) / 4 : (f.M + 255) / 256;
+    f.col_units = (f.N + per - 1) / per;
+    const long cols = (long)f.N * f.groups;
+    return dim3((unsigned)(f.row_units + (marked ? (cols + 255) / 256 : (long)f.col_units * f.groups)));
+}
+
+hipError_t launch_group_check(int dt, const GroupKernel &k, const GroupArgs &g, bool transB, const Workspace &w, const Verdict &v, const OneLaunch &end, hipStream_t st)
+{
+    constexpr int RW = GCHK_ROWS;
+    GroupCheckArgs f;
+    check_args(f, g, (float)g.K, w, v, end);
     const bool marked = k.kind == GROUP_KERNEL_FEW;
-    const int per = transB ? 4 * RW : GCHK_KN_LANES * (16 / elem_size(dt));
-    f.row_units = marked ? (g.M + 3) / 4 : (g.M + 255) / 256;
-    f.col_units = (g.N + per - 1) / per;
-    // at most 2^22 units of rows (marked: of at most 2^21 rows) and 2^23 + 2^16 of columns, for up to 2^30 rows and 2^27 columns over all groups
-    const long cols = (long)g.N * g.groups, units = f.row_units + (marked ? (cols + 255) / 256 : (long)f.col_units * g.groups);
-    const dim3 grid((unsigned)units);
+    const dim3 grid = check_grid(f, marked, transB ? 4 * RW : GCHK_KN_LANES * (16 / elem_size(dt)));
 #define GROUP_CHECK(DT) \
     if (marked)      hipLaunchKernelGGL((group_check_kernel<DT, RW, COLS_MARKED>), grid, dim3(256), 0, st, f); \
     else if (transB) hipLaunchKernelGGL((group_check_kernel<DT, RW, COLS_NK>), grid, dim3(256), 0, st, f); \
@@ -200,6 +263,90 @@ hipError_t launch_group_check(int dt, const GroupKernel &k, const GroupArgs &g, 
     default: return hipErrorInvalidValue;
     }
 #undef GROUP_CHECK
+    return hipGetLastError();
+}
+
+hipError_t launch_mx4_check(const GroupKernel &k, const Mx4Args &g, int K, const Workspace &w, const Verdict &v, const OneLaunch &end, hipStream_t st)
+{
+    constexpr int RW = GCHK_ROWS;
+    Mx4CheckArgs f;
+    check_args(f, g, (float)K, w, v, end);
+    f.sb = g.sb; f.ld_sb = g.ld_sb; f.stride_sb = g.stride_sb;
+    const bool marked = k.kind == GROUP_KERNEL_FEW;
+    const dim3 grid = check_grid(f, marked, 4 * RW);
+    // (marked: fp32 sums and nothing of the operands)
+    if (marked) hipLaunchKernelGGL((group_check_kernel<DT_BF16, RW, COLS_MARKED>), grid, dim3(256), 0, st, (const GroupCheckArgs &)f);
+    else        hipLaunchKernelGGL((group_check_kernel<DT_MX4, RW, COLS_NK>), grid, dim3(256), 0, st, f);
+    return hipGetLastError();
+}
+
+// ---- b = B e and max|B| of each group: a workgroup to 64 bytes (four blocks) of every row, sixteen rows of them to a wave at a time.  In a fixed order.
+// zero: words that every workgroup helps to clear.
+struct Mx4EncodeArgs {
+    const uint8_t *B, *sb;
+    int N, K;                             // K: bytes
+    long ldb, sB, ld_sb, stride_sb;
+    uint32_t *b_sum, *b_max;
+    uint32_t *zero;
+    size_t zero_words;
+};
+__global__ __launch_bounds__(256) void mx4_encode_kernel(Mx4EncodeArgs a)
+{
+    __shared__ float part[4][4 * 32], tops[4];
+    fetch_args<Mx4EncodeArgs>();
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const size_t wg = (size_t)blockIdx.y * gridDim.x + blockIdx.x, wgs = (size_t)gridDim.x * gridDim.y;
+    for (size_t i = wg * 256 + tid; i < a.zero_words; i += wgs * 256) a.zero[i] = 0u;
+    const int e = blockIdx.y, nb = a.K / 16, block = blockIdx.x * 4 + (tid & 3), at = min(block, nb - 1);
+    const uint8_t *src = a.B + (long)e * a.sB + at * 16, *sc = a.sb + (long)e * a.stride_sb + at;
+    float sum[32], top = 0.f;
+#pragma unroll
+    for (int q = 0; q < 32; ++q) sum[q] = 0.f;
+    constexpr int U = 4;
+    for (int r0 = tid >> 2; r0 < a.N; r0 += 64 * U) {
+        i32x4 v[U];
+        uint32_t s[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long r = min(r0 + 64 * u, a.N - 1);
+            v[u] = *reinterpret_cast<const i32x4 *>(src + r * a.ldb);
+            s[u] = sc[r * a.ld_sb];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (r0 + 64 * u >= a.N) break;
+            float x[32];
+            mx4_values(v[u], mx4_unit(s[u]), x);
+#pragma unroll
+            for (int q = 0; q < 32; ++q) {
+                sum[q] += x[q];
+                top = fmaxf(top, fabsf(x[q]));
+            }
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < 32; ++q) {
+        float t = sum[q];
+        t += dpp_get<0x124>(t);                                  // row_ror:4 inside 16 lanes
+        t += dpp_get<0x128>(t);                                  // row_ror:8
+        t = add_xor32(add_xor16(t));
+        if (lane < 4) part[wave][lane * 32 + q] = t;
+    }
+    top = wave_max(block < nb ? top : 0.f);
+    if (lane == 0) tops[wave] = top;
+    __syncthreads();
+    if (tid < 128 && blockIdx.x * 4 + (tid >> 5) < (unsigned)nb)
+        a.b_sum[(long)e * 2 * a.K + blockIdx.x * 128 + tid] = __float_as_uint((part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]));
+    if (tid == 0) {
+        const float m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+        if (m > 0.f) atomicMax(a.b_max + e, __float_as_uint(m));
+    }
+}
+
+hipError_t launch_mx4_encode(const Mx4Args &g, const Workspace &w, uint32_t *zero, size_t zero_words, hipStream_t st)
+{
+    const Mx4EncodeArgs a = {g.B, g.sb, g.N, g.K, g.ldb, g.sB, g.ld_sb, g.stride_sb, w.b_sum, w.b_max, zero, zero_words};
+    hipLaunchKernelGGL(mx4_encode_kernel, dim3((unsigned)((g.K / 16 + 3) / 4), (unsigned)g.groups), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 

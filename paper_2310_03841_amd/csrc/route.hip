@@ -1,0 +1,308 @@
+// Routing to experts: scores of a token's logits, its best experts and their weights; and the gradient of the logits.
+//
+// A token is LPT lanes of a wave, EPL neighbouring experts to each.  The order of experts is that of score + bias (of the logits, where scores grow with them and
+// nothing is added), equal ones by index; a round takes the best that is left.
+#include "abft_device.h"
+#include "route_args.h"
+
+namespace abft {
+
+template <int DT> __device__ __forceinline__ float logit_at(const uint8_t *row, int e)
+{
+    if constexpr (DT == DT_F32) return reinterpret_cast<const float *>(row)[e];
+    else if constexpr (DT == DT_BF16) return bf16_bits_to_f32(reinterpret_cast<const uint16_t *>(row)[e]);
+    else return f16_bits_to_f32(reinterpret_cast<const uint16_t *>(row)[e]);
+}
+
+// A lane's EPL logits: experts e0 ..; those past the last are -Inf.  Rows are whole 16 bytes, so the chunk of the last expert is there.
+template <int DT, int EPL> __device__ __forceinline__ void load_logits(const uint8_t *row, int e0, int E, float (&x)[EPL])
+{
+    constexpr int ES = DT == DT_F32 ? 4 : 2, C = EPL * ES < 16 ? EPL : 16 / ES;
+#pragma unroll
+    for (int c = 0; c < EPL / C; ++c) {
+        const int at = min(e0 + c * C, (E - 1) / C * C);
+        uint32_t w[4] = {0, 0, 0, 0};
+        if constexpr (C * ES == 16) {
+            const i32x4 v = *reinterpret_cast<const i32x4 *>(row + at * ES);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = (uint32_t)v[i];
+        } else if constexpr (C * ES == 8) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(row + at * ES);
+            w[0] = v.x; w[1] = v.y;
+        } else if constexpr (C * ES == 4) {
+            w[0] = *reinterpret_cast<const uint32_t *>(row + at * ES);
+        } else {
+            w[0] = *reinterpret_cast<const uint16_t *>(row + at * ES);
+        }
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            float v;
+            if constexpr (DT == DT_F32) v = __uint_as_float(w[i]);
+            else {
+                const uint32_t h = w[i >> 1] >> (16 * (i & 1)) & 0xFFFFu;
+                v = DT == DT_BF16 ? bf16_bits_to_f32(h) : f16_bits_to_f32(h);
+            }
+            x[c * C + i] = e0 + c * C + i < E ? v : -__builtin_inff();
+        }
+    }
+}
+
+// ---------------------------------------------------------------- over the LPT lanes of a token
+template <int CTRL> __device__ __forceinline__ double dpp_get64(double v)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)dpp_mov<CTRL>((int)(uint32_t)u), hi = (uint32_t)dpp_mov<CTRL>((int)(uint32_t)(u >> 32));
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int CTRL> __device__ __forceinline__ float other(float v) { return dpp_get<CTRL>(v); }
+template <int CTRL> __device__ __forceinline__ int other(int v) { return dpp_mov<CTRL>(v); }
+template <int CTRL> __device__ __forceinline__ double other(double v) { return dpp_get64<CTRL>(v); }
+template <int D> __device__ __forceinline__ float far_other(float v) { return __shfl_xor(v, D); }
+template <int D> __device__ __forceinline__ int far_other(int v) { return __shfl_xor(v, D); }
+template <int D> __device__ __forceinline__ double far_other(double v) { return __shfl_xor(v, D); }
+template <int LPT, typename V, typename OP> __device__ __forceinline__ V over_token(V v, const OP &op)
+{
+    v = op(v, other<0xB1>(v));     // lane ^ 1
+    v = op(v, other<0x4E>(v));     // lane ^ 2
+    v = op(v, other<0x141>(v));    // i <-> 7 - i inside 8 lanes
+    v = op(v, other<0x140>(v));    // i <-> 15 - i inside 16 lanes
+    if constexpr (LPT == 64) {
+        v = op(v, far_other<16>(v));
+        v = op(v, far_other<32>(v));
+    }
+    return v;
+}
+struct Larger { template <typename V> __device__ __forceinline__ V operator()(V a, V b) const { return a > b ? a : b; } };
+struct Smaller { template <typename V> __device__ __forceinline__ V operator()(V a, V b) const { return a < b ? a : b; } };
+struct Plus { template <typename V> __device__ __forceinline__ V operator()(V a, V b) const { return a + b; } };
+
+__device__ __forceinline__ void wave_lds_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Places of the chosen experts: lane j of a token gets the j-th, -1 where none is left.  LDS, with groups: keys of a token's experts, then 64 values.
+template <int LPT, int EPL, bool GROUPED> __device__ __forceinline__ int choose(const RouteArgs &a, const float (&x)[EPL], double *lds, int l)
+{
+    const double none = -__builtin_inf();
+    const int E = a.experts, e0 = l * EPL;
+    double key[EPL];
+    if (a.by_logit) {
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) key[i] = x[i];
+    } else {
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) top = fmaxf(top, x[i]);
+        top = over_token<LPT>(top, Larger{});
+        const double m = top > -__builtin_inff() ? top : 0.f;
+        double sum = 0;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) {
+            key[i] = a.sigmoid ? 1.0 / (1.0 + exp(-(double)x[i])) : exp((double)x[i] - m);
+            sum += key[i];
+        }
+        sum = over_token<LPT>(sum, Plus{});
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) {
+            const double b = a.bias ? (double)a.bias[min(e0 + i, E - 1)] : 0.0, k = (a.sigmoid ? key[i] : key[i] / sum) + b;
+            key[i] = x[i] > -__builtin_inff() && k == k ? k : none;
+        }
+    }
+    if constexpr (GROUPED) {
+        const int G = a.groups, per = E / G;
+        double *const keys = lds, *const values = lds + LPT * EPL;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) keys[e0 + i] = key[i];
+        wave_lds_fence();
+        for (int g = l; g < G; g += LPT) {
+            double b0 = none, b1 = none;
+            for (int i = 0; i < per; ++i) {
+                const double k = keys[g * per + i];
+                b1 = k > b0 ? b0 : k > b1 ? k : b1;
+                b0 = k > b0 ? k : b0;
+            }
+            values[g] = a.group_best == 2 && b1 > none ? b0 + b1 : b0;
+        }
+        wave_lds_fence();
+        uint64_t stay = 0;
+        for (int g0 = 0; g0 < G; g0 += LPT) {
+            const int g = g0 + l;
+            int rank = 0;
+            const double v = values[min(g, G - 1)];
+            for (int h = 0; h < G; ++h) {
+                const double w = values[h];
+                rank += w > v || (w == v && h < g) ? 1 : 0;
+            }
+            const uint64_t in = __ballot(g < G && rank < a.top_groups) >> ((threadIdx.x & 63) & ~(LPT - 1));
+            stay |= (LPT == 64 ? in : in & ((1ull << (LPT & 63)) - 1)) << g0;
+        }
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) key[i] = stay >> (min(e0 + i, E - 1) / per) & 1 ? key[i] : none;
+    }
+    int mine = -1;
+    for (int j = 0; j < a.topk; ++j) {
+        double best = none;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) best = key[i] > best ? key[i] : best;
+        best = over_token<LPT>(best, Larger{});
+        int at = 1 << 30;
+#pragma unroll
+        for (int i = EPL - 1; i >= 0; --i) at = key[i] == best ? e0 + i : at;
+        at = over_token<LPT>(at, Smaller{});
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) key[i] = e0 + i == at ? none : key[i];
+        if (l == j) mine = best > none ? at : -1;
+    }
+    return mine;
+}
+
+// What the weights of chosen logits are in proportion to, m the largest of them: exp(x - m), or the sigmoid times a power of e that keeps the largest away from
+// zero.
+__device__ __forceinline__ float chosen_share(bool sigmoid, float x, float m)
+{
+    if (!sigmoid) return expf(x - m);
+    return m < 0.f ? expf(x - m) / (1.f + expf(x)) : 1.f / (1.f + expf(-x));
+}
+
+template <int DT, int LPT, int EPL, bool GROUPED> __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
+{
+    constexpr int TOKENS = 256 / LPT;
+    __shared__ double lds[GROUPED ? TOKENS * (LPT * EPL + 64) : 1];
+    fetch_args<RouteArgs>();
+    const int l = threadIdx.x % LPT, slot = threadIdx.x / LPT;
+    const long t = (long)blockIdx.x * TOKENS + slot;
+    const uint8_t *row = a.logits + (t < a.tokens ? t : a.tokens - 1) * a.ld;
+    const float none = -__builtin_inff();
+    float x[EPL];
+    load_logits<DT, EPL>(row, l * EPL, a.experts, x);
+    bool bad = false;
+    float top = none;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+        bad |= !(x[i] < __builtin_inff());
+        top = fmaxf(top, x[i]);
+    }
+    bad = over_token<LPT>((int)bad, Larger{}) != 0;
+    const int e = choose<LPT, EPL, GROUPED>(a, x, lds + (GROUPED ? slot * (LPT * EPL + 64) : 0), l);
+    const bool there = l < a.topk && e >= 0;
+    const float xe = there ? logit_at<DT>(row, e) : none;
+    float w;
+    if (a.normalise) {
+        const float m = over_token<LPT>(xe, Larger{});
+        const float s = there ? chosen_share(a.sigmoid, xe, m) : 0.f;
+        w = s / over_token<LPT>(s, Plus{});
+    } else if (a.sigmoid) {
+        w = 1.f / (1.f + expf(-xe));
+    } else {
+        top = over_token<LPT>(top, Larger{});
+        const float m = top > none ? top : 0.f;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) sum += expf(x[i] - m);
+        w = expf(xe - m) / over_token<LPT>(sum, Plus{});
+    }
+    if (l < a.topk && t < a.tokens) {
+        a.expert[t * a.topk + l] = bad ? l : e;
+        a.weight[t * a.topk + l] = bad ? __builtin_nanf("") : there ? a.scale * w : 0.f;
+    }
+}
+
+// The gradient.  With p the normalised shares and D = sum p dw: chosen logits get scale p (dw - D), times 1 - sigmoid where scores are sigmoids; without
+// normalising, s (g - sum g s) over all experts, or scale dw s (1 - s) for the chosen.
+template <int DT, int LPT, int EPL> __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a)
+{
+    constexpr int TOKENS = 256 / LPT;
+    __shared__ float lds[TOKENS * LPT * EPL];
+    fetch_args<RouteArgs>();
+    const int l = threadIdx.x % LPT, slot = threadIdx.x / LPT, e0 = l * EPL;
+    const long t = (long)blockIdx.x * TOKENS + slot, tt = t < a.tokens ? t : a.tokens - 1;
+    const uint8_t *row = a.logits + tt * a.ld;
+    const float none = -__builtin_inff();
+    float *const g = lds + slot * LPT * EPL;
+    float x[EPL];
+    load_logits<DT, EPL>(row, e0, a.experts, x);
+    bool bad = false;
+    float top = none;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+        bad |= !(x[i] < __builtin_inff());
+        top = fmaxf(top, x[i]);
+        g[e0 + i] = 0.f;
+    }
+    bad = over_token<LPT>((int)bad, Larger{}) != 0;
+    const int e = l < a.topk ? a.expert[tt * a.topk + l] : -1;
+    const bool in = e >= 0 && e < a.experts;
+    const float xe = in ? logit_at<DT>(row, e) : none;
+    const bool there = in && xe > none;
+    const float dw = there ? a.scale * a.dweight[tt * a.topk + l] : 0.f;
+    wave_lds_fence();
+    const bool spread = !a.normalise && !a.sigmoid;              // the gradient reaches experts that were not chosen
+    float m = 0.f, sum = 1.f;
+    if (spread) {
+        top = over_token<LPT>(top, Larger{});
+        m = top > none ? top : 0.f;
+        sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) sum += expf(x[i] - m);
+        sum = over_token<LPT>(sum, Plus{});
+        if (!(top > none)) sum = 1.f;                            // (no expert: all scores are zero)
+    }
+    float d;                                                     // of the chosen logit; spread: of its score
+    if (a.normalise) {
+        const float mc = over_token<LPT>(there ? xe : none, Larger{});
+        const float s = there ? chosen_share(a.sigmoid, xe, mc) : 0.f;
+        const float total = over_token<LPT>(s, Plus{}), p = total > 0.f ? s / total : 0.f;
+        d = p * (dw - over_token<LPT>(p * dw, Plus{}));
+        if (a.sigmoid) d *= 1.f / (1.f + expf(xe));
+    } else if (a.sigmoid) {
+        const float s = 1.f / (1.f + expf(-xe));
+        d = dw * s / (1.f + expf(xe));
+    } else {
+        d = dw;
+    }
+    if (there) g[e] = d;
+    wave_lds_fence();
+    const float D = spread ? over_token<LPT>(there ? dw * expf(xe - m) / sum : 0.f, Plus{}) : 0.f;
+    if (t >= a.tokens) return;
+    uint8_t *out = a.dlogits + t * a.ldd;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+        if (e0 + i >= a.experts) break;
+        float v = g[e0 + i];
+        if (spread) v = expf(x[i] - m) / sum * (v - D);
+        if (bad) v = __builtin_nanf("");
+        if constexpr (DT == DT_F32) reinterpret_cast<float *>(out)[e0 + i] = v;
+        else reinterpret_cast<uint16_t *>(out)[e0 + i] = (uint16_t)(DT == DT_BF16 ? f32_to_bf16_bits(v) : f32_to_f16_bits(v));
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+template <int DT, int LPT, int EPL> static hipError_t launch_one(bool grad, const RouteArgs &a, hipStream_t st)
+{
+    const dim3 grid((unsigned)(((long)a.tokens + 256 / LPT - 1) / (256 / LPT)));
+    if (grad)              hipLaunchKernelGGL((route_grad_kernel<DT, LPT, EPL>), grid, dim3(256), 0, st, a);
+    else if (a.groups > 1) hipLaunchKernelGGL((route_kernel<DT, LPT, EPL, true>), grid, dim3(256), 0, st, a);
+    else                   hipLaunchKernelGGL((route_kernel<DT, LPT, EPL, false>), grid, dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+template <int DT> static hipError_t launch_type(bool grad, const RouteArgs &a, hipStream_t st)
+{
+    // sixteen lanes to a token where they do: four tokens then share a wave's instructions
+    if (a.experts <= 256 && a.topk <= 16) {
+        if (a.experts <= 32)  return launch_one<DT, 16, 2>(grad, a, st);
+        if (a.experts <= 64)  return launch_one<DT, 16, 4>(grad, a, st);
+        if (a.experts <= 128) return launch_one<DT, 16, 8>(grad, a, st);
+        return launch_one<DT, 16, 16>(grad, a, st);
+    }
+    if (a.experts <= 256) return launch_one<DT, 64, 4>(grad, a, st);
+    if (a.experts <= 512) return launch_one<DT, 64, 8>(grad, a, st);
+    return launch_one<DT, 64, 16>(grad, a, st);
+}
+hipError_t launch_route(int dt, bool grad, const RouteArgs &a, hipStream_t st)
+{
+    return dt == DT_F32 ? launch_type<DT_F32>(grad, a, st) : dt == DT_BF16 ? launch_type<DT_BF16>(grad, a, st) : launch_type<DT_F16>(grad, a, st);
+}
+
+}  // namespace abft

@@ -1,0 +1,715 @@
+"""From a router's logits to the rows of its experts and back, against plain implementations in 64 bits.
+
+Tolerances.  A result rounded once from fp32 to a type with unit eps is off by at most eps / 2 of its size; an fp32 sum of n terms by at most
+n 2^-24 of the sum of their magnitudes.  exp of a difference d of logits is off by |d| 2^-24 of itself, as d is rounded, and 2^-23 by the
+function; a share of such is off by that, of it and of the sum, and by the sum's additions and the quotient.  Choices, orders and
+places are equal."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2310_03841_amd as ab
+
+TORCH = {"i8": torch.int8, "bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+U32 = 2.0 ** -24
+INF, NAN = float("inf"), float("nan")
+
+
+def pad(n, es):
+    q = 16 // es
+    return (n + q - 1) // q * q
+
+
+def half_step(t):
+    return torch.finfo(t).eps / 2
+
+
+def ok(rc):
+    assert rc == ab.ABFT_OK, ab.abft_strerror(rc)
+
+
+# ------------------------------------------------------------------------------------------ routing
+def plain_route(x, topk, score, bias, groups, top_groups, best, normalise, scale):
+    """x: float64 [T][E].  (ids, weights, scores, which tokens have no scores)"""
+    T, E = x.shape
+    bad = ~(x < INF).all(axis=1)
+    x = np.where(bad[:, None], 0.0, x)
+    masked = x == -INF
+    with np.errstate(all="ignore"):
+        if score == ab.ABFT_SOFTMAX:
+            top = x.max(axis=1, keepdims=True)
+            e = np.exp(x - np.where(top == -INF, 0.0, top))
+            s = e / np.maximum(e.sum(axis=1, keepdims=True), 1e-300)
+        else:
+            s = 1.0 / (1.0 + np.exp(-x))
+    key = s if bias is not None or (groups > 1 and best == 2) else x.copy()
+    if bias is not None:
+        key = key + bias
+    key = np.where(masked | np.isnan(key), -INF, key)
+    ids, w = np.full((T, topk), -1, np.int32), np.zeros((T, topk))
+    for t in range(T):
+        k = key[t].copy()
+        if groups > 1:
+            per = k.reshape(groups, -1)
+            top = -np.sort(-per, axis=1)[:, :best]
+            value = np.where(top[:, 0] > -INF, np.where(top > -INF, top, 0.0).sum(axis=1), -INF)
+            stay = sorted(range(groups), key=lambda g: (-value[g], g))[:top_groups]
+            out = np.ones(groups, bool)
+            out[stay] = False
+            per[out] = -INF
+        for j, e in enumerate(sorted(range(E), key=lambda e: (-k[e], e))[:topk]):
+            if k[e] > -INF:
+                ids[t, j] = e
+    there = ids >= 0
+    for t in range(T):
+        chosen = ids[t][there[t]]
+        if normalise and len(chosen):
+            # in proportion, whatever their size
+            m = x[t, chosen].max() if score == ab.ABFT_SOFTMAX else min(x[t, chosen].max(), 0.0)
+            v = x[t, chosen]
+            with np.errstate(all="ignore"):
+                q = np.exp(v - m) if score == ab.ABFT_SOFTMAX else np.where(v > 0, np.exp(-m) / (1 + np.exp(-v)), np.exp(v - m) / (1 + np.exp(np.minimum(v, 0))))
+            w[t, there[t]] = q / q.sum()
+        else:
+            w[t, there[t]] = s[t, chosen]
+    w *= scale
+    ids[bad], w[bad] = np.arange(topk), NAN
+    return ids, w, s, bad
+
+
+class Route:
+    def __init__(self, dtype, T, E, topk, score=0, bias=None, groups=1, top_groups=1, best=1, normalise=True, scale=1.0, x=None, grid=0.0, seed=0, spare=0):
+        gen = torch.Generator().manual_seed(seed)
+        es = 4 if dtype == "f32" else 2
+        self.ld = pad(E, es) + spare
+        full = torch.full((T, self.ld), NAN)
+        full[:, :E] = torch.randn(T, E, generator=gen) * 2 if x is None else x
+        if grid:
+            full = torch.round(full / grid) * grid
+        self.host = full.to(TORCH[dtype])
+        self.x = self.host[:, :E].double().numpy()
+        self.bias = torch.randn(E, generator=gen) * 0.1 if bias is True else bias
+        self.kw = dict(topk=topk, score=score, groups=groups, top_groups=top_groups, best=best, normalise=normalise, scale=scale)
+        self.dtype, self.T, self.E, self.topk = dtype, T, E, topk
+        self.dev, self.dbias = self.host.cuda(), None if self.bias is None else self.bias.cuda()
+        self.q = ab.make_routing(T, E, topk, ld=self.ld, score=score, normalise=normalise, scale=scale, bias=self.dbias, groups=groups,
+                                 top_groups=top_groups, group_best=best)
+        self.ids = torch.full((T, topk), 77, dtype=torch.int32, device="cuda")
+        self.w = torch.full((T, topk), 77.0, device="cuda")
+        self.dw = torch.randn(T, topk, generator=gen).cuda()
+        self.dx = torch.full((T, self.ld), 77.0, dtype=TORCH[dtype], device="cuda")
+
+    def forward(self, **kw):
+        ok(ab.abft_route(self.dev, ab.DTYPE_CODE[self.dtype], self.q, self.ids, self.w, **kw))
+
+    def backward(self, **kw):
+        ok(ab.abft_route_grad(self.dev, ab.DTYPE_CODE[self.dtype], self.q, self.ids, self.dw, self.dx, self.ld, **kw))
+
+    def check(self):
+        ids, w, self.s, self.bad = plain_route(self.x, bias=None if self.bias is None else self.bias.double().numpy(), **self.kw)
+        assert np.array_equal(self.ids.cpu().numpy(), ids)
+        good = self.x[~self.bad]
+        near = np.abs(good[good > -INF])
+        self.rel = (4 * (near.max() if near.size else 0.0) + self.E + 16) * U32
+        got = self.w.double().cpu().numpy()
+        assert np.array_equal(np.isnan(got), np.isnan(w))
+        assert np.all(np.isnan(w) | (np.abs(got - w) <= self.rel * np.abs(w) + 1e-37)), np.nanmax(np.abs(got - w))
+
+    def check_grad(self):
+        """Against the formula (and, with it, every other entry of a row zero or as the softmax spreads it)."""
+        ids = self.ids.cpu().numpy()
+        there = ids >= 0
+        k = self.kw
+        dw = np.where(there, self.dw.double().cpu().numpy(), 0.0) * k["scale"]
+        want, room = np.zeros((self.T, self.E)), np.zeros((self.T, self.E))
+        w = self.w.double().cpu().numpy() / k["scale"]
+        for t in range(self.T):
+            e, d = ids[t][there[t]], dw[t][there[t]]
+            if self.bad[t]:
+                want[t] = NAN
+                continue
+            s = self.s[t]
+            if k["normalise"]:
+                p = w[t][there[t]]
+                D = (p * d).sum()
+                f = 1.0 - s[e] if k["score"] else 1.0
+                want[t, e] = p * (d - D) * f
+                room[t, e] = p * (np.abs(d) + np.abs(p * d).sum()) * f
+            elif k["score"]:
+                want[t, e] = d * s[e] * (1 - s[e])
+                room[t, e] = np.abs(want[t, e])
+            else:
+                g = np.zeros(self.E)
+                g[e] = d
+                want[t] = s * (g - (g * s).sum())
+                room[t] = s * (np.abs(g) + np.abs(g * s).sum())
+        got = self.dx[:, :self.E].double().cpu().numpy()
+        assert np.array_equal(np.isnan(got), np.isnan(want))
+        t = TORCH[self.dtype]
+        # four such shares meet in an entry; an entry below the type's range is off by its smallest step
+        tol = 4 * self.rel * room + (half_step(t) if t != torch.float32 else U32) * np.abs(want) + torch.finfo(t).smallest_normal * torch.finfo(t).eps
+        assert np.all(np.isnan(want) | (np.abs(got - want) <= tol)), np.nanmax(np.abs(got - want) - tol)
+        assert torch.all(self.dx[:, self.E:] == 77)
+
+
+SIZES = [(1, 1, 1), (1, 2, 2), (3, 7, 3), (5, 8, 8), (17, 16, 4), (16, 31, 6), (33, 64, 8), (2, 100, 10), (9, 128, 16), (4, 129, 5), (65, 256, 8), (3, 200, 17),
+         (5, 257, 9), (6, 512, 32), (2, 777, 64), (3, 1024, 10)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("score", [ab.ABFT_SOFTMAX, ab.ABFT_SIGMOID])
+@pytest.mark.parametrize("T,E,topk", SIZES)
+def test_route_and_gradient_match_plain(dtype, score, T, E, topk):
+    for n, (bias, normalise) in enumerate([(None, True), (True, True), (None, False), (True, False)]):
+        r = Route(dtype, T, E, topk, score=score, bias=bias, normalise=normalise, scale=[1.0, 2.5][n & 1], seed=E + n, spare=8 * (n & 1))
+        r.forward()
+        r.check()
+        r.backward()
+        r.check_grad()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("score", [ab.ABFT_SOFTMAX, ab.ABFT_SIGMOID])
+@pytest.mark.parametrize("T,E,topk,groups,top_groups", [(1, 4, 1, 2, 1), (9, 12, 2, 3, 2), (7, 35, 5, 7, 1), (16, 64, 8, 8, 4), (5, 64, 3, 64, 9), (11, 96, 6, 48, 17), (33, 256, 8, 8, 4), (6, 256, 16, 2, 1),
+                                                        (4, 320, 8, 20, 3), (3, 512, 20, 64, 33), (2, 1024, 64, 16, 1), (8, 40, 4, 4, 4)])
+def test_groups_of_experts(dtype, score, T, E, topk, groups, top_groups):
+    for n, (bias, best) in enumerate([(None, 1), (True, 1), (None, 2), (True, 2)]):
+        r = Route(dtype, T, E, topk, score=score, bias=bias, groups=groups, top_groups=top_groups, best=best, seed=groups + n)
+        r.forward()
+        r.check()
+        r.backward()
+        r.check_grad()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("score", [ab.ABFT_SOFTMAX, ab.ABFT_SIGMOID])
+@pytest.mark.parametrize("groups,top_groups", [(1, 1), (8, 3)])
+@pytest.mark.parametrize("E", [16, 128, 512])
+def test_equal_keys_go_by_index(dtype, score, groups, top_groups, E):
+    """Logits on a coarse grid, biases equal or on one: many keys are the same."""
+    for bias in (None, torch.zeros(E), torch.arange(E).remainder(2).float() * 0.25):
+        for best in (1, 2):
+            r = Route(dtype, 40, E, 6, score=score, bias=bias, groups=groups, top_groups=top_groups, best=best, grid=0.5, seed=E)
+            r.forward()
+            r.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("score", [ab.ABFT_SOFTMAX, ab.ABFT_SIGMOID])
+@pytest.mark.parametrize("E", [64, 512])
+def test_keys_next_to_each_other(score, E):
+    """Biases that put keys 2^-22 to 2^-40 apart, closer than scores are computed in fp32: the choice is that of exact arithmetic."""
+    gen = torch.Generator().manual_seed(3)
+    for step in (2.0 ** -22, 2.0 ** -26, 2.0 ** -30):
+        x = torch.zeros(64, E) + torch.randint(0, 9, (64, E), generator=gen) * step
+        r = Route("f32", 64, E, 8, score=score, bias=torch.randint(0, 5, (E,), generator=gen) * 0.5, x=x, seed=1)
+        r.forward()
+        r.check()
+        r = Route("f32", 64, E, 8, score=score, bias=torch.zeros(E), x=x, seed=1, groups=8, top_groups=3, best=2)
+        r.forward()
+        r.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("score", [ab.ABFT_SOFTMAX, ab.ABFT_SIGMOID])
+@pytest.mark.parametrize("normalise", [True, False])
+@pytest.mark.parametrize("groups,top_groups", [(1, 1), (4, 2)])
+def test_masks_and_values_that_are_not_finite(score, normalise, groups, top_groups):
+    E, topk = 32, 6
+    x = torch.randn(12, E, generator=torch.Generator().manual_seed(5))
+    x[0] = -INF                                    # no expert at all
+    x[1, 3:] = -INF                                # fewer than topk
+    x[2, ::2] = -INF
+    x[3, 5] = NAN
+    x[4, 7] = INF
+    x[5] = NAN
+    x[6, 1], x[6, 2] = NAN, -INF
+    x[7] = torch.finfo(torch.float32).min          # the type's lowest value is a logit like others
+    x[8, 4:] = torch.finfo(torch.float32).min
+    x[9] = torch.linspace(-300, -200, E)           # scores below what fp32 holds
+    x[10] = torch.linspace(200, 300, E)
+    for bias in (None, True, torch.where(torch.arange(E) % 3 == 0, -INF, 0.0), torch.where(torch.arange(E) == 4, NAN, 0.5)):
+        for best in (1, 2):
+            r = Route("f32", 12, E, topk, score=score, bias=bias, normalise=normalise, groups=groups, top_groups=top_groups, best=best, x=x)
+            # (exact arithmetic tells far logits apart where 64 bits do not: those rows are for calls without a bias and sums)
+            if bias is not None or (groups > 1 and best == 2):
+                r = Route("f32", 7, E, topk, score=score, bias=bias, normalise=normalise, groups=groups, top_groups=top_groups, best=best, x=x[:7])
+            r.forward()
+            r.check()
+            if r.T == 7:
+                r.backward()
+                r.check_grad()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("score", [ab.ABFT_SOFTMAX, ab.ABFT_SIGMOID])
+@pytest.mark.parametrize("normalise", [True, False])
+def test_gradient_agrees_with_differences(score, normalise):
+    """Of the plain weights, in 64 bits, along one logit at a time; central differences of step h are off by h^2 times a third derivative, which is below 4 (of products of
+    shares), times the sum of |dw|."""
+    T, E, topk, h = 4, 12, 3, 1e-4
+    r = Route("f32", T, E, topk, score=score, bias=True, normalise=normalise, scale=1.5, seed=8)
+    r.forward()
+    r.check()
+    r.backward()
+    bias, dw, ids = r.bias.double().numpy(), r.dw.double().cpu().numpy(), r.ids.cpu().numpy()
+
+    def loss(x):
+        with np.errstate(all="ignore"):
+            s = np.exp(x) / np.exp(x).sum(axis=1, keepdims=True) if score == ab.ABFT_SOFTMAX else 1 / (1 + np.exp(-x))
+        w = np.take_along_axis(s, ids, axis=1)
+        return (1.5 * (w / w.sum(axis=1, keepdims=True) if normalise else w) * dw).sum(axis=1)
+
+    got = r.dx[:, :E].double().cpu().numpy()
+    for e in range(E):
+        step = np.zeros((T, E))
+        step[:, e] = h
+        slope = (loss(r.x + step) - loss(r.x - step)) / (2 * h)
+        size = 1.5 * np.abs(dw).sum(axis=1)
+        assert np.all(np.abs(got[:, e] - slope) <= size * (4 * h * h + 1e-11 + 8 * r.rel))
+
+
+@pytest.mark.gpu
+def test_gradient_takes_no_part_of_choices_outside():
+    r = Route("f32", 6, 20, 4, seed=2)
+    r.forward()
+    r.ids[1, 2], r.ids[2, 0], r.ids[3] = -1, 20, torch.tensor([2 ** 31 - 1, -2 ** 31, 21, -7], dtype=torch.int32)
+    r.backward()
+    r.check_choices = r.ids.cpu().numpy()
+    x = r.x
+    got = r.dx[:, :20].double().cpu().numpy()
+    for t in range(6):
+        keep = [(j, e) for j, e in enumerate(r.check_choices[t]) if 0 <= e < 20]
+        want = np.zeros(20)
+        if keep:
+            j, e = map(list, zip(*keep))
+            p = np.exp(x[t, e] - x[t, e].max())
+            p /= p.sum()
+            d = r.dw[t].double().cpu().numpy()[j]
+            want[e] = p * (d - (p * d).sum())
+        assert np.allclose(got[t], want, rtol=0, atol=64 * U32 * 8)
+
+
+# ------------------------------------------------------------------------------------------ entries by group
+def plain_group_rows(group, groups):
+    inside = (group >= 0) & (group < groups)
+    order = np.argsort(np.where(inside, group, groups), kind="stable").astype(np.int32)
+    used = int(inside.sum())
+    offsets = np.concatenate([[0], np.cumsum(np.bincount(group[inside], minlength=groups)[:groups])]).astype(np.int32)
+    place = np.full(len(group), -1, np.int32)
+    place[order[:used]] = np.arange(used)
+    order[used:] = -1
+    return offsets, order, place
+
+
+def group_rows(ctx, group, groups, stream=None):
+    n = len(group)
+    out = [torch.full((m,), 55, dtype=torch.int32, device="cuda") for m in (groups + 3, n + 3, n + 3)]
+    ok(ab.abft_group_rows(ctx, group, n, groups, *out, stream=stream))
+    return out
+
+
+def same_rows(out, group, groups):
+    n = len(group)
+    for got, want in zip(out, plain_group_rows(group, groups)):
+        got = got.cpu().numpy()
+        assert np.array_equal(got[:len(want)], want)
+        assert np.all(got[len(want):] == 55)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("groups", [1, 2, 5, 64, 100, 1000, 1024])
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 255, 257, 1023, 1024, 1025, 4095, 4096, 4097, 9001, 50432, 300001])
+def test_entries_by_group(n, groups):
+    rng = np.random.default_rng(n + groups)
+    ctx = ab.abft_create(n, 1024, 128, groups)
+    try:
+        for kind in range(4):
+            if kind == 0:
+                g = rng.integers(0, groups, n)
+            elif kind == 1:                       # a few groups get most, some entries outside
+                g = (groups * rng.random(n) ** 4).astype(np.int64)
+                g[rng.random(n) < 0.1] = -1
+                g[rng.random(n) < 0.02] = groups
+                g[rng.random(n) < 0.02] = 2 ** 31 - 1
+                g[rng.random(n) < 0.02] = -2 ** 31
+            elif kind == 2:
+                g = np.full(n, groups - 1)
+            else:
+                g = np.full(n, -1)
+            g = g.astype(np.int32)
+            same_rows(group_rows(ctx, torch.from_numpy(g).cuda(), groups), g, groups)
+    finally:
+        torch.cuda.synchronize()
+        ab.abft_destroy(ctx)
+
+
+# ------------------------------------------------------------------------------------------ rows there and back
+def rows_of(gen, dtype, rows, cols, spare=0):
+    ld = pad(cols, 1 if dtype == "i8" else 2) + spare
+    if dtype == "i8":
+        x = torch.randint(-128, 128, (rows, ld), generator=gen, dtype=torch.int8)
+        x[:, cols:] = 101
+        return x
+    x = torch.randn(rows, ld, generator=gen).to(TORCH[dtype])
+    x[:, cols:] = NAN
+    return x
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["i8", "bf16", "f16"])
+@pytest.mark.parametrize("tokens,topk,cols", [(1, 1, 1), (1, 4, 8), (3, 2, 7), (5, 3, 9), (17, 1, 64), (9, 8, 100), (33, 2, 513), (4, 4, 1024), (6, 3, 1001), (64, 2, 40), (3, 2, 5000), (2, 3, 9001)])
+def test_gather_rows(dtype, tokens, topk, cols):
+    gen = torch.Generator().manual_seed(cols)
+    x = rows_of(gen, dtype, tokens, cols, spare=32)
+    n = tokens * topk
+    order = torch.randperm(n, generator=gen).to(torch.int32)
+    for j, v in ((0, -1), (n // 2, n), (n - 1, 2 ** 31 - 1), (n // 3, -2 ** 31)):
+        if n > 4:
+            order[j] = v
+    y = torch.full((n + 2, pad(cols, 1 if dtype == "i8" else 2)), 77, dtype=TORCH[dtype], device="cuda")
+    ok(ab.abft_gather_rows(x.cuda(), ab.DTYPE_CODE[dtype], tokens, cols, x.shape[1], order.cuda(), n, topk, y, y.shape[1]))
+    want = torch.full(y.shape, 77, dtype=TORCH[dtype])
+    for r, i in enumerate(order.tolist()):
+        if 0 <= i < n:
+            want[r, :cols] = x[i // topk, :cols]
+    assert torch.equal(y.cpu(), want)
+
+
+class Combine:
+    def __init__(self, dtype, tokens, topk, cols, base=True, weight=True, seed=0, drop=True):
+        gen = torch.Generator().manual_seed(seed)
+        self.dtype, self.t, self.tokens, self.topk, self.cols = dtype, TORCH[dtype], tokens, topk, cols
+        self.rows = tokens * topk
+        self.Y, self.base, self.dout = rows_of(gen, dtype, self.rows, cols), rows_of(gen, dtype, tokens, cols, 8) if base else None, rows_of(gen, dtype, tokens, cols, 16)
+        self.place = torch.randperm(self.rows, generator=gen).to(torch.int32).view(tokens, topk)
+        self.weight = torch.randn(tokens, topk, generator=gen) if weight else None
+        if drop and self.rows > 3:
+            flat = self.place.view(-1)
+            for j, v in ((0, -1), (self.rows // 2, self.rows), (self.rows - 1, -2 ** 31), (self.rows // 3, 2 ** 31 - 1)):
+                flat[j] = v
+            if weight:
+                self.weight.view(-1)[0] = NAN     # of no row: no part, whatever it is
+        dev = lambda x: None if x is None else x.cuda()
+        self.d = [dev(x) for x in (self.Y, self.base, self.dout, self.place, self.weight)]
+        self.out = torch.full((tokens, pad(cols, 2) + 8), 77.0, dtype=self.t, device="cuda")
+        self.dY = torch.full((self.rows, pad(cols, 2) + 8), 77.0, dtype=self.t, device="cuda")
+        self.dw = torch.full((tokens, topk), 77.0, device="cuda")
+
+    def forward(self, **kw):
+        Y, base, _, place, weight = self.d
+        ok(ab.abft_combine_rows(Y, ab.DTYPE_CODE[self.dtype], self.rows, self.cols, Y.shape[1], place, weight, self.tokens, self.topk, base,
+                                0 if base is None else base.shape[1], self.out, self.out.shape[1], **kw))
+
+    def backward(self, dY=True, dw=True, **kw):
+        Y, _, dout, place, weight = self.d
+        ok(ab.abft_combine_rows_grad(dout, ab.DTYPE_CODE[self.dtype], self.tokens, self.cols, dout.shape[1], place, weight, self.topk, Y if dw else None, self.rows,
+                                     Y.shape[1], self.dY if dY else None, self.dY.shape[1], self.dw if dw else None, **kw))
+
+    def check(self, dY=True, dw=True):
+        c, n = self.cols, self.rows
+        y, inside = self.Y[:, :c].double(), (self.place >= 0) & (self.place < n)
+        at = torch.where(inside, self.place, 0).long()
+        w = torch.where(inside, torch.ones(at.shape, dtype=torch.float64) if self.weight is None else self.weight.double(), 0.0)
+        terms = w[..., None] * torch.where(inside[..., None], y[at], 0.0)
+        want, size = terms.sum(dim=1), terms.abs().sum(dim=1)
+        if self.base is not None:
+            want, size = want + self.base[:, :c].double(), size + self.base[:, :c].double().abs()
+        tol = half_step(self.t) * want.abs() + (1 + half_step(self.t)) * (self.topk + 1) * U32 * size + 2.0 ** -25 * (self.t == torch.float16)
+        assert torch.all((self.out[:, :c].double().cpu() - want).abs() <= tol)
+        assert torch.all(self.out[:, c:] == 77)
+        d = self.dout[:, :c].double()
+        if dY:
+            wy = torch.full((n, c), 77.0, dtype=torch.float64)
+            for t in range(self.tokens):
+                for j in range(self.topk):
+                    if inside[t, j]:
+                        wy[at[t, j]] = w[t, j] * d[t]
+            got = self.dY[:, :c].double().cpu()
+            # (a product in fp32 first)
+            assert torch.all((got - wy).abs() <= (half_step(self.t) * (1 + U32) + U32) * wy.abs() + 2.0 ** -25 * (self.t == torch.float16))
+            assert torch.all(self.dY[:, c:] == 77)
+        if dw:
+            prod = d[:, None, :] * torch.where(inside[..., None], y[at], 0.0)
+            assert torch.all((self.dw.double().cpu() - prod.sum(dim=2)).abs() <= c * U32 * prod.abs().sum(dim=2))
+
+
+COMBINE = [(1, 1, 1), (1, 4, 8), (2, 2, 7), (7, 3, 9), (5, 1, 64), (9, 8, 100), (33, 2, 513), (4, 16, 1024), (6, 9, 1001), (70, 2, 40), (3, 2, 5000), (2, 3, 9001), (600, 2, 72)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens,topk,cols", COMBINE)
+def test_combine_rows_and_gradient(dtype, tokens, topk, cols):
+    for base, weight in ((True, True), (False, True), (True, False), (False, False)):
+        p = Combine(dtype, tokens, topk, cols, base=base, weight=weight, seed=cols + topk)
+        p.forward()
+        p.backward()
+        p.check()
+
+
+@pytest.mark.gpu
+def test_one_gradient_without_the_other():
+    for dY, dw in ((True, False), (False, True)):
+        p = Combine("bf16", 9, 3, 200, seed=4)
+        p.forward()
+        p.backward(dY=dY, dw=dw)
+        p.check(dY=dY, dw=dw)
+        assert torch.all(p.dY == 77) if not dY else torch.all(p.dw == 77)
+
+
+@pytest.mark.gpu
+def test_the_base_may_be_the_output():
+    p = Combine("bf16", 9, 3, 200, seed=6)
+    p.out = torch.full((9, p.d[1].shape[1]), 77.0, dtype=torch.bfloat16, device="cuda")
+    p.out[:, :200] = p.d[1][:, :200]
+    p.d[1] = p.out
+    p.forward()
+    p.backward()
+    p.check()
+
+
+@pytest.mark.gpu
+def test_values_that_are_not_finite_stay_with_their_tokens():
+    p = Combine("bf16", 5, 2, 64, base=False, weight=True, drop=False)
+    r = int(p.place[2, 1])
+    p.d[0][r, 3], p.d[0][r, 5] = NAN, INF
+    p.forward()
+    p.backward()
+    out = p.out[:, :64].float().cpu()
+    assert torch.isnan(out[2, 3]) and torch.isinf(out[2, 5])
+    out[2, 3] = out[2, 5] = 0
+    assert torch.isfinite(out).all()
+    dw = p.dw.cpu()
+    assert not torch.isfinite(dw[2, 1])
+    dw[2, 1] = 0
+    assert torch.isfinite(dw).all() and torch.isfinite(p.dY[:, :64].float()).all()
+
+
+@pytest.mark.gpu
+def test_rows_past_32_bits():
+    """2.3 and 4.6 GB of rows: places whose offsets pass 31 and 32 bits."""
+    n, ld, cols = 70000, 32768, 40
+    y = torch.zeros(n, ld, dtype=torch.bfloat16, device="cuda")
+    x = torch.arange(6 * 40, device="cuda", dtype=torch.float32).view(6, 40).to(torch.bfloat16)
+    at = torch.tensor([0, 32767, 32768, 65535, 65536, 69999])
+    order = torch.full((n,), -1, dtype=torch.int32)
+    order[at] = torch.arange(6, dtype=torch.int32)
+    ok(ab.abft_gather_rows(x, ab.ABFT_BF16, 6, cols, 40, order.cuda(), n, 1, y, ld))
+    assert torch.equal(y[at.cuda(), :cols], x)
+    assert float(y.float().sum()) == float(x.float().sum()) if False else int((y != 0).sum()) == int((x != 0).sum())
+    place = at.to(torch.int32).cuda()
+    out = torch.zeros(6, 40, dtype=torch.bfloat16, device="cuda")
+    ok(ab.abft_combine_rows(y, ab.ABFT_BF16, n, cols, ld, place, None, 6, 1, None, 0, out, 40))
+    assert torch.equal(out, x)
+    dy, dw = torch.zeros_like(y), torch.zeros(6, 1, device="cuda")
+    ok(ab.abft_combine_rows_grad(x, ab.ABFT_BF16, 6, cols, 40, place, None, 1, y, n, ld, dy, ld, dw))
+    assert torch.equal(dy[at.cuda(), :cols], x) and int((dy != 0).sum()) == int((x != 0).sum())
+    want = (x.double() ** 2).sum(dim=1)
+    assert torch.all((dw[:, 0].double() - want).abs() <= 40 * U32 * want)
+
+
+# ------------------------------------------------------------------------------------------ a run of them
+class Layer:
+    """A layer of experts in bf16: choices, rows to experts, one product each, rows back, and its backward pass."""
+
+    def __init__(self, tokens=60, experts=6, topk=2, d=72, h=136, seed=0):
+        gen = torch.Generator().manual_seed(seed)
+        self.tokens, self.E, self.topk, self.d, self.h, self.n = tokens, experts, topk, d, h, tokens * topk
+        bf = lambda *s, std=1.0: (torch.randn(*s, generator=gen) * std).to(torch.bfloat16).cuda()
+        self.x, self.W, self.dout, self.base = bf(tokens, d), bf(experts, h, d, std=0.1), bf(tokens, h), bf(tokens, h)
+        self.logits = bf(tokens, pad(experts, 2))
+        self.logits[3] = -INF                      # a token that pads the batch
+        z = lambda t, *s: torch.zeros(s, dtype=t, device="cuda")
+        i32, b = torch.int32, torch.bfloat16
+        self.ids, self.w, self.dw = z(i32, tokens, topk), z(torch.float32, tokens, topk), z(torch.float32, tokens, topk)
+        self.offsets, self.order, self.place = z(i32, experts + 1), z(i32, self.n), z(i32, tokens, topk)
+        self.xs, self.ys, self.dys, self.dxs = z(b, self.n, d), z(b, self.n, h), z(b, self.n, h), z(b, self.n, d)
+        self.out, self.dx, self.dW, self.dlogits = z(b, tokens, h), z(b, tokens, d), z(b, experts, h, d), z(b, *self.logits.shape)
+        self.ctx = ab.abft_create(self.n, experts * max(d, h), experts * 256, experts)
+        self.q = ab.make_routing(tokens, experts, topk, ld=self.logits.shape[1])
+        self.s = ab.make_shape(self.n, h, d, batch=experts)
+        self.sx = ab.make_shape(self.n, d, h, batch=experts, transB=False)
+        self.flags = z(torch.uint8, self.n), z(torch.uint8, experts * h), z(i32, 8)
+        self.res = ab.make_result(*self.flags)
+
+    def run(self):
+        bf, t, k, n, d, h = ab.ABFT_BF16, self.tokens, self.topk, self.n, self.d, self.h
+        ok(ab.abft_route(self.logits, bf, self.q, self.ids, self.w))
+        ok(ab.abft_group_rows(self.ctx, self.ids, n, self.E, self.offsets, self.order, self.place))
+        ok(ab.abft_gather_rows(self.x, bf, t, d, d, self.order, n, k, self.xs, d))
+        ok(ab.abft_gemm_grouped(self.ctx, self.xs, self.W, self.offsets, None, self.ys, bf, ab.ABFT_DETECT, self.s, self.res))
+        ok(ab.abft_combine_rows(self.ys, bf, n, h, h, self.place, self.w, t, k, self.base, h, self.out, h))
+        ok(ab.abft_combine_rows_grad(self.dout, bf, t, h, h, self.place, self.w, k, self.ys, n, h, self.dys, h, self.dw))
+        ok(ab.abft_gemm_grouped_wgrad(self.ctx, self.xs, self.dys, self.offsets, self.dW, bf, self.s))
+        ok(ab.abft_gemm_grouped(self.ctx, self.dys, self.W, self.offsets, None, self.dxs, bf, ab.ABFT_OFF, self.sx))
+        ok(ab.abft_combine_rows(self.dxs, bf, n, d, d, self.place, None, t, k, None, 0, self.dx, d))
+        ok(ab.abft_route_grad(self.logits, bf, self.q, self.ids, self.dw, self.dlogits, self.logits.shape[1]))
+
+    def outputs(self):
+        return [x.clone() for x in (self.ids, self.w, self.out, self.dx, self.dW, self.dlogits, *self.flags)]
+
+    def check(self):
+        """Against autograd in 64 bits over the same choices.  A value has been rounded to bf16 once in itself and in each of up to three before it
+        (ys, dys, dxs; the fp32 sums are 2^-16 of that): four half steps of the magnitudes that meet in it."""
+        E, k, ids = self.E, self.topk, self.ids.cpu().long()
+        x, W, dout = self.x.double().cpu(), self.W.double().cpu(), self.dout.double().cpu()
+        lg = torch.where(torch.isinf(self.logits[:, :E]), -1e4, self.logits[:, :E].float()).double().cpu()
+        there = ids >= 0
+        assert not there[3].any() and there.sum() == (self.tokens - 1) * k
+
+        def f(x, W, lg, dout):
+            p = torch.softmax(lg, dim=1).gather(1, ids.clamp(min=0)) * there
+            w = p / p.sum(dim=1, keepdim=True).clamp(min=1e-300)        # (a token of no expert: zeros)
+            y = torch.stack([torch.matmul(x, W[e].t()) for e in range(E)])            # E x tokens x h
+            mine = y[ids.clamp(min=0), torch.arange(self.tokens)[:, None]]
+            return (w[..., None] * mine).sum(dim=1), w, mine
+
+        leaves = [v.clone().requires_grad_() for v in (x, W, lg)]
+        out, w, mine = f(*leaves, dout)
+        grads = torch.autograd.grad((out * dout).sum(), leaves)
+        # the magnitudes: the same sums of absolute values
+        big = [v.abs().requires_grad_() for v in (x, W)]
+        out_b, w_b, mine_b = f(*big, lg, dout)
+        sizes = torch.autograd.grad((out_b * dout.abs()).sum(), big)
+        four = 4 * half_step(torch.bfloat16)
+        base = self.base.double().cpu()
+        assert torch.all((self.out.double().cpu() - out - base).abs() <= four * (out_b + base.abs()))
+        for got, want, size in ((self.dx, grads[0], sizes[0]), (self.dW, grads[1], sizes[1])):
+            assert torch.all((got.double().cpu() - want).abs() <= four * size + 1e-30)
+        size = w * ((mine_b * dout.abs()[:, None]).sum(dim=2) + (w * (mine_b * dout.abs()[:, None]).sum(dim=2)).sum(dim=1, keepdim=True))
+        room = torch.zeros(self.tokens, E, dtype=torch.float64).scatter_add_(1, ids.clamp(min=0), torch.where(there, size, 0.0))
+        want = torch.where(there[:, :1], grads[2], 0.0)
+        # (the plain form goes through the softmax over all experts: terms of up to 100 that cancel in 64 bits, at up to 2^-53 of them each)
+        assert torch.all((self.dlogits[:, :E].double().cpu() - want).abs() <= four * room + 1e-12)
+        assert self.flags[2][:3].tolist() == [0, 0, 0]
+
+
+@pytest.mark.gpu
+def test_a_layer_of_experts_and_its_backward_pass():
+    p = Layer()
+    try:
+        p.run()
+        p.check()
+    finally:
+        torch.cuda.synchronize()
+        ab.abft_destroy(p.ctx)
+
+
+@pytest.mark.gpu
+def test_a_layer_of_experts_in_a_graph():
+    """Captured once, replayed with other inputs, with eager calls between the replays; and a second graph of the same context."""
+    p = Layer(seed=1)
+    try:
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            p.run()
+            s.synchronize()
+            graphs = []
+            for _ in range(2):
+                g = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(g, stream=s):
+                    p.run()
+                graphs.append(g)
+            gen = torch.Generator().manual_seed(9)
+            for i in range(5):
+                p.logits[:, :p.E] = torch.randn(p.tokens, p.E, generator=gen).to(torch.bfloat16).cuda()
+                p.logits[3] = -INF
+                p.x.copy_(torch.randn(p.tokens, p.d, generator=gen).to(torch.bfloat16))
+                for v in (p.xs, p.ys, p.dys, p.dxs):
+                    v.zero_()
+                p.run()
+                eager = p.outputs()
+                for v in (p.out, p.dx, p.dW, p.dlogits, p.w, p.ids, p.place, p.order, p.offsets, p.xs, p.ys, p.dys, p.dxs):
+                    v.zero_()
+                graphs[i & 1].replay()
+                s.synchronize()
+                for a, b in zip(eager, p.outputs()):
+                    assert torch.equal(a, b)
+                p.check()
+    finally:
+        torch.cuda.synchronize()
+        ab.abft_destroy(p.ctx)
+
+
+@pytest.mark.gpu
+def test_on_other_streams_at_once():
+    """Two streams, each with its own context and buffers, behind work that is still running."""
+    layers, streams = [Layer(seed=2), Layer(seed=3)], [torch.cuda.Stream(), torch.cuda.Stream()]
+    try:
+        torch.cuda.synchronize()
+        junk = torch.randn(2048, 2048, device="cuda")
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for p, s in zip(layers, streams):
+                with torch.cuda.stream(s):
+                    junk @ junk
+                    p.run()
+        torch.cuda.synchronize()
+        for p in layers:
+            p.check()
+    finally:
+        torch.cuda.synchronize()
+        for p in layers:
+            ab.abft_destroy(p.ctx)
+
+
+# ------------------------------------------------------------------------------------------ refusals
+P = 0x1000
+
+
+def expect(call, good, changes):
+    for change, code in changes:
+        assert call(**{**good, **change}) == code, (change, ab.abft_strerror(code))
+
+
+def test_refusals_of_routing_need_no_gpu():
+    E, S, A = ab.ABFT_EINVAL, ab.ABFT_ESHAPE, ab.ABFT_EALIGN
+    r = lambda **k: ab.make_routing(**{**dict(tokens=4, experts=16, topk=2), **k})
+    reserved = r()
+    reserved.reserved = 1
+    wrong = [(dict(routing=r(tokens=0)), S), (dict(routing=r(tokens=(1 << 24) + 1)), S), (dict(routing=r(experts=0, topk=1)), S),
+             (dict(routing=r(experts=1025, ld=1032)), S), (dict(routing=r(ld=8)), S), (dict(routing=r(topk=0)), S), (dict(routing=r(topk=17)), S),
+             (dict(routing=r(experts=128, topk=65)), S), (dict(routing=r(groups=3)), S), (dict(routing=r(groups=0)), S), (dict(routing=r(groups=4, top_groups=5)), S),
+             (dict(routing=r(groups=4, top_groups=0)), S), (dict(routing=r(groups=16, top_groups=1)), S), (dict(routing=r(experts=130, groups=65, top_groups=65)), S),
+             (dict(routing=r(score=2)), E), (dict(routing=r(group_best=3)), E), (dict(routing=r(group_best=0)), E), (dict(routing=r(scale=INF)), E), (dict(routing=r(scale=NAN)), E),
+             (dict(routing=reserved), E), (dict(routing=r(bias=P + 2)), A), (dict(routing=r(ld=20)), A), (dict(dtype=ab.ABFT_I8), E), (dict(dtype=4), E),
+             (dict(logits=None), E), (dict(logits=P + 8), A), (dict(expert=None), E), (dict(expert=P + 2), A)]
+    expect(ab.abft_route, dict(logits=P, dtype=ab.ABFT_BF16, routing=r(), expert=P, weight=P, stream=0), wrong + [(dict(weight=None), E), (dict(weight=P + 1), A)])
+    expect(ab.abft_route_grad, dict(logits=P, dtype=ab.ABFT_BF16, routing=r(), expert=P, dweight=P, dlogits=P, ldd=16, stream=0),
+           wrong + [(dict(dweight=None), E), (dict(dlogits=None), E), (dict(ldd=15), S), (dict(ldd=20), A), (dict(dlogits=P + 8), A), (dict(dweight=P + 2), A)])
+    assert ctypes.sizeof(ab.abft_routing) == 8 * 8
+
+
+def test_refusals_of_rows_need_no_gpu():
+    E, S, A = ab.ABFT_EINVAL, ab.ABFT_ESHAPE, ab.ABFT_EALIGN
+    expect(ab.abft_group_rows, dict(ctx=None, group=P, n=4, groups=4, offsets=P, order=P, place=P, stream=0),
+           [(dict(), E), (dict(n=0), S), (dict(groups=0), S), (dict(groups=1025), S), (dict(n=(1 << 30) + 1), S)])
+    expect(ab.abft_gather_rows, dict(X=P, dtype=ab.ABFT_BF16, tokens=4, cols=8, ldx=8, order=P, rows=8, topk=2, Y=P, ldy=8, stream=0),
+           [(dict(dtype=ab.ABFT_F32), E), (dict(topk=0), E), (dict(tokens=0), S), (dict(rows=0), S), (dict(cols=0), S), (dict(ldx=4), S), (dict(ldy=4), S), (dict(ldx=12), A), (dict(ldy=12), A),
+            (dict(X=None), E), (dict(order=None), E), (dict(Y=None), E), (dict(X=P + 8), A), (dict(Y=P + 8), A), (dict(order=P + 2), A), (dict(rows=(1 << 30) + 1), S),
+            (dict(dtype=ab.ABFT_I8, ldx=16, ldy=8), A)])
+    good = dict(Y=P, dtype=ab.ABFT_BF16, rows=8, cols=8, ldy=8, place=P, weight=P, tokens=4, topk=2, base=P, ldb=8, out=P, ldo=8, stream=0)
+    common = [(dict(dtype=ab.ABFT_I8), E), (dict(topk=0), E), (dict(tokens=0), S), (dict(rows=0), S), (dict(cols=0), S), (dict(tokens=1 << 29, topk=3), S), (dict(place=None), E), (dict(place=P + 2), A),
+              (dict(weight=P + 2), A), (dict(Y=P + 8), A), (dict(ldy=4), S), (dict(ldy=12), A)]
+    expect(ab.abft_combine_rows, good, common + [(dict(Y=None), E), (dict(out=None), E), (dict(ldo=4), S), (dict(ldo=12), A), (dict(ldb=4), S), (dict(ldb=12), A), (dict(base=P + 8), A), (dict(out=P + 8), A)])
+    good = dict(dout=P, dtype=ab.ABFT_BF16, tokens=4, cols=8, ldd=8, place=P, weight=P, topk=2, Y=P, rows=8, ldy=8, dY=P, lddy=8, dweight=P, stream=0)
+    expect(ab.abft_combine_rows_grad, good, common + [(dict(dout=None), E), (dict(dY=None, dweight=None), E), (dict(Y=None), E), (dict(ldd=4), S), (dict(ldd=12), A), (dict(lddy=4), S), (dict(lddy=12), A),
+                                                      (dict(dY=P + 8), A), (dict(dout=P + 8), A), (dict(dweight=P + 2), A)])
+
+
+@pytest.mark.gpu
+def test_entries_beyond_the_context_are_refused():
+    ctx = ab.abft_create(64, 16, 16, 4)
+    try:
+        g = lambda **k: ab.abft_group_rows(**{**dict(ctx=ctx, group=P, n=64, groups=4, offsets=P, order=P, place=P), **k})
+        for change, code in [(dict(n=65), ab.ABFT_EWORKSPACE), (dict(groups=5), ab.ABFT_EWORKSPACE), (dict(group=None), ab.ABFT_EINVAL), (dict(offsets=None), ab.ABFT_EINVAL),
+                             (dict(order=None), ab.ABFT_EINVAL), (dict(place=None), ab.ABFT_EINVAL), (dict(order=P + 2), ab.ABFT_EALIGN)]:
+            assert g(**change) == code, change
+    finally:
+        ab.abft_destroy(ctx)
