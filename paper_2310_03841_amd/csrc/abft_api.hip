@@ -967,7 +967,7 @@ extern "C" int abft_gemm_mx4(abft_ctx *ctx, const void *A, const void *B, const 
         ctx->pred_valid = false;
         ctx->vobs_valid = false;
         ctx->arm.batch = -1;
-        HIP_TRY(k.kind == GROUP_KERNEL_FEW ? launch_mx4_few(q->out, false, g, nullptr, tau_k, 0.f, st) : launch_mx4_rows(q->out, k.tiles, false, g, st));
+        HIP_TRY(launch_mx4(k, q->out, false, g, nullptr, tau_k, 0.f, st));
         if (ctx->done_event && !capturing(st)) HIP_TRY(hipEventRecord(ctx->done_event, st));
         return ABFT_OK;
     }
@@ -983,9 +983,7 @@ extern "C" int abft_gemm_mx4(abft_ctx *ctx, const void *A, const void *B, const 
     const float tau_cols = v.tau_override_cols > 0.f ? v.tau_override_cols : v.tau_override;
     rc = enqueue_group(ctx, DT_BF16, cached, g, sh, v, st,
                        [&](const Workspace &w, uint32_t *zero, size_t words) { return launch_mx4_encode(g, w, zero, words, st); },
-                       [&](const Workspace &w) {
-                           return k.kind == GROUP_KERNEL_FEW ? launch_mx4_few(q->out, true, g, w.b_max, tau_k, tau_cols, st) : launch_mx4_rows(q->out, k.tiles, true, g, st);
-                       },
+                       [&](const Workspace &w) { return launch_mx4(k, q->out, true, g, w.b_max, tau_k, tau_cols, st); },
                        [&](const Workspace &w, const OneLaunch &end) { return launch_mx4_check(k, g, (int)s->K, w, v, end, st); });
     if (rc) return rc;
     ctx->b_valid = true;

@@ -238,6 +238,8 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, SRC sou
     const GemmArgs &g = source.template get<PROT>(tile);
     using T = Traits<DT>;
     constexpr bool SCALED = OT != DT;
+    constexpr bool FACTORS = SCALED && DT != DT_MX4;         // of rows and columns (those of 4 bits are the MFMAs' own: a bias is left)
+    constexpr bool SUMS16 = !T::IS_INT && DT != DT_MX4;      // 16-bit types: tiles may have reduced slabs of A (of 4 bits none do)
     typedef typename T::acc_t acc_t;
     constexpr int BN = 256, THREADS = 64 * FAST_WAVES;
     constexpr int TM = BM / 2, TN = BN / 4;         // waves: two rows of four
@@ -272,12 +274,18 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, SRC sou
     }
     float *const scol = reinterpret_cast<float *>(amax_w + FAST_WAVES), *const sbias = scol + BN, *const srow = sbias + BN;
     if constexpr (SCALED) {
-        if (tid < BN) { scol[tid] = sc.col; sbias[tid] = sc.bias; }
-        if (tid < BM) srow[tid] = sc.row;
+        if (tid < BN) {
+            if constexpr (FACTORS) scol[tid] = sc.col;
+            sbias[tid] = sc.bias;
+        }
+        if (FACTORS && tid < BM) srow[tid] = sc.row;
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
     // each step one rounding of fp32: the sum, times the row's scale, times the column's, the bias with it
-    auto scaled = [&](acc_t v, float row, float col, float b) __attribute__((always_inline)) { return __builtin_fmaf((float)v * row, col, b); };
+    auto scaled = [&](acc_t v, float row, float col, float b) __attribute__((always_inline)) {
+        if constexpr (FACTORS) return __builtin_fmaf((float)v * row, col, b);
+        else return (float)v + b;
+    };
     if (PROT && ep.owned > 0) {
         // what the pass over A's slabs left in registers (nothing in a tile that reduced no slab: where K has fewer slabs than the
         // tile row has tiles, that is most tiles)
@@ -290,7 +298,7 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, SRC sou
             // (finite, and so is the sum of four)
             if constexpr (!T::IS_INT) dots_bad |= lane < 32 && !(fabsf(v) < 0x1p125f);
         }
-        if constexpr (!T::IS_INT) {
+        if constexpr (SUMS16) {
             constexpr uint32_t INF_BITS = DT == DT_BF16 ? 0x7F80u : 0x7C00u;
             const uint32_t hi = ep.pass.amax >> 16, lo = ep.pass.amax & 0xFFFFu;
             uint32_t w = hi > lo ? hi : lo;
@@ -402,14 +410,14 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, SRC sou
 
     // scales and bias of the lane's columns, in registers: read again with every group of rows they were 512 KB of LDS traffic to a tile
     // (protected, there are registers for the scales alone)
-    i32x4 col4[SCALED ? NI : 1][4], bias4[SCALED && !PROT ? NI : 1][4];
+    i32x4 col4[FACTORS ? NI : 1][4], bias4[SCALED && !PROT ? NI : 1][4];
     if constexpr (SCALED) {
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int c = wn * TN + ni * 32 + 8 * q + 4 * lh;
-                col4[ni][q] = *reinterpret_cast<const i32x4 *>(scol + c);
+                if constexpr (FACTORS) col4[ni][q] = *reinterpret_cast<const i32x4 *>(scol + c);
                 if constexpr (!PROT) bias4[ni][q] = *reinterpret_cast<const i32x4 *>(sbias + c);
             }
     }
@@ -420,7 +428,7 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, SRC sou
             // ---- register path: one read of every accumulator serves the sums and the store
             acc_t rowsum = T::zero();
             float rscale = 1.f;
-            if constexpr (SCALED) rscale = srow[wm * TM + mi * 32 + l32];
+            if constexpr (FACTORS) rscale = srow[wm * TM + mi * 32 + l32];
             static_for<0, NI>([&](auto ni_c) {
                 constexpr int ni = decltype(ni_c)::value;
                 static_for<0, 4>([&](auto q_c) {
@@ -444,7 +452,7 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, SRC sou
                     }
                     uint8_t *d = wbuf + l32 * CROW + (ni * 32 + 8 * q + 4 * lh) * OS;
                     if constexpr (SCALED) {
-                        const i32x4 c4 = col4[ni][q];
+                        const i32x4 c4 = FACTORS ? col4[FACTORS ? ni : 0][q] : i32x4{0, 0, 0, 0};
                         const i32x4 b4 = PROT ? *reinterpret_cast<const i32x4 *>(sbias + wn * TN + ni * 32 + 8 * q + 4 * lh) : bias4[PROT ? 0 : ni][q];
                         auto f = [&](int e) __attribute__((always_inline)) { return __uint_as_float((uint32_t)e); };
                         uint2 w;
@@ -509,11 +517,11 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, SRC sou
                 acc_t v = from_word<acc_t>(*reinterpret_cast<const uint32_t *>(wbuf + r * SROW + lane * 4));
                 if (has_bias) v = add_t(v, bias_lds[wn * TN + lane]);
                 if constexpr (SCALED) {
-                    float x = scaled(v, srow[wm * TM + mi * 32 + r], scol[wn * TN + lane], sbias[wn * TN + lane]);
+                    float x = scaled(v, FACTORS ? srow[wm * TM + mi * 32 + r] : 1.f, FACTORS ? scol[wn * TN + lane] : 1.f, sbias[wn * TN + lane]);
                     // (the compiler makes product, sum and fp16 value one instruction with one rounding, where the register path has two)
                     asm("" : "+v"(x));
                     Traits<OT>::store_c(Cb, (long)(br + r) * g.ldc + gc, x);
-                } else T::store_c(Cb, (long)(br + r) * g.ldc + gc, v);
+                } else Traits<OT>::store_c(Cb, (long)(br + r) * g.ldc + gc, v);
                 if (PROT) colacc = add_t(colacc, v);
                 if constexpr (STO) {
                     const float sv = stored_value<DT>((float)v);
@@ -627,14 +635,14 @@ __device__ __forceinline__ void gemm_epilogue_impl(const GemmArgs &tile, SRC sou
             float v = (float)rp_part[t] + (float)rp_part[BM + t] + ((float)rp_part[2 * BM + t] + (float)rp_part[3 * BM + t]);
             const bool mine = ln < RW && m0 + t < M;
             const uint32_t which = (uint32_t)__ballot(mine && !(fabsf(v) < __builtin_inff()));
-            if constexpr (!T::IS_INT) v = dots_again<DT>(g, ep, bz, m0 + wave * RW, which, v);
+            if constexpr (SUMS16) v = dots_again<DT>(g, ep, bz, m0 + wave * RW, which, v);
             if (mine) atomic_add_word(g.rc_pred + (long)bz * M + m0 + t, v);
         }
         // column sums of A over this tile's rows, for the slabs this workgroup reduced
         for (int t = tid; t < ep.owned * KE && !g.a_given; t += THREADS) {
             const int k = (ep.slab0 + (t / KE) * ep.slab_step) * KE + (t % KE);
             acc_t v = from_word<acc_t>(ep.col_lds[t]);
-            if constexpr (!T::IS_INT) {
+            if constexpr (SUMS16) {
                 // (a wave's 64 columns are one slab's)
                 const uint64_t which = __ballot(!(fabsf(v) < __builtin_inff()));
                 if (__builtin_expect(which != 0, 0)) v = columns_again<DT>(g, bz, m0, M - m0 < BM ? M - m0 : BM, k - (t % KE), which, v);

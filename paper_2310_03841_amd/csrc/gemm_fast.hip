@@ -201,13 +201,13 @@ static hipError_t launch_fast_one(GemmArgs &g, int batch, hipStream_t st)
     auto kern = STO && !big_rows ? gemm_fast_kernel<DT, PROT ? FAST_OWN : FAST_PLAIN, SMALL> : gemm_fast_kernel<DT, PROT ? FAST_OWN : FAST_PLAIN, ALL>;
     if constexpr (PROT) {
         const size_t aux = fast_aux_bytes(DT, slabs, g.tiles_n);
-        smem = fast_lds_bytes<FAST_OWN>() + aux;
+        smem = fast_lds_bytes<DT, FAST_OWN>() + aux;
         if (g.beside.n) {
             kern = STO && !big_rows ? gemm_fast_kernel<DT, FAST_BESIDE, SMALL> : gemm_fast_kernel<DT, FAST_BESIDE, ALL>;
-            smem = fast_lds_bytes<FAST_BESIDE>();
+            smem = fast_lds_bytes<DT, FAST_BESIDE>();
         }
     } else {
-        smem = fast_lds_bytes<FAST_PLAIN>();
+        smem = fast_lds_bytes<DT, FAST_PLAIN>();
     }
     if (smem > (size_t)smem_max) return hipErrorInvalidValue;
     e = ensure_max_lds(reinterpret_cast<const void *>(kern), smem_max);
@@ -226,7 +226,7 @@ bool gemm_fast_eligible(int dt, int M, int N, int K, bool transB, long lda, long
            lda * elem_size(dt) < (1L << 23) && ldb * elem_size(dt) < (1L << 23) &&
            // what the pass over A's slabs keeps per tile fits behind the operand buffers (protected or
            // not: a problem takes the same kernel in every mode)
-           fast_lds_bytes<FAST_OWN>() + fast_aux_bytes(dt, K / ke, (N + 255) / 256) <= 160 * 1024;
+           fast_lds_bytes<DT_BF16, FAST_OWN>() + fast_aux_bytes(dt, K / ke, (N + 255) / 256) <= 160 * 1024;
 }
 
 void gemm_fast_tile(int *tm, int *tn) { *tm = 256; *tn = 256; }

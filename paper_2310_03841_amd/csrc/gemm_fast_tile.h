@@ -3,6 +3,7 @@
 #include "abft_device.h"
 #include "gemm_args.h"
 #include "gemm_epilogue.h"
+#include "mx4_device.h"
 
 namespace abft {
 
@@ -35,14 +36,17 @@ template <int BM, int FM, int FN> struct FastLds {
     static constexpr int load_of_a(int mi) { return mi < FM ? NR + mi : mi - FM; }
     static constexpr int load_of_b(int ni) { return ni < FN ? NR + FM + 2 * ni : MI - FM + 2 * (ni - FN); }      // h = 0
 };
-template <int MODE, int BM> struct FastShape;
-template <int MODE> struct FastShape<MODE, 256> { typedef FastLds<256, MODE == FAST_OWN ? 3 : 4, 0> lds; };
-template <int MODE> struct FastShape<MODE, 128> { typedef FastLds<128, 2, 2> lds; };
-template <int MODE> constexpr int fast_lds_bytes()
+// 4-bit operands: behind the buffers lie two of the powers of two of a slab, eight bytes to a row, 256 rows of A and of B.
+constexpr int FAST_SCALES = 2 * 256 * 8;
+template <int DT, int MODE, int BM> struct FastShape;
+template <int DT, int MODE> struct FastShape<DT, MODE, 256> { typedef FastLds<256, MODE == FAST_OWN || DT == DT_MX4 ? 3 : 4, 0> lds; };
+template <int DT, int MODE> struct FastShape<DT, MODE, 128> { typedef FastLds<128, 2, 2> lds; };
+template <int DT, int MODE> constexpr int fast_ring_bytes()
 {
-    const int b = FastShape<MODE, 256>::lds::BYTES, s = FastShape<MODE, 128>::lds::BYTES;
+    const int b = FastShape<DT, MODE, 256>::lds::BYTES, s = FastShape<DT, MODE, 128>::lds::BYTES;
     return b > s ? b : s;
 }
+template <int DT, int MODE> constexpr int fast_lds_bytes() { return fast_ring_bytes<DT, MODE>() + (DT == DT_MX4 ? 2 * FAST_SCALES : 0); }
 
 // One BM x 256 tile with origin (m0, n0) of batch item bz.
 // What the pass over A keeps lies behind the operand buffers.
@@ -52,7 +56,7 @@ template <int DT, int OT, int BM, int MODE, int STO, bool AT, bool BT, typename 
 __device__ __forceinline__ void fast_tile(const GemmArgs &g, SRC source, uint8_t *smem, int m0, int n0, int bz, int tn)
 {
     using T = Traits<DT>;
-    using L = typename FastShape<MODE, BM>::lds;
+    using L = typename FastShape<DT, MODE, BM>::lds;
     typedef typename T::accv_t accv_t;
     typedef __attribute__((address_space(3))) uint8_t *lds_ptr;
     typedef __attribute__((address_space(3))) void *lds_void;
@@ -125,8 +129,57 @@ __device__ __forceinline__ void fast_tile(const GemmArgs &g, SRC source, uint8_t
     auto load = [&](auto q_c, int s, Buf to) __attribute__((always_inline)) {
         constexpr int q = decltype(q_c)::value;
         const lds_ptr dst = lds + ((L::ring3(q) ? to.f : to.r) + wave * 8 * SLAB_BYTES) + L::at(q);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(L::is_a(q) ? a_src : b_src, (lds_void)dst, 16, off[q], s * (L::is_a(q) ? a_step : b_step), 0, 0);
+        int at = s * (L::is_a(q) ? a_step : b_step);
+        // (4 bits: slabs past the last one lie past the descriptor's end, and cost no memory)
+        if constexpr (DT == DT_MX4) at = s < nslab ? at : 0x7FFFFFFF;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(L::is_a(q) ? a_src : b_src, (lds_void)dst, 16, off[q], at, 0, 0);
     };
+    // 4 bits: the powers of two of a slab go through LDS as the units with two buffers do, two loads of a wave ahead of those; a lane reads the word of its rows' next four
+    // blocks two steps at a time, and bytes 0 and 2 of it, shifted, are those of its own blocks.  (Straight into registers, two steps ahead of their use: loads come back in order, so a
+    // wait for these is one for the operands of slabs to come; bf16 out, 12608 x 1024 x 4096 in 8 groups 65 us.)
+    constexpr bool MX4 = DT == DT_MX4;
+    constexpr int SCALE_LOADS = MX4 ? 2 : 0;
+    [[maybe_unused]] uint32_t sa[2][MX4 ? MI : 1], sb[2][MX4 ? NI : 1];
+    [[maybe_unused]] int sa_off, sb_off;
+    [[maybe_unused]] __amdgpu_buffer_rsrc_t sa_src, sb_src;
+    typedef const __attribute__((address_space(3))) uint32_t *lds_word;
+    constexpr int SCALES_AT = fast_ring_bytes<DT, MODE>();
+    auto scale_load = [&](int s) __attribute__((always_inline)) {
+        if constexpr (MX4) {
+            const lds_ptr dst = lds + (SCALES_AT + (s & 1) * FAST_SCALES + wave * 256);
+            const int at = s < nslab ? s * 8 : 0x7FFFFFFF;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(sa_src, (lds_void)dst, 4, sa_off, at, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(sb_src, (lds_void)(dst + FAST_SCALES / 2), 4, sb_off, at, 0, 0);
+        }
+    };
+    auto scale_read = [&](auto h_c, int s) __attribute__((always_inline)) {
+        if constexpr (MX4) {
+            constexpr int h = decltype(h_c)::value;
+            const lds_ptr at = lds + (SCALES_AT + (s & 1) * FAST_SCALES + l32 * 8);
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi) sa[h][mi] = *(lds_word)(at + wm * TM * 8 + (mi * 32 * 8 + 4 * h));
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni) sb[h][ni] = *(lds_word)(at + wn * TN * 8 + (FAST_SCALES / 2 + ni * 32 * 8 + 4 * h));
+        }
+    };
+    // ahead of steps 0 and 2
+    auto scale_turn = [&](auto t_c) __attribute__((always_inline)) {
+        constexpr int t = decltype(t_c)::value, h = t >> 1;
+        if constexpr (MX4 && (t & 1) == 0) {
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi) sa[h][mi] >>= 8 * lh;
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni) sb[h][ni] >>= 8 * lh;
+        }
+    };
+    if constexpr (MX4) {
+        const auto rows = source.scale_rows(m0, n0);
+        // (rows past the end bring zeros)
+        sa_src = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(rows.a), 0, min(M - m0, BM) * rows.lda, RSRC_FLAGS);
+        sb_src = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(rows.b), 0, min(N - n0, 256) * rows.ldb, RSRC_FLAGS);
+        sa_off = (wave * 32 + (lane >> 1)) * rows.lda + 4 * (lane & 1);
+        sb_off = (wave * 32 + (lane >> 1)) * rows.ldb + 4 * (lane & 1);
+    }
     // ---- main loop, software-pipelined by hand.  A slab is four MFMA steps of 32 bytes of K.
     // The fragments of step t+1 are read from LDS while the MFMAs of step t run (two register
     // sets).  The barrier sits between steps 2 and 3: by then every wave has
@@ -198,11 +251,16 @@ __device__ __forceinline__ void fast_tile(const GemmArgs &g, SRC source, uint8_t
     // MFMA j of step t (set t & 1)
     auto mfma = [&](auto first_c, auto t_c, auto j_c) __attribute__((always_inline)) {
         constexpr int set = decltype(t_c)::value & 1, mi = decltype(j_c)::value / NI, ni = decltype(j_c)::value % NI;
-        acc[mi][ni] = T::mfma(fb[set][ni], fa[set][mi], decltype(first_c)::value ? zerov : acc[mi][ni]);
+        if constexpr (MX4) {
+            constexpr int t = decltype(t_c)::value;
+            acc[mi][ni] = mfma_mx4<2 * (t & 1)>(fb[set][ni], fa[set][mi], decltype(first_c)::value ? zerov : acc[mi][ni], sb[t >> 1][ni], sa[t >> 1][mi]);
+        } else {
+            acc[mi][ni] = T::mfma(fb[set][ni], fa[set][mi], decltype(first_c)::value ? zerov : acc[mi][ni]);
+        }
     };
     // Protected tiles reduce the slabs of A they own (slab s belongs to tile column s mod
     // tiles_n) while those are resident: see gemm_apass.h.
-    constexpr int AUX_OFF = fast_lds_bytes<MODE>();    // behind the buffers of the larger tile
+    constexpr int AUX_OFF = fast_lds_bytes<DT, MODE>();    // behind the buffers of the larger tile
     static_assert(epi_total_bytes(BM, 256) <= AUX_OFF, "the epilogue reads the column sums there while it fills the LDS ahead of them");
     EpiProt<DT, MI> ep;
     ep.slab0 = tn; ep.slab_step = g.tiles_n; ep.owned = (OWN && tn < nslab) ? (nslab - tn + g.tiles_n - 1) / g.tiles_n : 0;
@@ -237,11 +295,14 @@ __device__ __forceinline__ void fast_tile(const GemmArgs &g, SRC source, uint8_t
             f0 = f1; f1 = f2; f2 = f;
             r0 = r1; r1 = r;
         };
+        scale_load(0);
         static_for<0, NLD>([&](auto q_c) { load(q_c, 0, Buf{f0, r0}); });
+        scale_load(1);
         static_for<0, NLD>([&](auto q_c) { load(q_c, 1, Buf{f1, r1}); });
         // Start as soon as slab 0 is in place: loads complete in order, so "at most the loads of the
         // slab behind it outstanding" means everything issued before them has landed.
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(NLD) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(NLD + SCALE_LOADS) : "memory");
+        scale_read(std::integral_constant<int, 0>{}, 0);
         static_for<0, NFR>([&](auto j_c) { fragment(j_c, std::integral_constant<int, 0>{}, Buf{f0, r0}); });
         if constexpr (AT || BT) turned(std::integral_constant<int, 0>{}, Buf{f0, r0});
         // The barrier of slab s: slab s + 1 is in place; what was requested after it are the units with three buffers of
@@ -337,6 +398,12 @@ __device__ __forceinline__ void fast_tile(const GemmArgs &g, SRC source, uint8_t
                 constexpr int at = t == 3 ? 0 : t + 1;
                 constexpr int q0 = FIRST && t < 3 ? NR + NF * t / 3 : L::by_step(at), q1 = FIRST && t < 3 ? NR + NF * (t + 1) / 3 : L::by_step(at + 1);
                 constexpr int RPM = NMF >= NFR ? 1 : 2;                // fragment reads behind an MFMA
+                scale_turn(t_c);
+                if constexpr (t == 0) scale_read(std::integral_constant<int, 1>{}, s);
+                if constexpr (t == 3) {
+                    scale_load(s + 2);
+                    scale_read(std::integral_constant<int, 0>{}, s + 1);
+                }
                 __builtin_amdgcn_sched_barrier(0);
                 static_for<0, NMF>([&](auto j_c) {
                     constexpr int j = decltype(j_c)::value;
@@ -401,8 +468,14 @@ __device__ __forceinline__ void fast_tile(const GemmArgs &g, SRC source, uint8_t
                 ++s;
             }
         }
-        for (; s < mid_end; ++s) slab(std::false_type{}, s);
-        for (; s < nslab; ++s) tail_slab(s);
+        if constexpr (MX4) {
+            // All alike: a branch around loads lets the compiler move MFMAs with scales, which it does not hold to their block, behind it, and a slab's fragments with them.
+            for (; s < nslab; ++s) slab(std::false_type{}, s);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        } else {
+            for (; s < mid_end; ++s) slab(std::false_type{}, s);
+            for (; s < nslab; ++s) tail_slab(s);
+        }
     }
     __syncthreads();
     gemm_epilogue<DT, OT, BM, PROT, STO>(g, source, acc, smem, m0, n0, bz, ep, sc);

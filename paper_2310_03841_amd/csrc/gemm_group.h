@@ -159,8 +159,10 @@ __global__ __launch_bounds__(256) void gemm_group_kernel(typename GroupArgsOf<DT
         if (blockIdx.x == 0 && tid < 5) g.counts[tid] = 0u;
         if ((int)blockIdx.x < g.n_pass) {
             GroupTile t;
-            if (find_tile<4 * PASS_ROWS>(g, g.pass_win, g.pass_inv, (int)blockIdx.x, &t)) {
-                if constexpr (MX4) mx4_pass<4>(g, t.e, t.first, t.rows, t.tm * 4 * PASS_ROWS, t.tn, smem);
+            int log2 = 0;
+            if constexpr (MX4) log2 = g.pass_log2;
+            if (find_tile<4 * PASS_ROWS>(g, g.pass_win, g.pass_inv, (int)blockIdx.x, &t, log2)) {
+                if constexpr (MX4) mx4_pass<4>(g, t.e, t.first, t.rows, t.tm * 4 * PASS_ROWS << log2, log2, t.tn, smem);
                 else group_pass<DT, 4>(g, t.e, t.first, t.rows, t.tm * 4 * PASS_ROWS, t.tn, smem);
             }
             return;
@@ -308,7 +310,7 @@ __global__ __launch_bounds__(256) void gemm_group_kernel(typename GroupArgsOf<DT
             else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
             if (s + NS - 1 < nslab) issue(s + NS - 1);
         };
-        static_assert(NS == 3 || NS == 4, "what arrive() tells apart");
+        static_assert(NS >= 2 && NS <= 4, "what arrive() tells apart");
         const bool ragged = K % KE != 0;
         arrive(0);
         read(0, set0{});
@@ -478,7 +480,7 @@ template <int DT, int OT, int BM, int BN, int NS, bool PROT, int GROUP, bool TRA
 static hipError_t launch_one(typename GroupArgsOf<DT>::type &g, hipStream_t st)
 {
     constexpr int smem = group_lds_bytes<DT>(BM, BN, NS, OT != DT);
-    static_assert(smem >= group_pass_lds<DT, 4>(), "the pass over A runs in the LDS of a tile");
+    static_assert(smem >= (DT == DT_MX4 ? mx4_pass_lds<4>() : group_pass_lds<DT, 4>()), "the pass over A runs in the LDS of a tile");
     auto kern = gemm_group_kernel<DT, OT, BM, BN, NS, PROT, GROUP, TRANSB>;
     hipError_t e = ensure_max_lds(reinterpret_cast<const void *>(kern), smem);
     if (e != hipSuccess) return e;

@@ -11,6 +11,7 @@
 #include "gemm_fast_tile.h"
 #include "group_args.h"
 #include "group_passes.h"
+#include "mx4_pass.h"
 
 namespace abft {
 
@@ -56,6 +57,19 @@ template <int OT, int GROUP> struct GroupSource {
         return s;
     }
 };
+
+// Of 4-bit operands besides: the scales of a tile's rows of A and of B.
+template <int OT> struct Mx4Source : GroupSource<OT, BIG_ROWS> {
+    struct Rows { const uint8_t *a, *b; int lda, ldb; };
+    __device__ __forceinline__ Mx4Source(int e, int first, int rows) : GroupSource<OT, BIG_ROWS>{e, first, rows} {}
+    __device__ __forceinline__ Rows scale_rows(int m0, int n0) const
+    {
+        const Mx4Args &a = kernel_args<Mx4Args>();
+        return {a.sa + (long)(this->first + m0) * a.ld_sa, a.sb + (long)this->e * a.stride_sb + (long)n0 * a.ld_sb, (int)a.ld_sa, (int)a.ld_sb};
+    }
+};
+template <int DT, int OT, int GROUP> struct BigSource { typedef GroupSource<OT, GROUP> type; };
+template <int OT> struct BigSource<DT_MX4, OT, BIG_ROWS> { typedef Mx4Source<OT> type; };
 
 struct BigTile { int e, first, rows, m0, tn; bool tall; };
 
@@ -153,12 +167,12 @@ template <int GROUP, bool PROT> __device__ __forceinline__ bool big_tile(const G
 }
 
 template <int DT, int OT, bool PROT, int GROUP, bool BT>
-__global__ __launch_bounds__(64 * FAST_WAVES) void gemm_group_big_kernel(GroupArgs)
+__global__ __launch_bounds__(64 * FAST_WAVES) void gemm_group_big_kernel(typename GroupArgsOf<DT>::type)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     constexpr bool DEPTH = GROUP == BIG_DEPTH;
     constexpr int MODE = PROT ? FAST_BESIDE : FAST_PLAIN, ES = Traits<DT>::ES;
-    fetch_args<GroupArgs>();
+    fetch_args<typename GroupArgsOf<DT>::type>();
     GroupLane kept = {0, 0};
     int rank = 0;
     if constexpr (!DEPTH) kept = group_lane(kernel_args<GroupArgs>(), threadIdx.x & 63);
@@ -178,16 +192,17 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void gemm_group_big_kernel(GroupAr
         g.N = a.N;
         g.K = DEPTH ? b.rows : a.K;
         g.lda = a.lda; g.ldb = a.ldb;
-        const GroupSource<OT, GROUP> source = {b.e, b.first, b.rows};
+        const typename BigSource<DT, OT, GROUP>::type source{b.e, b.first, b.rows};
         if (b.tall) fast_tile<DT, OT, 256, MODE, STO_NO, DEPTH, BT>(g, source, smem, b.m0, b.tn * 256, 0, b.tn);
         else fast_tile<DT, OT, 128, MODE, STO_NO, DEPTH, BT>(g, source, smem, b.m0, b.tn * 256, 0, b.tn);
     }
     if constexpr (PROT) {
-        constexpr int ROWS = FAST_WAVES * PASS_ROWS;
         const GroupArgs &a = kernel_args<GroupArgs>();
-        int passes = 0;
+        int rows_log2 = __builtin_ctz(FAST_WAVES * PASS_ROWS), passes = 0;
+        if constexpr (DT == DT_MX4) rows_log2 += max(kernel_args<Mx4Args>().pass_log2 - 1, 0);       // (of items of four waves)
+        const int ROWS = 1 << rows_log2;
         GroupLane mine = kept;
-        auto passes_of = [&](int rows) __attribute__((always_inline)) { return (rows + ROWS - 1) / ROWS * a.pass_win; };
+        auto passes_of = [&](int rows) __attribute__((always_inline)) { return ((rows + ROWS - 1) >> rows_log2) * a.pass_win; };
         for (int e0 = 0; e0 < a.groups; e0 += 64) {
             if (a.groups > 64) mine = group_lane(a, e0 + (threadIdx.x & 63));
             passes += wave_sum(passes_of(mine.rows));
@@ -201,17 +216,18 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void gemm_group_big_kernel(GroupAr
             if (!find_group(a, kept, passes_of, &L, &b.e, &b.first, &b.rows)) break;
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             const int row = L / a.pass_win;
-            group_pass<DT, FAST_WAVES>(a, b.e, b.first, b.rows, row * ROWS, L - row * a.pass_win, smem);
+            if constexpr (DT == DT_MX4) mx4_pass<FAST_WAVES>(kernel_args<Mx4Args>(), b.e, b.first, b.rows, row * ROWS, rows_log2 - __builtin_ctz(FAST_WAVES * PASS_ROWS), L - row * a.pass_win, smem);
+            else group_pass<DT, FAST_WAVES>(a, b.e, b.first, b.rows, row * ROWS, L - row * a.pass_win, smem);
         }
     }
 }
 
-template <int DT, int OT, bool PROT, int GROUP, bool BT> static hipError_t launch_big_one(GroupArgs &g, hipStream_t st)
+template <int DT, int OT, bool PROT, int GROUP, bool BT> static hipError_t launch_big_one(typename GroupArgsOf<DT>::type &g, hipStream_t st)
 {
     hipError_t e;
     const int cus = device_cu_count(&e);
     if (e != hipSuccess) return e;
-    constexpr int smem = fast_lds_bytes<PROT ? FAST_BESIDE : FAST_PLAIN>();
+    constexpr int smem = fast_lds_bytes<DT, PROT ? FAST_BESIDE : FAST_PLAIN>();
     auto kern = gemm_group_big_kernel<DT, OT, PROT, GROUP, BT>;
     e = ensure_max_lds(reinterpret_cast<const void *>(kern), smem);
     if (e != hipSuccess) return e;

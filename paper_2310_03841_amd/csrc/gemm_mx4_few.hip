@@ -16,8 +16,6 @@
 
 namespace abft {
 
-constexpr int MX4_FEW_PAIRS = 4;            // pieces of 128 bytes of a row that a wave has on their way
-
 struct Mx4FewArgs {
     Mx4Args g;
     const uint32_t *b_max;
@@ -28,9 +26,10 @@ struct Mx4FewArgs {
 
 template <int NB> constexpr int mx4_few_part_bytes() { return 4 * NB * 64 * 16 + 4 * NB * 16 * 4 + 16; }
 
-template <int OT, bool PROT, int NB> __global__ __launch_bounds__(256) void gemm_mx4_few_kernel(Mx4FewArgs f)
+// U: pieces of 128 bytes of a row that a wave has on their way
+template <int OT, bool PROT, int NB, int U> __global__ __launch_bounds__(256) void gemm_mx4_few_kernel(Mx4FewArgs f)
 {
-    constexpr int BN = 16 * NB, U = MX4_FEW_PAIRS;
+    constexpr int BN = 16 * NB;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     fetch_args<Mx4FewArgs>();
     const Mx4Args &g = f.g;
@@ -40,8 +39,8 @@ template <int OT, bool PROT, int NB> __global__ __launch_bounds__(256) void gemm
         if (blockIdx.x == 0 && tid < 5) g.counts[tid] = 0u;
         if ((int)blockIdx.x < g.n_pass) {
             GroupTile t;
-            if (find_tile<4 * PASS_ROWS>(g, g.pass_win, g.pass_inv, (int)blockIdx.x, &t))
-                mx4_pass<4, false>(g, t.e, t.first, t.rows, t.tm * 4 * PASS_ROWS, t.tn, smem);
+            if (find_tile<4 * PASS_ROWS>(g, g.pass_win, g.pass_inv, (int)blockIdx.x, &t, g.pass_log2))
+                mx4_pass<4, false>(g, t.e, t.first, t.rows, t.tm * 4 * PASS_ROWS << g.pass_log2, g.pass_log2, t.tn, smem);
             return;
         }
     }
@@ -94,20 +93,23 @@ template <int OT, bool PROT, int NB> __global__ __launch_bounds__(256) void gemm
         float top = 0.f;
         for (int i = tid; i < nch * 8; i += 256) {
             const int c = i >> 3, w = (i & 7) >> 1, half = i & 1;
-            uint32_t x[16], s[16];
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                x[r] = *reinterpret_cast<const uint32_t *>(At + (long)min(r, rows - 1) * g.lda + c * 16 + 4 * w);
-                s[r] = St[(long)min(r, rows - 1) * g.ld_sa + c];
-            }
             f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+            for (int r0 = 0; r0 < rows; r0 += 4) {
+                uint32_t x[4], s[4];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const uint32_t v = half ? x[r] >> 16 : x[r];
-                const f32x2 p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, mx4_unit(s[r]), 0), q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, mx4_unit(s[r]), 1);
-                if (r < rows) {
-                    sum += f32x4{p[0], p[1], q[0], q[1]};
-                    top = fmaxf(fmaxf(fmaxf(top, fabsf(p[0])), fmaxf(fabsf(p[1]), fabsf(q[0]))), fabsf(q[1]));
+                for (int j = 0; j < 4; ++j) {
+                    const long r = min(r0 + j, rows - 1);
+                    x[j] = *reinterpret_cast<const uint32_t *>(At + r * g.lda + c * 16 + 4 * w);
+                    s[j] = St[r * g.ld_sa + c];
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t v = half ? x[j] >> 16 : x[j];
+                    const f32x2 p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, mx4_unit(s[j]), 0), q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, mx4_unit(s[j]), 1);
+                    if (r0 + j < rows) {
+                        sum += f32x4{p[0], p[1], q[0], q[1]};
+                        top = fmaxf(fmaxf(fmaxf(top, fabsf(p[0])), fmaxf(fabsf(p[1]), fabsf(q[0]))), fabsf(q[1]));
+                    }
                 }
             }
             *reinterpret_cast<f32x4 *>(sums + 4 * i) = sum;
@@ -229,13 +231,13 @@ long mx4_few_workgroups(const Mx4Args &g)
     return ((g.groups == 1 ? (g.M + 15) / 16 : g.M / 16 + std::min(g.M, g.groups)) * (long)((g.N + bn - 1) / bn) + 7) / 8 * 8;
 }
 
-template <int OT, bool PROT, int NB> static hipError_t launch_few_one(Mx4FewArgs &f, hipStream_t st)
+template <int OT, bool PROT, int NB, int U> static hipError_t launch_few_of(Mx4FewArgs &f, hipStream_t st)
 {
     Mx4Args &g = f.g;
-    auto kern = gemm_mx4_few_kernel<OT, PROT, NB>;
+    auto kern = gemm_mx4_few_kernel<OT, PROT, NB, U>;
     f.sums_off = (mx4_few_part_bytes<NB>() + 15) & ~15;
     int smem = f.sums_off;
-    if (PROT) smem = std::max(smem + g.K * 8, group_pass_lds<DT_MX4, 4>());
+    if (PROT) smem = std::max(smem + g.K * 8, mx4_pass_lds<4, false>());
     const hipError_t e = ensure_max_lds(reinterpret_cast<const void *>(kern), MX4_FEW_MAX_SUMS + 32 * 1024);
     if (e != hipSuccess) return e;
     g.tiles_n = (g.N + 16 * NB - 1) / (16 * NB);
@@ -243,6 +245,13 @@ template <int OT, bool PROT, int NB> static hipError_t launch_few_one(Mx4FewArgs
     const long wgs = (PROT ? g.n_pass : 0) + mx4_few_workgroups(g);
     hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), smem, st, f);
     return hipGetLastError();
+}
+
+// Registers for no more pieces than a wave has: with few, more waves share a SIMD, and they have more on their way together.
+template <int OT, bool PROT, int NB> static hipError_t launch_few_one(Mx4FewArgs &f, hipStream_t st)
+{
+    const int pieces = (f.g.K + 4 * SLAB_BYTES - 1) / (4 * SLAB_BYTES);      // of a wave
+    return pieces <= 1 ? launch_few_of<OT, PROT, NB, 1>(f, st) : pieces <= 2 ? launch_few_of<OT, PROT, NB, 2>(f, st) : launch_few_of<OT, PROT, NB, 4>(f, st);
 }
 
 template <int OT> static hipError_t launch_few_type(bool protect, Mx4FewArgs &f, hipStream_t st)

@@ -34,6 +34,7 @@ struct GroupArgs {
 struct Mx4Args : GroupArgs {
     const uint8_t *sa, *sb;               // powers of two of the blocks, with a bias of 127: rows of A, of B
     long ld_sa, ld_sb, stride_sb;         // bytes
+    int pass_log2;                        // rows to an item of the pass over A: 2^pass_log2 times those of one trip
 };
 template <int DT> struct GroupArgsOf { typedef GroupArgs type; };
 template <> struct GroupArgsOf<DT_MX4> { typedef Mx4Args type; };
@@ -114,10 +115,14 @@ struct GroupTile { int e, tm, tn, first, rows; };
 // The tile of workgroup `bid` of those that take tiles, of BM rows each: false, there is none for it.  Every wave finds it by itself, 64 groups at
 // a time.  Consecutive tiles of an XCD are a group's, in the order of map_tile, so what shares rows of A or B meets in one L2.
 // tiles_n, inv: tiles along the other direction, map_inverse of them.
-template <int BM> __device__ __forceinline__ bool find_tile(const GroupArgs &g, int tiles_n, uint32_t inv, int bid, GroupTile *t)
+// BM: a power of two, times 2^log2.
+template <int BM> __device__ __forceinline__ bool find_tile(const GroupArgs &g, int tiles_n, uint32_t inv, int bid, GroupTile *t, int log2 = 0)
 {
+    static_assert((BM & (BM - 1)) == 0, "shifts for quotients");
     const int lane = threadIdx.x & 63;
-    auto tiles_of = [&](int rows) __attribute__((always_inline)) { return (rows + BM - 1) / BM * tiles_n; };
+    const int shift = __builtin_ctz(BM) + log2;
+    auto rows_of = [&](int rows) __attribute__((always_inline)) { return (int)(((uint32_t)rows + (1u << shift) - 1u) >> shift); };
+    auto tiles_of = [&](int rows) __attribute__((always_inline)) { return rows_of(rows) * tiles_n; };
     GroupLane mine = {0, 0};
     int total = 0;
     if (g.groups == 1) {
@@ -135,7 +140,7 @@ template <int BM> __device__ __forceinline__ bool find_tile(const GroupArgs &g, 
     if (i >= q + (xcd < r ? 1 : 0)) return false;                // more workgroups than tiles
     int L = xcd * q + (xcd < r ? xcd : r) + i;
     if (g.groups > 1 && !find_group(g, mine, tiles_of, &L, &t->e, &t->first, &t->rows)) return false;
-    tile_at(L, (t->rows + BM - 1) / BM, tiles_n, inv, &t->tm, &t->tn);
+    tile_at(L, rows_of(t->rows), tiles_n, inv, &t->tm, &t->tn);
     return true;
 }
 

@@ -36,19 +36,20 @@ struct Mx4CheckArgs : GroupCheckArgs {
 template <int DT> struct GroupCheckArgsOf { typedef GroupCheckArgs type; };
 template <> struct GroupCheckArgsOf<DT_MX4> { typedef Mx4CheckArgs type; };
 
-// Dots of RW rows of 4-bit B with a vector of 2 K terms: a block to a lane, 64 at a time.
-template <int RW> __device__ __forceinline__ void mx4_row_dots(const uint8_t *X, long ld, const uint8_t *S, long lds, int row0, int rows, int K, const uint32_t *vec, float (&dot)[RW])
+// Dots of RW rows of 4-bit B with a vector of 2 K terms, the vector's 32 terms of a lane's block in registers.  LPR lanes to a row, as many as a row has blocks (or 64, and the
+// vector in pieces): 64 / LPR rows at a time, each one's loads ahead of the sums of the one before.  dot[j] belongs to row row0 + j * (64 / LPR) + lane / LPR.
+template <int RW, int LPR> __device__ __forceinline__ void mx4_row_dots(const uint8_t *X, long ld, const uint8_t *S, long lds, int row0, int rows, int K, const uint32_t *vec, float (&dot)[RW])
 {
-    const int lane = threadIdx.x & 63, nb = K / 16;
+    const int lane = threadIdx.x & 63, l = lane % LPR, nb = K / 16;
 #pragma unroll
     for (int j = 0; j < RW; ++j) dot[j] = 0.f;
-    for (int b0 = 0; b0 < nb; b0 += 64) {
-        const int at = min(b0 + lane, nb - 1);
+    for (int b0 = 0; b0 < nb; b0 += LPR) {
+        const int at = min(b0 + l, nb - 1);
         i32x4 v[RW];
         uint32_t s[RW];
 #pragma unroll
         for (int j = 0; j < RW; ++j) {
-            const long r = min(row0 + j, rows - 1);
+            const long r = min(row0 + j * (64 / LPR) + lane / LPR, rows - 1);
             v[j] = *reinterpret_cast<const i32x4 *>(X + r * ld + at * 16);
             s[j] = S[r * lds + at];
         }
@@ -57,20 +58,19 @@ template <int RW> __device__ __forceinline__ void mx4_row_dots(const uint8_t *X,
         for (int q4 = 0; q4 < 8; ++q4) {
             const i32x4_word w = *reinterpret_cast<const i32x4_word *>(vec + at * 32 + 4 * q4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) a[4 * q4 + i] = __uint_as_float((uint32_t)w[i]);
+            for (int i = 0; i < 4; ++i) a[4 * q4 + i] = b0 + l < nb ? __uint_as_float((uint32_t)w[i]) : 0.f;
         }
-        if (b0 + lane < nb) {
 #pragma unroll
-            for (int j = 0; j < RW; ++j) {
-                float x[32];
-                mx4_values(v[j], mx4_unit(s[j]), x);
+        for (int j = 0; j < RW; ++j) {
+            float x[32];
+            mx4_values(v[j], mx4_unit(s[j]), x);
 #pragma unroll
-                for (int q = 0; q < 32; ++q) dot[j] = __builtin_fmaf(x[q], a[q], dot[j]);
-            }
+            for (int q = 0; q < 32; ++q) dot[j] = __builtin_fmaf(x[q], a[q], dot[j]);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 #pragma unroll
-    for (int j = 0; j < RW; ++j) dot[j] = wave_sum(dot[j]);
+    for (int j = 0; j < RW; ++j) dot[j] = seg_sum(dot[j], LPR);
 }
 
 constexpr int GCHK_KN_LANES = 4;          // chunk columns of a unit over a B stored K x N (64 lanes run along k)
@@ -78,7 +78,8 @@ constexpr int GCHK_KN_LANES = 4;          // chunk columns of a unit over a B st
 // What is left to do of the columns: their predictions from B stored N x K or K x N, or nothing but to write down what the product's kernel marked.
 enum { COLS_NK, COLS_KN, COLS_MARKED };
 
-template <int DT, int RW, int COLS>
+// RW: rows of B to a wave (4 bits: to LPR lanes of one)
+template <int DT, int RW, int COLS, int LPR = 64>
 __global__ __launch_bounds__(256) void group_check_kernel(typename GroupCheckArgsOf<DT>::type f)
 {
     using T = Traits<DT>;
@@ -157,16 +158,17 @@ __global__ __launch_bounds__(256) void group_check_kernel(typename GroupCheckArg
     int n = 0;
     acc_t pred = T::zero();
     if constexpr (COLS == COLS_NK) {
-        const int row0 = (unit * 4 + wave) * RW;
-        n = row0 + lane;
-        mine_ok = lane < RW && n < N;
+        constexpr int ROWS = 64 / LPR;                           // side by side
+        const int row0 = (unit * 4 + wave) * RW * ROWS, l = lane % LPR;
+        n = row0 + l * ROWS + lane / LPR;
+        mine_ok = l < RW && n < N;
         // (a group without rows: nothing of its matrix is read)
         if (rows > 0 && row0 < N) {
             acc_t dot[RW];
-            if constexpr (MX4) mx4_row_dots<RW>(Bb, f.ldb, f.sb + (long)e * f.stride_sb, f.ld_sb, row0, N, K, asum, dot);
+            if constexpr (MX4) mx4_row_dots<RW, LPR>(Bb, f.ldb, f.sb + (long)e * f.stride_sb, f.ld_sb, row0, N, K, asum, dot);
             else row_dots<DT, RW>(Bb, f.ldb, row0, N, K, asum, false, dot);
 #pragma unroll
-            for (int j = 0; j < RW; ++j) pred = lane == j ? dot[j] : pred;
+            for (int j = 0; j < RW; ++j) pred = l == j ? dot[j] : pred;
         }
     } else {
         const int cx = tid % GCHK_KN_LANES, ky = tid / GCHK_KN_LANES;
@@ -268,15 +270,19 @@ hipError_t launch_group_check(int dt, const GroupKernel &k, const GroupArgs &g, 
 
 hipError_t launch_mx4_check(const GroupKernel &k, const Mx4Args &g, int K, const Workspace &w, const Verdict &v, const OneLaunch &end, hipStream_t st)
 {
-    constexpr int RW = GCHK_ROWS;
+    constexpr int RW = 8;
     Mx4CheckArgs f;
     check_args(f, g, (float)K, w, v, end);
     f.sb = g.sb; f.ld_sb = g.ld_sb; f.stride_sb = g.stride_sb;
     const bool marked = k.kind == GROUP_KERNEL_FEW;
-    const dim3 grid = check_grid(f, marked, 4 * RW);
+    const int blocks = g.K / 16, lpr = blocks <= 8 ? 8 : blocks <= 16 ? 16 : blocks <= 32 ? 32 : 64;
+    const dim3 grid = check_grid(f, marked, 4 * RW * (64 / lpr));
     // (marked: fp32 sums and nothing of the operands)
-    if (marked) hipLaunchKernelGGL((group_check_kernel<DT_BF16, RW, COLS_MARKED>), grid, dim3(256), 0, st, (const GroupCheckArgs &)f);
-    else        hipLaunchKernelGGL((group_check_kernel<DT_MX4, RW, COLS_NK>), grid, dim3(256), 0, st, f);
+    if (marked)         hipLaunchKernelGGL((group_check_kernel<DT_BF16, GCHK_ROWS, COLS_MARKED>), grid, dim3(256), 0, st, (const GroupCheckArgs &)f);
+    else if (lpr == 8)  hipLaunchKernelGGL((group_check_kernel<DT_MX4, RW, COLS_NK, 8>), grid, dim3(256), 0, st, f);
+    else if (lpr == 16) hipLaunchKernelGGL((group_check_kernel<DT_MX4, RW, COLS_NK, 16>), grid, dim3(256), 0, st, f);
+    else if (lpr == 32) hipLaunchKernelGGL((group_check_kernel<DT_MX4, RW, COLS_NK, 32>), grid, dim3(256), 0, st, f);
+    else                hipLaunchKernelGGL((group_check_kernel<DT_MX4, RW, COLS_NK, 64>), grid, dim3(256), 0, st, f);
     return hipGetLastError();
 }
 

@@ -14,7 +14,7 @@ constexpr int PASS_ROWS = 8;                 // rows of a wave
 constexpr int PASS_BYTES = 1024;             // of a row
 
 // LDS: each wave's sums of the window's columns, and a maximum to a wave
-template <int DT, int WAVES> constexpr int group_pass_lds() { return WAVES * PASS_BYTES / Traits<DT>::ES * (DT == DT_MX4 ? 2 : 1) * 4 + WAVES * 4; }
+template <int DT, int WAVES> constexpr int group_pass_lds() { return WAVES * PASS_BYTES / Traits<DT>::ES * 4 + WAVES * 4; }
 
 // Rows row0 .. of group e (which has `rows` from `first` on), WAVES * PASS_ROWS at most; window win.  SUMS: e^T A is wanted too.
 template <int DT, int WAVES, bool SUMS = true> __device__ __forceinline__ void group_pass(const GroupArgs &g, int e, int first, int rows, int row0, int win, uint8_t *smem)
