@@ -7,6 +7,7 @@
 #include "abft_device.h"
 #include "gemm_epilogue.h"
 #include "mx4_device.h"
+#include "route_args.h"
 
 namespace abft {
 
@@ -72,7 +73,7 @@ template <int DT, int LPR, int NC> __global__ __launch_bounds__(256) void mx4_qu
     constexpr int EXP = DT == DT_BF16 ? 7 : 10, TOP = DT == DT_BF16 ? 255 : 31;      // place of the exponent, that of Inf and NaN
     const int l = threadIdx.x % LPR;
     const int nq = (a.cols + 31) / 32 * 4, nch = (a.cols + 7) / 8;               // quarters of blocks, chunks of the row
-    const long r = (long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+    const long r = flat_block() * (256 / LPR) + threadIdx.x / LPR;
     const int t = r < a.rows ? source_row(a.order, a.tokens, a.topk, (int)r) : -1;
     if (t < 0) return;                                           // (all lanes of a row together)
     const uint8_t *src = a.X + t * a.ldx;
@@ -111,7 +112,7 @@ template <int DT, int LPR, int NC> __global__ __launch_bounds__(256) void mx4_de
 {
     fetch_args<Mx4RowArgs>();
     const int l = threadIdx.x % LPR, nch = (a.cols + 7) / 8;
-    const long r = (long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+    const long r = flat_block() * (256 / LPR) + threadIdx.x / LPR;
     if (r >= a.rows) return;
     const uint8_t *src = a.Q + r * a.ldq, *sc = a.S + r * a.lds;
     uint8_t *dst = const_cast<uint8_t *>(a.X) + r * a.ldx;
@@ -150,7 +151,7 @@ template <int DT> struct Quantize {
     template <int LPR, int NC> struct Launch {
         static hipError_t go(const Mx4RowArgs &a, hipStream_t st)
         {
-            hipLaunchKernelGGL((mx4_quantize_kernel<DT, LPR, NC>), dim3((unsigned)(((long)a.rows + 256 / LPR - 1) / (256 / LPR))), dim3(256), 0, st, a);
+            hipLaunchKernelGGL((mx4_quantize_kernel<DT, LPR, NC>), flat_grid(((long)a.rows + 256 / LPR - 1) / (256 / LPR)), dim3(256), 0, st, a);
             return hipGetLastError();
         }
     };
@@ -159,7 +160,7 @@ template <int DT> struct Dequantize {
     template <int LPR, int NC> struct Launch {
         static hipError_t go(const Mx4RowArgs &a, hipStream_t st)
         {
-            hipLaunchKernelGGL((mx4_dequantize_kernel<DT, LPR, NC>), dim3((unsigned)(((long)a.rows + 256 / LPR - 1) / (256 / LPR))), dim3(256), 0, st, a);
+            hipLaunchKernelGGL((mx4_dequantize_kernel<DT, LPR, NC>), flat_grid(((long)a.rows + 256 / LPR - 1) / (256 / LPR)), dim3(256), 0, st, a);
             return hipGetLastError();
         }
     };

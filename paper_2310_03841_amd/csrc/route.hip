@@ -3,6 +3,7 @@
 // A token is LPT lanes of a wave, EPL neighbouring experts to each.  The order of experts is that of score + bias (of the logits, where scores grow with them and
 // nothing is added), equal ones by index; a round takes the best that is left.
 #include "abft_device.h"
+#include "gemm_epilogue.h"
 #include "route_args.h"
 
 namespace abft {
@@ -47,6 +48,33 @@ template <int DT, int EPL> __device__ __forceinline__ void load_logits(const uin
     }
 }
 
+// And back, rounded once; nothing past the last.
+template <int DT, int EPL> __device__ __forceinline__ void store_logits(uint8_t *row, int e0, int E, const float (&v)[EPL])
+{
+    constexpr int ES = DT == DT_F32 ? 4 : 2, C = EPL * ES < 16 ? EPL : 16 / ES, W = C * ES / 4;
+#pragma unroll
+    for (int c = 0; c < EPL / C; ++c) {
+        const int e = e0 + c * C;
+        uint32_t w[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            if constexpr (DT == DT_F32) w[i] = __float_as_uint(v[c * C + i]);
+            else w[i] = pack2<DT>(v[c * C + 2 * i], v[c * C + 2 * i + 1]);
+        }
+        uint8_t *const at = row + (long)e * ES;
+        if (e + C <= E) {
+            if constexpr (W == 4) *reinterpret_cast<i32x4 *>(at) = i32x4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+            else if constexpr (W == 2) *reinterpret_cast<uint2 *>(at) = make_uint2(w[0], w[1]);
+            else *reinterpret_cast<uint32_t *>(at) = w[0];
+        } else {
+            for (int i = 0; i < C && e + i < E; ++i) {
+                if constexpr (DT == DT_F32) reinterpret_cast<uint32_t *>(at)[i] = w[i];
+                else reinterpret_cast<uint16_t *>(at)[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+            }
+        }
+    }
+}
+
 // ---------------------------------------------------------------- over the LPT lanes of a token
 template <int CTRL> __device__ __forceinline__ double dpp_get64(double v)
 {
@@ -60,6 +88,11 @@ template <int CTRL> __device__ __forceinline__ double other(double v) { return d
 template <int D> __device__ __forceinline__ float far_other(float v) { return __shfl_xor(v, D); }
 template <int D> __device__ __forceinline__ int far_other(int v) { return __shfl_xor(v, D); }
 template <int D> __device__ __forceinline__ double far_other(double v) { return __shfl_xor(v, D); }
+template <int CTRL> __device__ __forceinline__ long long other(long long v)
+{
+    return __builtin_bit_cast(long long, dpp_get64<CTRL>(__builtin_bit_cast(double, v)));
+}
+template <int D> __device__ __forceinline__ long long far_other(long long v) { return __shfl_xor(v, D); }
 template <int LPT, typename V, typename OP> __device__ __forceinline__ V over_token(V v, const OP &op)
 {
     v = op(v, other<0xB1>(v));     // lane ^ 1
@@ -82,80 +115,168 @@ __device__ __forceinline__ void wave_lds_fence()
     __builtin_amdgcn_wave_barrier();
 }
 
-// Places of the chosen experts: lane j of a token gets the j-th, -1 where none is left.  LDS, with groups: keys of a token's experts, then 64 values.
-template <int LPT, int EPL, bool GROUPED> __device__ __forceinline__ int choose(const RouteArgs &a, const float (&x)[EPL], double *lds, int l)
-{
-    const double none = -__builtin_inf();
-    const int E = a.experts, e0 = l * EPL;
-    double key[EPL];
-    if (a.by_logit) {
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) key[i] = x[i];
-    } else {
-        float top = -__builtin_inff();
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) top = fmaxf(top, x[i]);
-        top = over_token<LPT>(top, Larger{});
-        const double m = top > -__builtin_inff() ? top : 0.f;
-        double sum = 0;
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) {
-            key[i] = a.sigmoid ? 1.0 / (1.0 + exp(-(double)x[i])) : exp((double)x[i] - m);
-            sum += key[i];
-        }
-        sum = over_token<LPT>(sum, Plus{});
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) {
-            const double b = a.bias ? (double)a.bias[min(e0 + i, E - 1)] : 0.0, k = (a.sigmoid ? key[i] : key[i] / sum) + b;
-            key[i] = x[i] > -__builtin_inff() && k == k ? k : none;
-        }
+// ---------------------------------------------------------------- keys in the order they are chosen by
+// As integers: of fp32 (zeros of either sign alike), and of fp64.  NONE: behind all, -Inf too.
+template <typename KEY> struct Order;
+template <> struct Order<float> {
+    typedef int type;
+    static constexpr int NONE = -0x7FFFFFFF - 1;
+    __device__ static __forceinline__ int of(float k)
+    {
+        const int i = __float_as_int(k + 0.f);
+        return i ^ ((i >> 31) & 0x7FFFFFFF);
     }
+    __device__ static __forceinline__ float value(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7FFFFFFF)); }
+};
+template <> struct Order<double> {
+    typedef long long type;
+    static constexpr long long NONE = -0x7FFFFFFFFFFFFFFFll - 1;
+    __device__ static __forceinline__ long long of(double k)
+    {
+        const long long i = __double_as_longlong(k + 0.0);
+        return i ^ ((i >> 63) & 0x7FFFFFFFFFFFFFFFll);
+    }
+};
+
+// Scores, off by some 2^-20 at most where they are computed in fp32.
+template <typename KEY, int LPT, int EPL> __device__ __forceinline__ void scores(bool sigmoid, const float (&x)[EPL], float top, KEY (&s)[EPL])
+{
+    if (sigmoid) {
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) {
+            if constexpr (sizeof(KEY) == 8) s[i] = 1.0 / (1.0 + exp(-(double)x[i]));
+            else s[i] = __builtin_amdgcn_rcpf(1.f + __expf(-x[i]));
+        }
+        return;
+    }
+    const float m = top > -__builtin_inff() ? top : 0.f;
+    KEY sum = 0;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+        if constexpr (sizeof(KEY) == 8) s[i] = exp((double)x[i] - (double)m);
+        else s[i] = __expf(x[i] - m);
+        sum += s[i];
+    }
+    sum = over_token<LPT>(sum, Plus{});
+    if constexpr (sizeof(KEY) == 8) {
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) s[i] /= sum;
+    } else {
+        const float inv = __builtin_amdgcn_rcpf(sum);
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) s[i] *= inv;
+    }
+}
+
+// What a token's lanes share in LDS: keys of its experts and values of its groups, and the choices.
+template <int LPT, int EPL, bool GROUPED> struct RouteLds {
+    double keys[GROUPED ? LPT * EPL : 1], values[GROUPED ? ROUTE_MAX_GROUPS : 1];
+    int chosen[LPT + 1];
+};
+
+// The experts of a token: lane j gets the j-th, -1 where none is left.  False in fp32: keys are so near each other that fp32 may have their order, or what is chosen, wrong; 64 bits then
+// tell (some 1 of 300 tokens with random biases).  Told apart are neighbours among the chosen and the first that is not, and the last group that stays and the first that
+// does not.  Keys of fp32 logits are exact.
+template <typename KEY, int LPT, int EPL, bool GROUPED>
+__device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL], float top, RouteLds<LPT, EPL, GROUPED> &lds, int l, int *mine)
+{
+    typedef Order<KEY> O;
+    typedef typename O::type order_t;
+    constexpr bool ROUNDED = sizeof(KEY) == 4;
+    const int E = a.experts, e0 = l * EPL;
+    const float inf = __builtin_inff();
+    order_t key[EPL];
+    KEY s[EPL];
+    bool sure = true;
+    const bool scored = !a.by_logit;
+    if (scored) {
+        scores<KEY, LPT, EPL>(a.sigmoid, x, top, s);
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) {
+            const KEY k = a.bias ? s[i] + (KEY)a.bias[min(e0 + i, E - 1)] : s[i];
+            s[i] = x[i] > -inf && k > -(KEY)inf ? k : -(KEY)inf;             // (a NaN too)
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) s[i] = (KEY)x[i];
+    }
+    // without a bias logits are in the order of the scores
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) key[i] = s[i] > -(KEY)inf ? O::of(a.bias ? s[i] : (KEY)x[i]) : O::NONE;
     if constexpr (GROUPED) {
         const int G = a.groups, per = E / G;
-        double *const keys = lds, *const values = lds + LPT * EPL;
+        KEY *const keys = reinterpret_cast<KEY *>(lds.keys), *const values = reinterpret_cast<KEY *>(lds.values);
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) keys[e0 + i] = key[i];
+        for (int i = 0; i < EPL; ++i) keys[e0 + i] = s[i];
         wave_lds_fence();
         for (int g = l; g < G; g += LPT) {
-            double b0 = none, b1 = none;
+            KEY b0 = -(KEY)inf, b1 = -(KEY)inf;
             for (int i = 0; i < per; ++i) {
-                const double k = keys[g * per + i];
+                const KEY k = keys[g * per + i];
                 b1 = k > b0 ? b0 : k > b1 ? k : b1;
                 b0 = k > b0 ? k : b0;
             }
-            values[g] = a.group_best == 2 && b1 > none ? b0 + b1 : b0;
+            values[g] = a.group_best == 2 && b1 > -(KEY)inf ? b0 + b1 : b0;
         }
         wave_lds_fence();
         uint64_t stay = 0;
+        KEY in_min = (KEY)inf, out_max = -(KEY)inf;
         for (int g0 = 0; g0 < G; g0 += LPT) {
             const int g = g0 + l;
             int rank = 0;
-            const double v = values[min(g, G - 1)];
+            const KEY v = values[min(g, G - 1)];
             for (int h = 0; h < G; ++h) {
-                const double w = values[h];
+                const KEY w = values[h];
                 rank += w > v || (w == v && h < g) ? 1 : 0;
             }
-            const uint64_t in = __ballot(g < G && rank < a.top_groups) >> ((threadIdx.x & 63) & ~(LPT - 1));
-            stay |= (LPT == 64 ? in : in & ((1ull << (LPT & 63)) - 1)) << g0;
+            const bool in = g < G && rank < a.top_groups;
+            if (in && v < in_min) in_min = v;
+            if (g < G && !in && v > out_max) out_max = v;
+            const uint64_t b = __ballot(in) >> ((threadIdx.x & 63) & ~(LPT - 1));
+            stay |= (LPT == 64 ? b : b & ((1ull << (LPT & 63)) - 1)) << g0;
+        }
+        if (ROUNDED && scored) {
+            in_min = over_token<LPT>(in_min, Smaller{});
+            out_max = over_token<LPT>(out_max, Larger{});
+            // (groups without an expert are the last in any arithmetic)
+            sure = out_max == -(KEY)inf || in_min - out_max > (KEY)0x1p-17f * (1 + fabsf((float)out_max));
         }
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) key[i] = stay >> (min(e0 + i, E - 1) / per) & 1 ? key[i] : none;
+        for (int i = 0; i < EPL; ++i) key[i] = stay >> (min(e0 + i, E - 1) / per) & 1 ? key[i] : O::NONE;
     }
-    int mine = -1;
-    for (int j = 0; j < a.topk; ++j) {
-        double best = none;
+    // rounds: the best that is left, of equal ones that of the first lane, there the first.  Its lane writes it down.
+    const bool check = ROUNDED && a.bias != nullptr;                         // then one round more, for the first that is not chosen
+    const int base = (threadIdx.x & 63) & ~(LPT - 1);
+    float my_key = 0.f;
+    for (int j = 0; j < a.topk + (check ? 1 : 0); ++j) {
+        order_t best = O::NONE;
 #pragma unroll
         for (int i = 0; i < EPL; ++i) best = key[i] > best ? key[i] : best;
+        const order_t own = best;
         best = over_token<LPT>(best, Larger{});
-        int at = 1 << 30;
+        const uint64_t who = __ballot(own == best) >> base;                  // (of the token's lanes, and others above them)
+        const bool owner = l == (int)__builtin_ctzll(who);
+        int slot = EPL;
 #pragma unroll
-        for (int i = EPL - 1; i >= 0; --i) at = key[i] == best ? e0 + i : at;
-        at = over_token<LPT>(at, Smaller{});
+        for (int i = EPL - 1; i >= 0; --i) slot = key[i] == best ? i : slot;
+        slot = owner ? slot : EPL;
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) key[i] = e0 + i == at ? none : key[i];
-        if (l == j) mine = best > none ? at : -1;
+        for (int i = 0; i < EPL; ++i) key[i] = slot == i ? O::NONE : key[i];
+        if (owner) lds.chosen[j] = best != O::NONE ? e0 + slot : -1;
+        if constexpr (ROUNDED) my_key = l == j ? O::value(best) : my_key;
     }
-    return mine;
+    wave_lds_fence();
+    *mine = l < a.topk ? lds.chosen[l] : -1;
+    if constexpr (ROUNDED) {
+        if (check) {
+            const int e = l <= a.topk ? lds.chosen[l] : -1, next = l < a.topk ? lds.chosen[l + 1] : -1;
+            const float next_key = __shfl_down(my_key, 1);
+            (void)e;
+            if (next >= 0 && !(my_key - next_key > 0x1p-18f * (1.f + fabsf(my_key)))) sure = false;
+        }
+        return over_token<LPT>((int)sure, Smaller{}) != 0;
+    }
+    return true;
 }
 
 // What the weights of chosen logits are in proportion to, m the largest of them: exp(x - m), or the sigmoid times a power of e that keeps the largest away from
@@ -169,7 +290,7 @@ __device__ __forceinline__ float chosen_share(bool sigmoid, float x, float m)
 template <int DT, int LPT, int EPL, bool GROUPED> __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
 {
     constexpr int TOKENS = 256 / LPT;
-    __shared__ double lds[GROUPED ? TOKENS * (LPT * EPL + 64) : 1];
+    __shared__ RouteLds<LPT, EPL, GROUPED> lds[TOKENS];
     fetch_args<RouteArgs>();
     const int l = threadIdx.x % LPT, slot = threadIdx.x / LPT;
     const long t = (long)blockIdx.x * TOKENS + slot;
@@ -185,7 +306,11 @@ template <int DT, int LPT, int EPL, bool GROUPED> __global__ __launch_bounds__(2
         top = fmaxf(top, x[i]);
     }
     bad = over_token<LPT>((int)bad, Larger{}) != 0;
-    const int e = choose<LPT, EPL, GROUPED>(a, x, lds + (GROUPED ? slot * (LPT * EPL + 64) : 0), l);
+    top = over_token<LPT>(top, Larger{});
+    int e;
+    // (a token without scores is not worth the second look)
+    const bool sure = choose<float, LPT, EPL, GROUPED>(a, x, top, lds[slot], l, &e) || bad;
+    if (__builtin_expect(__any(!sure), 0)) choose<double, LPT, EPL, GROUPED>(a, x, top, lds[slot], l, &e);
     const bool there = l < a.topk && e >= 0;
     const float xe = there ? logit_at<DT>(row, e) : none;
     float w;
@@ -196,7 +321,6 @@ template <int DT, int LPT, int EPL, bool GROUPED> __global__ __launch_bounds__(2
     } else if (a.sigmoid) {
         w = 1.f / (1.f + expf(-xe));
     } else {
-        top = over_token<LPT>(top, Larger{});
         const float m = top > none ? top : 0.f;
         float sum = 0.f;
 #pragma unroll
@@ -266,16 +390,14 @@ template <int DT, int LPT, int EPL> __global__ __launch_bounds__(256) void route
     wave_lds_fence();
     const float D = spread ? over_token<LPT>(there ? dw * expf(xe - m) / sum : 0.f, Plus{}) : 0.f;
     if (t >= a.tokens) return;
-    uint8_t *out = a.dlogits + t * a.ldd;
+    float v[EPL];
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
-        if (e0 + i >= a.experts) break;
-        float v = g[e0 + i];
-        if (spread) v = expf(x[i] - m) / sum * (v - D);
-        if (bad) v = __builtin_nanf("");
-        if constexpr (DT == DT_F32) reinterpret_cast<float *>(out)[e0 + i] = v;
-        else reinterpret_cast<uint16_t *>(out)[e0 + i] = (uint16_t)(DT == DT_BF16 ? f32_to_bf16_bits(v) : f32_to_f16_bits(v));
+        v[i] = g[e0 + i];
+        if (spread) v[i] = expf(x[i] - m) / sum * (v[i] - D);
+        if (bad) v[i] = __builtin_nanf("");
     }
+    store_logits<DT, EPL>(a.dlogits + t * a.ldd, e0, a.experts, v);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -290,7 +412,7 @@ template <int DT, int LPT, int EPL> static hipError_t launch_one(bool grad, cons
 template <int DT> static hipError_t launch_type(bool grad, const RouteArgs &a, hipStream_t st)
 {
     // sixteen lanes to a token where they do: four tokens then share a wave's instructions
-    if (a.experts <= 256 && a.topk <= 16) {
+    if (a.experts <= 256 && a.topk < 16) {
         if (a.experts <= 32)  return launch_one<DT, 16, 2>(grad, a, st);
         if (a.experts <= 64)  return launch_one<DT, 16, 4>(grad, a, st);
         if (a.experts <= 128) return launch_one<DT, 16, 8>(grad, a, st);

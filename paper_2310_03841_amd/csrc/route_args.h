@@ -5,6 +5,14 @@
 
 namespace abft {
 
+// Workgroups in a row, dealt out over two directions of a launch where one has not that many (MAX_GRID_X); a few more than asked for.
+inline dim3 flat_grid(long wgs)
+{
+    constexpr long X = 1L << 22;
+    return wgs <= X ? dim3((unsigned)wgs) : dim3((unsigned)X, (unsigned)((wgs + X - 1) / X));
+}
+__device__ __forceinline__ long flat_block() { return (long)blockIdx.y * gridDim.x + blockIdx.x; }
+
 constexpr int ROUTE_MAX_EXPERTS = 1024, ROUTE_MAX_TOPK = 64, ROUTE_MAX_GROUPS = 64;
 
 struct RouteArgs {

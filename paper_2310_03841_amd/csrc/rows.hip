@@ -7,10 +7,12 @@
 namespace abft {
 
 // ---------------------------------------------------------------- entries by group
-// A stable counting sort.  A workgroup has SEG entries, a wave 256 of them; a lane's rank among the equal ones of its wave comes from ballots over the bits of
+// A stable counting sort.  A wave takes 64 entries at a time; a lane's rank among the equal ones of its wave comes from ballots over the bits of
 // the group's number, so that nothing is counted with atomics and the order is the entries' own.  Of more entries than one workgroup's, a first kernel counts
 // each workgroup's groups, and every workgroup adds up those ahead of it.
-constexpr int ROWS_WAVES = 16, ROWS_TRIPS = 4, ROWS_SEG = ROWS_WAVES * 64 * ROWS_TRIPS;
+// Bound by latency: one workgroup for a call's few entries, of no more waves than they and the groups need (64 entries, 32 groups: sixteen waves 4.1 us, one 2.2).  50432 entries, 64 groups:
+// 4096 of them to a workgroup and one thread to a group's counts in all workgroups 4.6 + 6.2 us; 1024, and the threads sharing out the counts, 3.4 + 4.8.
+constexpr int ROWS_MOST = 1024;                              // threads
 
 struct GroupRowsArgs {
     const int *group;
@@ -31,18 +33,20 @@ __device__ __forceinline__ uint64_t same_group(int e, bool in, int bits)
     return m;
 }
 
-// cnt: [ROWS_WAVES][groups], zero.  Each trip's group and its rank in the wave.
-__device__ __forceinline__ void count_groups(const GroupRowsArgs &a, int *cnt, int (&e)[ROWS_TRIPS], int (&rank)[ROWS_TRIPS])
+// cnt: [waves][groups], zero.  Each trip's group and its rank in the wave.
+template <int TRIPS> __device__ __forceinline__ void count_groups(const GroupRowsArgs &a, int *cnt, int (&e)[TRIPS], int (&rank)[TRIPS])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long i0 = (long)blockIdx.x * ROWS_SEG + wave * 64 * ROWS_TRIPS + lane;
+    const long i0 = (long)blockIdx.x * (blockDim.x * TRIPS) + wave * 64 * TRIPS + lane;
 #pragma unroll
-    for (int j = 0; j < ROWS_TRIPS; ++j) e[j] = i0 + 64 * j < a.n ? a.group[i0 + 64 * j] : -1;
+    for (int j = 0; j < TRIPS; ++j) e[j] = i0 + 64 * j < a.n ? a.group[i0 + 64 * j] : -1;
     int *const mine = cnt + wave * a.groups;
 #pragma unroll
-    for (int j = 0; j < ROWS_TRIPS; ++j) {
+    for (int j = 0; j < TRIPS; ++j) {
         const bool in = e[j] >= 0 && e[j] < a.groups;
         if (!in) e[j] = -1;
+        rank[j] = 0;
+        if (i0 - lane + 64 * j >= a.n) continue;                 // (the wave together)
         const uint64_t m = same_group(e[j], in, a.bits);
         const int ahead = __popcll(m & ((1ull << lane) - 1)), all = __popcll(m);
         const int base = in ? mine[e[j]] : 0;
@@ -54,43 +58,55 @@ __device__ __forceinline__ void count_groups(const GroupRowsArgs &a, int *cnt, i
     }
 }
 
-__global__ __launch_bounds__(64 * ROWS_WAVES) void group_hist_kernel(GroupRowsArgs a)
+template <int TRIPS> __global__ __launch_bounds__(ROWS_MOST) void group_hist_kernel(GroupRowsArgs a)
 {
     extern __shared__ int rows_lds[];
-    for (int i = threadIdx.x; i < ROWS_WAVES * a.groups; i += 64 * ROWS_WAVES) rows_lds[i] = 0;
+    const int threads = blockDim.x, waves = threads >> 6;
+    for (int i = threadIdx.x; i < waves * a.groups; i += threads) rows_lds[i] = 0;
     __syncthreads();
-    int e[ROWS_TRIPS], rank[ROWS_TRIPS];
+    int e[TRIPS], rank[TRIPS];
     count_groups(a, rows_lds, e, rank);
     __syncthreads();
-    for (int g = threadIdx.x; g < a.groups; g += 64 * ROWS_WAVES) {
+    for (int g = threadIdx.x; g < a.groups; g += threads) {
         int s = 0;
-        for (int w = 0; w < ROWS_WAVES; ++w) s += rows_lds[w * a.groups + g];
+        for (int w = 0; w < waves; ++w) s += rows_lds[w * a.groups + g];
         a.hist[(long)blockIdx.x * a.groups + g] = (uint32_t)s;
     }
 }
 
-__global__ __launch_bounds__(64 * ROWS_WAVES) void group_place_kernel(GroupRowsArgs a)
+// At least as many threads as groups.
+template <int TRIPS> __global__ __launch_bounds__(ROWS_MOST) void group_place_kernel(GroupRowsArgs a)
 {
     extern __shared__ int rows_lds[];
-    int *const cnt = rows_lds, *const sums = cnt + ROWS_WAVES * a.groups;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    for (int i = tid; i < ROWS_WAVES * a.groups; i += 64 * ROWS_WAVES) cnt[i] = 0;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, threads = blockDim.x, waves = threads >> 6;
+    int *const cnt = rows_lds, *const sums = cnt + waves * a.groups, *const totals = sums + 16;        // totals: [2][groups]
+    for (int i = tid; i < (waves + 2) * a.groups + 16; i += threads) cnt[i] = 0;
     __syncthreads();
-    int e[ROWS_TRIPS], rank[ROWS_TRIPS];
+    int e[TRIPS], rank[TRIPS];
     count_groups(a, cnt, e, rank);
-    __syncthreads();
-    // a thread to a group: its entries in all workgroups, in those ahead, in the waves ahead
-    int total = 0, before = 0;
-    if (tid < a.groups) {
-        if (a.blocks == 1) {
-            for (int w = 0; w < ROWS_WAVES; ++w) total += cnt[w * a.groups + tid];
-        } else {
-#pragma unroll 8
-            for (int b = 0; b < a.blocks; ++b) {
-                const int h = (int)a.hist[(long)b * a.groups + tid];
+    // entries of each group in all workgroups, and in those ahead: the threads share out the workgroups
+    if (a.blocks > 1) {
+        const int parts = threads / a.groups, part = tid / a.groups, g = tid - part * a.groups;
+        if (part < parts) {
+            int total = 0, before = 0;
+#pragma unroll 4
+            for (int b = part; b < a.blocks; b += parts) {
+                const int h = (int)a.hist[(long)b * a.groups + g];
                 total += h;
                 before += b < (int)blockIdx.x ? h : 0;
             }
+            atomicAdd(totals + g, total);                        // (in LDS, of integers: in any order)
+            atomicAdd(totals + a.groups + g, before);
+        }
+    }
+    __syncthreads();
+    int total = 0, before = 0;
+    if (tid < a.groups) {
+        if (a.blocks == 1) {
+            for (int w = 0; w < waves; ++w) total += cnt[w * a.groups + tid];
+        } else {
+            total = totals[tid];
+            before = totals[a.groups + tid];
         }
     }
     int upto = total;
@@ -102,8 +118,7 @@ __global__ __launch_bounds__(64 * ROWS_WAVES) void group_place_kernel(GroupRowsA
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
     int ahead = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < ROWS_WAVES; ++w) {
+    for (int w = 0; w < waves; ++w) {
         const int s = sums[w];
         ahead += w < wave ? s : 0;
         all += s;
@@ -115,16 +130,16 @@ __global__ __launch_bounds__(64 * ROWS_WAVES) void group_place_kernel(GroupRowsA
             if (tid == a.groups - 1) a.offsets[a.groups] = all;
         }
         int at = first + before;
-        for (int w = 0; w < ROWS_WAVES; ++w) {
+        for (int w = 0; w < waves; ++w) {
             const int c = cnt[w * a.groups + tid];
             cnt[w * a.groups + tid] = at;
             at += c;
         }
     }
     __syncthreads();
-    const long i0 = (long)blockIdx.x * ROWS_SEG + wave * 64 * ROWS_TRIPS + lane;
+    const long i0 = (long)blockIdx.x * (threads * TRIPS) + wave * 64 * TRIPS + lane;
 #pragma unroll
-    for (int j = 0; j < ROWS_TRIPS; ++j) {
+    for (int j = 0; j < TRIPS; ++j) {
         const long i = i0 + 64 * j;
         if (i >= a.n) break;
         const int r = e[j] >= 0 ? cnt[wave * a.groups + e[j]] + rank[j] : -1;
@@ -134,26 +149,39 @@ __global__ __launch_bounds__(64 * ROWS_WAVES) void group_place_kernel(GroupRowsA
     }
 }
 
-static int rows_blocks(long n) { return (int)((n + ROWS_SEG - 1) / ROWS_SEG); }
-size_t group_rows_words(long n, int groups) { return rows_blocks(n) > 1 ? (size_t)rows_blocks(n) * groups : 0; }
+// One workgroup for up to 2048 entries, of 64 threads or as many as there are groups, and four entries to a thread; of more entries, 1024 threads with one each.
+constexpr int ROWS_ONE = 2048;
+static int rows_blocks(long n) { return n <= ROWS_ONE ? 1 : (int)((n + ROWS_MOST - 1) / ROWS_MOST); }
+size_t group_rows_words(long n, int groups) { return n <= ROWS_ONE ? 0 : (size_t)rows_blocks(n) * groups; }
+
+template <int TRIPS> static hipError_t launch_group_trips(const GroupRowsArgs &a, int threads, hipStream_t st)
+{
+    const int lds = ((threads / 64 + 2) * a.groups + 16) * 4;
+    constexpr int MOST = ((ROWS_MOST / 64 + 2) * GROUP_ROWS_MAX + 16) * 4;
+    auto hist = group_hist_kernel<TRIPS>;
+    auto place = group_place_kernel<TRIPS>;
+    if (lds > 64 * 1024) {
+        hipError_t e = ensure_max_lds(reinterpret_cast<const void *>(place), MOST);
+        if (e == hipSuccess) e = ensure_max_lds(reinterpret_cast<const void *>(hist), MOST);
+        if (e != hipSuccess) return e;
+    }
+    if (a.blocks > 1) {
+        hipLaunchKernelGGL(hist, dim3((unsigned)a.blocks), dim3((unsigned)threads), lds, st, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(place, dim3((unsigned)a.blocks), dim3((unsigned)threads), lds, st, a);
+    return hipGetLastError();
+}
 
 hipError_t launch_group_rows(const int *group, int n, int groups, int *offsets, int *order, int *place, uint32_t *hist, hipStream_t st)
 {
     int bits = 0;
     while ((1 << bits) < groups) ++bits;
     const GroupRowsArgs a = {group, n, groups, bits, rows_blocks(n), offsets, order, place, hist};
-    const int lds = (ROWS_WAVES * groups + ROWS_WAVES) * 4, most = (ROWS_WAVES * GROUP_ROWS_MAX + ROWS_WAVES) * 4;
-    hipError_t e = ensure_max_lds(reinterpret_cast<const void *>(group_place_kernel), most);
-    if (e != hipSuccess) return e;
-    if (a.blocks > 1) {
-        e = ensure_max_lds(reinterpret_cast<const void *>(group_hist_kernel), most);
-        if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(group_hist_kernel, dim3((unsigned)a.blocks), dim3(64 * ROWS_WAVES), lds, st, a);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL(group_place_kernel, dim3((unsigned)a.blocks), dim3(64 * ROWS_WAVES), lds, st, a);
-    return hipGetLastError();
+    if (a.blocks > 1) return launch_group_trips<1>(a, ROWS_MOST, st);
+    const int least = (groups + 63) / 64 * 64, whole = (n + 255) / 256 * 64;
+    return launch_group_trips<4>(a, least > whole ? least : whole, st);
 }
 
 // ---------------------------------------------------------------- rows in the order of their groups
@@ -165,30 +193,60 @@ struct GatherArgs {
     long ldx, ldy;
 };
 
-__global__ __launch_bounds__(256) void gather_rows_kernel(GatherArgs a)
+// Rows of more bytes than this go past the caches.  (On their way / so, us, 1024 columns of bf16: 12608 tokens to 4 experts each, 103 MB, 38.8 / 37.3, with the product of 768
+// columns that reads them 131.5 / 125.3, of 128 75.7 / 73.5; 3152 tokens, 26 MB, 15.4 / 15.2, with the product 49.3 / 51.5.)
+constexpr long FAR_BYTES = 64L << 20;
+
+// Bound by memory: a row read by each of its copies and written once, 205 MB at 6.2 TB/s there.  (Tokens dealt out to the XCDs, so that their copies meet in one L2: 48 us of the kernel
+// alone for 29.)
+// Chunk c of a row of so many bytes
+template <bool FAR> __device__ __forceinline__ void put_bytes(uint8_t *dst, const i32x4 &v, int c, int bytes)
 {
-    fetch_args<GatherArgs>();
-    const int lane = threadIdx.x & 63, nch = (a.bytes + 15) / 16;
-    for (long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6); r < a.rows; r += (long)gridDim.x * 4) {
-        const int i = a.order[r], t = i / a.topk;
-        if (i < 0 || t >= a.tokens) continue;
-        const uint8_t *src = a.X + t * a.ldx;
-        uint8_t *dst = a.Y + r * a.ldy;
-        for (int c = lane; c < nch; c += 64) {
-            const i32x4 v = *reinterpret_cast<const i32x4 *>(src + (long)c * 16);
-            const int n = a.bytes - c * 16;
-            if (n >= 16) *reinterpret_cast<i32x4 *>(dst + (long)c * 16) = v;
-            else for (int b = 0; b < n; ++b) dst[(long)c * 16 + b] = (uint8_t)((uint32_t)v[b >> 2] >> (8 * (b & 3)));
-        }
+    const int n = bytes - c * 16;
+    i32x4 *const at = reinterpret_cast<i32x4 *>(dst + (long)c * 16);
+    if (n >= 16 && FAR) __builtin_nontemporal_store(v, at);
+    else if (n >= 16) *at = v;
+    else for (int b = 0; b < n; ++b) dst[(long)c * 16 + b] = (uint8_t)((uint32_t)v[b >> 2] >> (8 * (b & 3)));
+}
+
+// 16 bytes of a row to a lane, LPR lanes to a row, NC such pieces of a lane on their way.
+template <int LPR, int NC, bool FAR> __device__ __forceinline__ void copy_row(const uint8_t *src, uint8_t *dst, int bytes, int l)
+{
+    const int nch = (bytes + 15) / 16;
+    for (int c0 = 0; c0 < nch; c0 += LPR * NC) {
+        i32x4 v[NC];
+#pragma unroll
+        for (int i = 0; i < NC; ++i) v[i] = *reinterpret_cast<const i32x4 *>(src + (long)min(c0 + LPR * i + l, nch - 1) * 16);
+#pragma unroll
+        for (int i = 0; i < NC; ++i) put_bytes<FAR>(dst, v[i], c0 + LPR * i + l, bytes);
     }
 }
 
+template <int LPR, int NC, bool FAR> __global__ __launch_bounds__(256) void gather_rows_kernel(GatherArgs a)
+{
+    fetch_args<GatherArgs>();
+    const long r = flat_block() * (256 / LPR) + threadIdx.x / LPR;
+    if (r >= a.rows) return;
+    const int i = a.order[r], t = i / a.topk;
+    if (i >= 0 && t < a.tokens) copy_row<LPR, NC, FAR>(a.X + t * a.ldx, a.Y + r * a.ldy, a.bytes, threadIdx.x % LPR);
+}
+
+template <int LPR, int NC, bool FAR> static hipError_t launch_gather_one(const GatherArgs &a, hipStream_t st)
+{
+    hipLaunchKernelGGL((gather_rows_kernel<LPR, NC, FAR>), flat_grid(((long)a.rows + 256 / LPR - 1) / (256 / LPR)), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
 hipError_t launch_gather_rows(int es, const void *X, int tokens, int cols, long ldx, const int *order, int rows, int topk, void *Y, long ldy, hipStream_t st)
 {
     const GatherArgs a = {(const uint8_t *)X, (uint8_t *)Y, order, tokens, rows, topk, cols * es, ldx, ldy};
-    const long wgs = ((long)rows + 3) / 4;
-    hipLaunchKernelGGL(gather_rows_kernel, dim3((unsigned)(wgs < MAX_GRID_X ? wgs : MAX_GRID_X)), dim3(256), 0, st, a);
-    return hipGetLastError();
+    const int nch = (a.bytes + 15) / 16;
+    if ((long)rows * a.bytes > FAR_BYTES && nch > 32) return nch <= 64 ? launch_gather_one<64, 1, true>(a, st) : nch <= 128 ? launch_gather_one<64, 2, true>(a, st) : launch_gather_one<64, 4, true>(a, st);
+    if (nch <= 8)   return launch_gather_one<8, 1, false>(a, st);
+    if (nch <= 16)  return launch_gather_one<16, 1, false>(a, st);
+    if (nch <= 32)  return launch_gather_one<32, 1, false>(a, st);
+    if (nch <= 64)  return launch_gather_one<64, 1, false>(a, st);
+    if (nch <= 128) return launch_gather_one<64, 2, false>(a, st);
+    return launch_gather_one<64, 4, false>(a, st);
 }
 
 // ---------------------------------------------------------------- and back to their tokens
@@ -199,86 +257,156 @@ __device__ __forceinline__ void put_chunk(uint8_t *dst, const uint32_t (&o)[4], 
     else for (int e = 0; e < n; ++e) reinterpret_cast<uint16_t *>(dst)[e] = (uint16_t)(o[e >> 1] >> (16 * (e & 1)));
 }
 
-template <int DT> __global__ __launch_bounds__(256) void combine_rows_kernel(CombineArgs a)
+// A slice of a token's row, NC chunks to each of LPR lanes, or the whole row; the rows of U choices are on their way together.
+template <int DT, int LPR, int NC> __global__ __launch_bounds__(256) void combine_rows_kernel(CombineArgs a)
 {
     using T = Traits<DT>;
+    constexpr int U = NC == 1 ? 4 : 2;
     fetch_args<CombineArgs>();
-    const int lane = threadIdx.x & 63, nch = (a.cols + 7) / 8, slices = (nch + 63) / 64;
-    const long items = (long)a.tokens * slices;
-    for (long it = (long)blockIdx.x * 4 + (threadIdx.x >> 6); it < items; it += (long)gridDim.x * 4) {
-        const int t = (int)(it / slices), c = (int)(it - (long)t * slices) * 64 + lane;
-        if (c >= nch) continue;
-        float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (a.base) {
-            const i32x4 v = *reinterpret_cast<const i32x4 *>(a.base + t * a.ldb + (long)c * 16);
+    const int nch = (a.cols + 7) / 8, slices = LPR == 64 ? (nch + 64 * NC - 1) / (64 * NC) : 1;
+    const long it = flat_block() * (256 / LPR) + threadIdx.x / LPR, t = it / slices;
+    const int c0 = (int)(it - t * slices) * 64 * NC + threadIdx.x % LPR;
+    if (t >= a.tokens) return;
+    const int *place = a.place + t * a.topk;
+    const float *weight = a.weight + (a.weight ? t * a.topk : 0);
+    float s[NC][8];
+    i32x4 b[NC];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] = (float)T::elem(v, e);
-        }
-        for (int j = 0; j < a.topk; ++j) {
-            const int r = a.place[(long)t * a.topk + j];
-            if (r < 0 || r >= a.rows) continue;
-            const float w = a.weight ? a.weight[(long)t * a.topk + j] : 1.f;
-            const i32x4 v = *reinterpret_cast<const i32x4 *>(a.Y + r * a.ldy + (long)c * 16);
+    for (int q = 0; q < NC; ++q) {
+        b[q] = i32x4{0, 0, 0, 0};
+        if (a.base) b[q] = *reinterpret_cast<const i32x4 *>(a.base + t * a.ldb + (long)min(c0 + LPR * q, nch - 1) * 16);
+    }
+    for (int j0 = 0; j0 < a.topk; j0 += U) {
+        int r[U];
+        float w[U];
+        i32x4 v[U][NC];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] = __builtin_fmaf(w, (float)T::elem(v, e), s[e]);
+        for (int u = 0; u < U; ++u) {
+            const int j = min(j0 + u, a.topk - 1);
+            r[u] = place[j];
+            w[u] = a.weight ? weight[j] : 1.f;
+            if (j0 + u >= a.topk || r[u] >= a.rows) r[u] = -1;
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int q = 0; q < NC; ++q)
+                if (r[u] >= 0) v[u][q] = *reinterpret_cast<const i32x4 *>(a.Y + r[u] * a.ldy + (long)min(c0 + LPR * q, nch - 1) * 16);
+        if (j0 == 0) {
+#pragma unroll
+            for (int q = 0; q < NC; ++q)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[q][e] = (float)T::elem(b[q], e);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (r[u] >= 0) {
+#pragma unroll
+                for (int q = 0; q < NC; ++q)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[q][e] = __builtin_fmaf(w[u], (float)T::elem(v[u][q], e), s[q][e]);
+            }
+    }
+#pragma unroll
+    for (int q = 0; q < NC; ++q) {
+        const int c = c0 + LPR * q;
         uint32_t o[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = pack2<DT>(s[2 * e], s[2 * e + 1]);
+        for (int e = 0; e < 4; ++e) o[e] = pack2<DT>(s[q][2 * e], s[q][2 * e + 1]);
         put_chunk(a.out + t * a.ldo + (long)c * 16, o, a.cols - c * 8);
     }
 }
 
-// The gradient, a wave to a token: dY[row] = w dout, dweight = dout . Y[row], summed in fp32 by a lane's chunks, then over the lanes.
-template <int DT> __global__ __launch_bounds__(256) void combine_grad_kernel(CombineArgs a)
+// The gradient, LPR lanes to a token, which keep NC chunks of dout each: dY[row] = w dout, dweight = dout . Y[row], summed in fp32 by a lane's chunks, then over the
+// lanes.  LONG: rows of more chunks, dout read again with every choice.
+template <int DT, int LPR, int NC, bool LONG> __global__ __launch_bounds__(256) void combine_grad_kernel(CombineArgs a)
 {
     using T = Traits<DT>;
     fetch_args<CombineArgs>();
-    const int lane = threadIdx.x & 63, nch = (a.cols + 7) / 8;
-    for (long t = (long)blockIdx.x * 4 + (threadIdx.x >> 6); t < a.tokens; t += (long)gridDim.x * 4) {
-        for (int j = 0; j < a.topk; ++j) {
-            const int r = a.place[t * a.topk + j];
-            const bool in = r >= 0 && r < a.rows;
-            float dot = 0.f;
-            if (in) {
-                const float w = a.weight ? a.weight[t * a.topk + j] : 1.f;
-                for (int c = lane; c < nch; c += 64) {
-                    const int n = a.cols - c * 8;
-                    const i32x4 d = mask_chunk(*reinterpret_cast<const i32x4 *>(a.dout + t * a.ldo + (long)c * 16), 2 * n);
-                    float x[8];
+    const int l = threadIdx.x % LPR, nch = (a.cols + 7) / 8;
+    const long t = flat_block() * (256 / LPR) + threadIdx.x / LPR;
+    if (t >= a.tokens) return;
+    i32x4 d[NC], y[NC];
+    auto load = [&](i32x4 (&v)[NC], const uint8_t *row, int c0) __attribute__((always_inline)) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = (float)T::elem(d, e);
-                    if (a.dweight) {
-                        const i32x4 y = mask_chunk(*reinterpret_cast<const i32x4 *>(a.Y + r * a.ldy + (long)c * 16), 2 * n);
+        for (int i = 0; i < NC; ++i) v[i] = *reinterpret_cast<const i32x4 *>(row + (long)min(c0 + LPR * i + l, nch - 1) * 16);
+    };
+    auto cut = [&](i32x4 (&v)[NC], int c0) __attribute__((always_inline)) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(x[e], (float)T::elem(y, e), dot);
-                    }
+        for (int i = 0; i < NC; ++i) {
+            const int c = c0 + LPR * i + l;
+            if (c >= nch - 1) v[i] = mask_chunk(v[i], c < nch ? 2 * (a.cols - c * 8) : 0);
+        }
+    };
+    const uint8_t *dout = a.dout + t * a.ldo;
+    if (!LONG) load(d, dout, 0);
+    bool whole = true;                                           // what lies behind the row is still in d
+    for (int j = 0; j < a.topk; ++j) {
+        const int r = a.place[t * a.topk + j];
+        const bool in = r >= 0 && r < a.rows;
+        float dot = 0.f;
+        if (in) {
+            const float w = a.weight ? a.weight[t * a.topk + j] : 1.f;
+            for (int c0 = 0; c0 < (LONG ? nch : 1); c0 += LPR * NC) {
+                if (LONG) load(d, dout, c0);
+                if (a.dweight) load(y, a.Y + r * a.ldy, c0);
+                if (LONG || whole) cut(d, c0);
+                whole = false;
+                if (a.dweight) cut(y, c0);
+#pragma unroll
+                for (int i = 0; i < NC; ++i) {
+                    const int c = c0 + LPR * i + l;
                     uint32_t o[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[e] = pack2<DT>(w * x[2 * e], w * x[2 * e + 1]);
-                    if (a.dY) put_chunk(a.dY + r * a.lddy + (long)c * 16, o, n);
+                    for (int e = 0; e < 4; ++e) {
+                        const float x0 = (float)T::elem(d[i], 2 * e), x1 = (float)T::elem(d[i], 2 * e + 1);
+                        if (a.dweight) dot = __builtin_fmaf(x1, (float)T::elem(y[i], 2 * e + 1), __builtin_fmaf(x0, (float)T::elem(y[i], 2 * e), dot));
+                        o[e] = pack2<DT>(w * x0, w * x1);
+                    }
+                    if (a.dY) put_chunk(a.dY + r * a.lddy + (long)c * 16, o, a.cols - c * 8);
                 }
             }
-            if (a.dweight) {
-                dot = wave_sum(dot);
-                if (lane == 0) a.dweight[t * a.topk + j] = in ? dot : 0.f;
-            }
+        }
+        if (a.dweight) {
+            dot = seg_sum(dot, LPR);
+            if (l == 0) a.dweight[t * a.topk + j] = in ? dot : 0.f;
         }
     }
 }
 
+template <int DT, int LPR, int NC> static hipError_t launch_combine_one(const CombineArgs &a, hipStream_t st)
+{
+    const long items = (long)a.tokens * (LPR == 64 ? ((a.cols + 7) / 8 + 64 * NC - 1) / (64 * NC) : 1);
+    hipLaunchKernelGGL((combine_rows_kernel<DT, LPR, NC>), flat_grid((items + 256 / LPR - 1) / (256 / LPR)), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+template <int DT, int LPR, int NC, bool LONG> static hipError_t launch_grad_one(const CombineArgs &a, hipStream_t st)
+{
+    hipLaunchKernelGGL((combine_grad_kernel<DT, LPR, NC, LONG>), flat_grid(((long)a.tokens + 256 / LPR - 1) / (256 / LPR)), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+template <int DT> static hipError_t launch_combine_type(bool grad, const CombineArgs &a, hipStream_t st)
+{
+    const int nch = (a.cols + 7) / 8;
+    if (!grad) {
+        if (nch <= 8)  return launch_combine_one<DT, 8, 1>(a, st);
+        if (nch <= 16) return launch_combine_one<DT, 16, 1>(a, st);
+        if (nch <= 32) return launch_combine_one<DT, 32, 1>(a, st);
+        if (nch <= 64 || a.tokens < 2048) return launch_combine_one<DT, 64, 1>(a, st);
+        return launch_combine_one<DT, 64, 2>(a, st);
+    }
+    if (nch <= 8)   return launch_grad_one<DT, 8, 1, false>(a, st);
+    if (nch <= 16)  return launch_grad_one<DT, 16, 1, false>(a, st);
+    if (nch <= 32)  return launch_grad_one<DT, 32, 1, false>(a, st);
+    if (nch <= 64)  return launch_grad_one<DT, 64, 1, false>(a, st);
+    if (nch <= 128) return launch_grad_one<DT, 64, 2, false>(a, st);
+    if (nch <= 256) return launch_grad_one<DT, 64, 4, false>(a, st);
+    if (nch <= 512) return launch_grad_one<DT, 64, 8, false>(a, st);
+    return launch_grad_one<DT, 64, 4, true>(a, st);
+}
 hipError_t launch_combine_rows(int dt, bool grad, const CombineArgs &a, hipStream_t st)
 {
-    const long slices = ((a.cols + 7) / 8 + 63) / 64, items = grad ? a.tokens : a.tokens * slices, wgs = (items + 3) / 4;
-    const dim3 grid((unsigned)(wgs < MAX_GRID_X ? wgs : MAX_GRID_X));
-    if (grad) {
-        if (dt == DT_BF16) hipLaunchKernelGGL(combine_grad_kernel<DT_BF16>, grid, dim3(256), 0, st, a);
-        else               hipLaunchKernelGGL(combine_grad_kernel<DT_F16>, grid, dim3(256), 0, st, a);
-    } else {
-        if (dt == DT_BF16) hipLaunchKernelGGL(combine_rows_kernel<DT_BF16>, grid, dim3(256), 0, st, a);
-        else               hipLaunchKernelGGL(combine_rows_kernel<DT_F16>, grid, dim3(256), 0, st, a);
-    }
-    return hipGetLastError();
+    return dt == DT_BF16 ? launch_combine_type<DT_BF16>(grad, a, st) : launch_combine_type<DT_F16>(grad, a, st);
 }
 
 }  // namespace abft
