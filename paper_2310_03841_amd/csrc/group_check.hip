@@ -286,7 +286,8 @@ hipError_t launch_mx4_check(const GroupKernel &k, const Mx4Args &g, int K, const
     return hipGetLastError();
 }
 
-// ---- b = B e and max|B| of each group: a workgroup to 64 bytes (four blocks) of every row, sixteen rows of them to a wave at a time.  In a fixed order.
+// ---- b = B e and max|B| of each group: a workgroup to 64 bytes (four blocks) of every row, sixteen rows of them to a wave at a time.  In a fixed order.  (16 waves, for what they have
+// on their way together: 32 groups of 4096 x 1024 50 us with four.)
 // zero: words that every workgroup helps to clear.
 struct Mx4EncodeArgs {
     const uint8_t *B, *sb;
@@ -296,31 +297,33 @@ struct Mx4EncodeArgs {
     uint32_t *zero;
     size_t zero_words;
 };
-__global__ __launch_bounds__(256) void mx4_encode_kernel(Mx4EncodeArgs a)
+constexpr int ENCODE_WAVES = 16;
+__global__ __launch_bounds__(64 * ENCODE_WAVES) void mx4_encode_kernel(Mx4EncodeArgs a)
 {
-    __shared__ float part[4][4 * 32], tops[4];
+    constexpr int W = ENCODE_WAVES, THREADS = 64 * W;
+    __shared__ float part[W][4 * 32], tops[W];
     fetch_args<Mx4EncodeArgs>();
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const size_t wg = (size_t)blockIdx.y * gridDim.x + blockIdx.x, wgs = (size_t)gridDim.x * gridDim.y;
-    for (size_t i = wg * 256 + tid; i < a.zero_words; i += wgs * 256) a.zero[i] = 0u;
+    for (size_t i = wg * THREADS + tid; i < a.zero_words; i += wgs * THREADS) a.zero[i] = 0u;
     const int e = blockIdx.y, nb = a.K / 16, block = blockIdx.x * 4 + (tid & 3), at = min(block, nb - 1);
     const uint8_t *src = a.B + (long)e * a.sB + at * 16, *sc = a.sb + (long)e * a.stride_sb + at;
     float sum[32], top = 0.f;
 #pragma unroll
     for (int q = 0; q < 32; ++q) sum[q] = 0.f;
     constexpr int U = 4;
-    for (int r0 = tid >> 2; r0 < a.N; r0 += 64 * U) {
+    for (int r0 = tid >> 2; r0 < a.N; r0 += 16 * W * U) {
         i32x4 v[U];
         uint32_t s[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const long r = min(r0 + 64 * u, a.N - 1);
+            const long r = min(r0 + 16 * W * u, a.N - 1);
             v[u] = *reinterpret_cast<const i32x4 *>(src + r * a.ldb);
             s[u] = sc[r * a.ld_sb];
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (r0 + 64 * u >= a.N) break;
+            if (r0 + 16 * W * u >= a.N) break;
             float x[32];
             mx4_values(v[u], mx4_unit(s[u]), x);
 #pragma unroll
@@ -341,10 +344,16 @@ __global__ __launch_bounds__(256) void mx4_encode_kernel(Mx4EncodeArgs a)
     top = wave_max(block < nb ? top : 0.f);
     if (lane == 0) tops[wave] = top;
     __syncthreads();
-    if (tid < 128 && blockIdx.x * 4 + (tid >> 5) < (unsigned)nb)
-        a.b_sum[(long)e * 2 * a.K + blockIdx.x * 128 + tid] = __float_as_uint((part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]));
+    if (tid < 128 && blockIdx.x * 4 + (tid >> 5) < (unsigned)nb) {
+        float t = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) t += part[w][tid];
+        a.b_sum[(long)e * 2 * a.K + blockIdx.x * 128 + tid] = __float_as_uint(t);
+    }
     if (tid == 0) {
-        const float m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+        float m = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) m = fmaxf(m, tops[w]);
         if (m > 0.f) atomicMax(a.b_max + e, __float_as_uint(m));
     }
 }
@@ -352,7 +361,7 @@ __global__ __launch_bounds__(256) void mx4_encode_kernel(Mx4EncodeArgs a)
 hipError_t launch_mx4_encode(const Mx4Args &g, const Workspace &w, uint32_t *zero, size_t zero_words, hipStream_t st)
 {
     const Mx4EncodeArgs a = {g.B, g.sb, g.N, g.K, g.ldb, g.sB, g.ld_sb, g.stride_sb, w.b_sum, w.b_max, zero, zero_words};
-    hipLaunchKernelGGL(mx4_encode_kernel, dim3((unsigned)((g.K / 16 + 3) / 4), (unsigned)g.groups), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(mx4_encode_kernel, dim3((unsigned)((g.K / 16 + 3) / 4), (unsigned)g.groups), dim3(64 * ENCODE_WAVES), 0, st, a);
     return hipGetLastError();
 }
 

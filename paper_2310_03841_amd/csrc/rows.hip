@@ -263,9 +263,8 @@ template <int DT, int LPR, int NC> __global__ __launch_bounds__(256) void combin
     using T = Traits<DT>;
     constexpr int U = NC == 1 ? 4 : 2;
     fetch_args<CombineArgs>();
-    const int nch = (a.cols + 7) / 8, slices = LPR == 64 ? (nch + 64 * NC - 1) / (64 * NC) : 1;
-    const long it = flat_block() * (256 / LPR) + threadIdx.x / LPR, t = it / slices;
-    const int c0 = (int)(it - t * slices) * 64 * NC + threadIdx.x % LPR;
+    const int nch = (a.cols + 7) / 8, c0 = (int)blockIdx.z * 64 * NC + threadIdx.x % LPR;
+    const long t = flat_block() * (256 / LPR) + threadIdx.x / LPR;
     if (t >= a.tokens) return;
     const int *place = a.place + t * a.topk;
     const float *weight = a.weight + (a.weight ? t * a.topk : 0);
@@ -374,10 +373,12 @@ template <int DT, int LPR, int NC, bool LONG> __global__ __launch_bounds__(256) 
     }
 }
 
+// A slice to a z of the grid.
 template <int DT, int LPR, int NC> static hipError_t launch_combine_one(const CombineArgs &a, hipStream_t st)
 {
-    const long items = (long)a.tokens * (LPR == 64 ? ((a.cols + 7) / 8 + 64 * NC - 1) / (64 * NC) : 1);
-    hipLaunchKernelGGL((combine_rows_kernel<DT, LPR, NC>), flat_grid((items + 256 / LPR - 1) / (256 / LPR)), dim3(256), 0, st, a);
+    dim3 grid = flat_grid(((long)a.tokens + 256 / LPR - 1) / (256 / LPR));
+    grid.z = LPR == 64 ? (unsigned)(((a.cols + 7) / 8 + 64 * NC - 1) / (64 * NC)) : 1u;
+    hipLaunchKernelGGL((combine_rows_kernel<DT, LPR, NC>), grid, dim3(256), 0, st, a);
     return hipGetLastError();
 }
 template <int DT, int LPR, int NC, bool LONG> static hipError_t launch_grad_one(const CombineArgs &a, hipStream_t st)
