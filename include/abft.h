@@ -480,6 +480,8 @@ int abft_tile_shape(abft_dtype dtype, const abft_shape *s, int *tile_m, int *til
  * column: 16 x 16 or 32, 64 x 64 or 128, or 256 x 256 (where the last rows of a group, and tiles of the last round, are 128 high).  It needs no context and no
  * GPU, and refuses a shape as the calls do; a C of 16-bit values is taken for one of int32 in its alignment. */
 int abft_group_tile_shape(abft_dtype dtype, int mode, const abft_shape *s, int *tile_m, int *tile_n);
+/* The same for abft_gemm_mx4 (its scales taken for as far apart as they need be). */
+int abft_mx4_tile_shape(int mode, const abft_shape *s, int *tile_m, int *tile_n);
 
 /* Kernel timing for reports (not a hot call: creates HIP events).  Between begin and end every
  * abft_gemm records events on the caller's stream around its kernels; up to max_calls calls are

@@ -25,7 +25,7 @@ __all__ = [
     "abft_route", "abft_route_grad", "abft_group_rows", "abft_gather_rows", "abft_combine_rows", "abft_combine_rows_grad", "abft_quantize_mx4",
     "abft_dequantize_mx4", "abft_gemm_mx4", "abft_encode_mx4", "AbftError", "lib", "lib_path", "exported_symbols",
     "abft_create", "abft_destroy", "abft_encode_b", "abft_gemm", "abft_gemm_bias", "abft_gemm_static", "abft_verify", "abft_correct",
-    "abft_correct_checksum", "abft_inject", "abft_discrepancy", "abft_workspace", "abft_tile_shape", "abft_group_tile_shape", "abft_strerror", "abft_last_hip_error",
+    "abft_correct_checksum", "abft_inject", "abft_discrepancy", "abft_workspace", "abft_tile_shape", "abft_group_tile_shape", "abft_mx4_tile_shape", "abft_strerror", "abft_last_hip_error",
     "abft_version", "abft_mfma_peak", "abft_profile_begin", "abft_profile_end", "make_shape", "make_result", "DTYPE_CODE",
 ]
 
@@ -157,6 +157,8 @@ _SIGS = {
                                        ctypes.POINTER(ctypes.c_int)]),
     "abft_group_tile_shape": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.POINTER(abft_shape),
                                              ctypes.POINTER(ctypes.c_int), ctypes.POINTER(ctypes.c_int)]),
+    "abft_mx4_tile_shape": (ctypes.c_int, [ctypes.c_int, ctypes.POINTER(abft_shape), ctypes.POINTER(ctypes.c_int),
+                                           ctypes.POINTER(ctypes.c_int)]),
     "abft_profile_begin": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int]),
     "abft_profile_end": (ctypes.c_int, [ctypes.c_void_p, ctypes.POINTER(ctypes.c_double),
                                         ctypes.POINTER(ctypes.c_int)]),
@@ -469,4 +471,12 @@ def abft_group_tile_shape(dtype: int, mode: int, shape: abft_shape):
     rc = lib().abft_group_tile_shape(dtype, mode, ctypes.byref(shape), ctypes.byref(tm), ctypes.byref(tn))
     if rc != ABFT_OK:
         raise AbftError(rc, "abft_group_tile_shape")
+    return tm.value, tn.value
+
+
+def abft_mx4_tile_shape(mode: int, shape: abft_shape):
+    tm, tn = ctypes.c_int(), ctypes.c_int()
+    rc = lib().abft_mx4_tile_shape(mode, ctypes.byref(shape), ctypes.byref(tm), ctypes.byref(tn))
+    if rc != ABFT_OK:
+        raise AbftError(rc, "abft_mx4_tile_shape")
     return tm.value, tn.value

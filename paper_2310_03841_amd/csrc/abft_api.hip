@@ -992,6 +992,24 @@ extern "C" int abft_gemm_mx4(abft_ctx *ctx, const void *A, const void *B, const 
     return ABFT_OK;
 }
 
+extern "C" int abft_mx4_tile_shape(int mode, const abft_shape *s, int *tile_m, int *tile_n)
+{
+    if (!s || !tile_m || !tile_n) return ABFT_EINVAL;
+    if (mode != ABFT_OFF && mode != ABFT_DETECT) return ABFT_EINVAL;
+    // (any pointer will do: nothing follows it)
+    static const uint8_t any[16] __attribute__((aligned(16))) = {};
+    const int64_t lds = s->K > 0 && s->K <= (1 << 29) ? round_up((s->K + 31) / 32, 16) : 16;
+    const abft_mx4 q = {any, any, lds, lds, s->N > 0 && s->N <= (1 << 29) ? lds * s->N : 16, nullptr, ABFT_BF16, 0};
+    Shape sh;
+    const int rc = check_mx4(nullptr, &q, s, true, &sh);
+    if (rc) return rc;
+    Mx4Args g = mx4_args(nullptr, nullptr, nullptr, nullptr, &q, sh);
+    GroupKernel k;
+    if (!mx4_plan(mode != ABFT_OFF, g, &k)) return ABFT_ESHAPE;
+    mx4_tile_shape(k, g, tile_m, tile_n);
+    return ABFT_OK;
+}
+
 // What the rows of a dispatch ask of their sizes; es: bytes of an element.
 static int check_rows(int64_t rows, int64_t cols, int64_t ld, int es)
 {

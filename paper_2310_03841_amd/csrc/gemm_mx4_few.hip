@@ -219,7 +219,7 @@ constexpr int MX4_FEW_MAX_SUMS = 64 * 1024;      // bytes of LDS for the column 
 bool mx4_few_fits(bool protect, const Mx4Args &g) { return !protect || (g.M <= 32L * g.groups && g.K * 8L <= MX4_FEW_MAX_SUMS); }
 
 // 32 columns to a workgroup, which reads its rows of A once for both halves, unless that leaves compute units without one.
-static int mx4_few_columns(const Mx4Args &g)
+int mx4_few_columns(const Mx4Args &g)
 {
     const long rows = ((long)g.M + g.groups - 1) / g.groups;                 // of a group on average
     return std::min(g.M, g.groups) * ((rows + 15) / 16) * ((g.N + 31) / 32) >= 512 ? 32 : 16;

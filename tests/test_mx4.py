@@ -263,6 +263,71 @@ def test_product_matches_plain(out, ends, N, K):
             p.close()
 
 
+# each kernel by name, unprotected and protected: which tiles a problem takes
+KERNELS = {
+    (16, 16): ([0, 1, 4, 9], 200, 520),
+    (16, 32): ([0, 2, 2, 22, 24] + list(range(25, 61)), 1030, 264),
+    (64, 64): ([0, 150, 150, 1201], 200, 1000),
+    (64, 128): ([0, 1000, 1530, 2311], 1100, 168),
+    (256, 256): ([0, 257, 257, 2900, 3029, 5000], 1546, 768),
+}
+DEEP = ([0, 255, 4400], 1090, 2304)                             # tiles of 256 x 256 of more slabs than three, and a last round of halves
+
+
+def tile_of(ends, N, K, mode):
+    up32 = up(K, 32)
+    return ab.abft_mx4_tile_shape(mode, ab.make_shape(ends[-1], N, K, batch=len(ends) - 1, lda=up32, ldb=up32, strideB=N * up32, ldc=up(N, 8)))
+
+
+def test_which_kernel_a_problem_takes():
+    for mode in (ab.ABFT_OFF, ab.ABFT_DETECT):
+        for tile, (ends, N, K) in KERNELS.items():
+            assert tile_of(ends, N, K, mode) == tile, (tile, mode)
+        assert tile_of(*DEEP, mode) == (256, 256)
+        # not whole slabs of 256 elements (as blocks of 32 cover them), or fewer than three of them
+        for K in (736, 769, 512, 3000):
+            assert tile_of(KERNELS[256, 256][0], 1546, K, mode) != (256, 256)
+        with pytest.raises(ab.AbftError):
+            ab.abft_mx4_tile_shape(mode, ab.make_shape(4, 16, 100, lda=96, ldb=128, ldc=16))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("out", ["bf16", "f16"])
+@pytest.mark.parametrize("ends,N,K", list(KERNELS.values()) + [DEEP])
+def test_each_kernel(out, ends, N, K):
+    """Clean, with a bias; flips all over its tiles; blocks of NaN."""
+    p = Product(ends, N, K, M=ends[-1] + 2, out=out, bias=True, seed=K)
+    try:
+        p.run()
+        p.check(clean=False)
+        sums = p.want()[0] - p.bias
+        p.run(ab.ABFT_DETECT)
+        p.check()
+        rng = np.random.default_rng(K)
+        sizes = np.diff(ends)
+        places = [(g, r, c) for g in np.flatnonzero(sizes)[[0, -1]] for r in (0, sizes[g] - 1) for c in (0, N - 1)]
+        places += [(g, rng.integers(sizes[g]), rng.integers(N)) for g in rng.choice(np.flatnonzero(sizes), 6)]
+        for g, r, c in places:
+            bit = 29 if abs(sums[ends[g] + r, c]) >= 2 else 30
+            ok(ab.abft_inject(p.ctx, None, ab.ABFT_BF16, p.shape, int(g), int(r), int(c), bit, ab.ABFT_INJECT_ACCUMULATOR))
+            p.run(ab.ABFT_DETECT | ab.ABFT_B_CHECKSUM_CACHED)
+            assert np.flatnonzero(p.row_flag.cpu().numpy()).tolist() == [ends[g] + r], (g, r, c)
+            assert np.flatnonzero(p.col_flag.cpu().numpy()).tolist() == [g * N + c], (g, r, c)
+        p.run(ab.ABFT_DETECT)
+        p.check()
+        # a row of A and a column of B with a block of NaN, in the last group with rows
+        g = int(np.flatnonzero(sizes)[-1])
+        r, c = ends[g + 1] - 1, g * N + N // 2
+        p.sA[r, 0], p.sB[c, (K - 1) // 32] = 255, 255
+        p.upload()
+        p.run(ab.ABFT_DETECT)
+        p.check(clean=False)
+        rf, cf = p.row_flag.cpu().numpy(), p.col_flag.cpu().numpy()
+        assert rf[r] == 1 and cf[c] == 1 and rf[:ends[g]].sum() == 0 and cf[:g * N].sum() == 0
+    finally:
+        p.close()
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("ends,N,K", [([0, 3, 3, 8], 70, 96), ([0, 20, 21, 22, 23], 70, 600), ([0, 130, 200, 290], 200, 136), ([0, 600, 1500], 520, 384), ([0, 2500], 1100, 512)])
 def test_a_flip_in_an_accumulator_is_found(ends, N, K):
