@@ -328,7 +328,7 @@ int abft_gather_rows(const void *X, abft_dtype dtype, int64_t tokens, int64_t co
                      void *Y, int64_t ldy, void *stream);
 
 /* out[t] = base[t] + the sum over j of weight[t][j] Y[place[t][j]], in fp32, j rising, rounded once; places outside [0, rows) have no part, whatever
- * their weight.  base: NULL, or added first (may be out itself); weight: NULL, or [tokens][topk]: ones.  ABFT_BF16 or ABFT_F16.  What lies
+ * their weight.  base: NULL, or added first (may be out itself, of the same pitch); weight: NULL, or [tokens][topk]: ones.  ABFT_BF16 or ABFT_F16.  What lies
  * between cols and ldo stays.  tokens * topk <= 2^30. */
 int abft_combine_rows(const void *Y, abft_dtype dtype, int64_t rows, int64_t cols, int64_t ldy, const int32_t *place, const float *weight,
                       int64_t tokens, int32_t topk, const void *base, int64_t ldb, void *out, int64_t ldo, void *stream);

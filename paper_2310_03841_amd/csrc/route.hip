@@ -269,9 +269,8 @@ __device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL]
     *mine = l < a.topk ? lds.chosen[l] : -1;
     if constexpr (ROUNDED) {
         if (check) {
-            const int e = l <= a.topk ? lds.chosen[l] : -1, next = l < a.topk ? lds.chosen[l + 1] : -1;
+            const int next = l < a.topk ? lds.chosen[l + 1] : -1;
             const float next_key = __shfl_down(my_key, 1);
-            (void)e;
             if (next >= 0 && !(my_key - next_key > 0x1p-18f * (1.f + fabsf(my_key)))) sure = false;
         }
         return over_token<LPT>((int)sure, Smaller{}) != 0;

@@ -16,7 +16,7 @@ constexpr int ROWS_MOST = 1024;                              // threads
 
 struct GroupRowsArgs {
     const int *group;
-    int n, groups, bits, blocks;
+    int n, groups, bits, blocks, iters;   // iters: times that a workgroup takes its threads' entries
     int *offsets, *order, *place;
     uint32_t *hist;                       // [blocks][groups]
 };
@@ -33,20 +33,19 @@ __device__ __forceinline__ uint64_t same_group(int e, bool in, int bits)
     return m;
 }
 
-// cnt: [waves][groups], zero.  Each trip's group and its rank in the wave.
-template <int TRIPS> __device__ __forceinline__ void count_groups(const GroupRowsArgs &a, int *cnt, int (&e)[TRIPS], int (&rank)[TRIPS])
+// Entries i0 .. of a wave, TRIPS times 64 of them.  cnt: [waves][groups], zero.  Each trip's group, -1 for none, and its rank in the wave.
+template <int TRIPS> __device__ __forceinline__ void count_groups(const GroupRowsArgs &a, int *cnt, long i0, int (&e)[TRIPS], int (&rank)[TRIPS])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long i0 = (long)blockIdx.x * (blockDim.x * TRIPS) + wave * 64 * TRIPS + lane;
 #pragma unroll
-    for (int j = 0; j < TRIPS; ++j) e[j] = i0 + 64 * j < a.n ? a.group[i0 + 64 * j] : -1;
+    for (int j = 0; j < TRIPS; ++j) e[j] = i0 + 64 * j + lane < a.n ? a.group[i0 + 64 * j + lane] : -1;
     int *const mine = cnt + wave * a.groups;
 #pragma unroll
     for (int j = 0; j < TRIPS; ++j) {
         const bool in = e[j] >= 0 && e[j] < a.groups;
         if (!in) e[j] = -1;
         rank[j] = 0;
-        if (i0 - lane + 64 * j >= a.n) continue;                 // (the wave together)
+        if (i0 + 64 * j >= a.n) continue;                        // (the wave together)
         const uint64_t m = same_group(e[j], in, a.bits);
         const int ahead = __popcll(m & ((1ull << lane) - 1)), all = __popcll(m);
         const int base = in ? mine[e[j]] : 0;
@@ -58,18 +57,20 @@ template <int TRIPS> __device__ __forceinline__ void count_groups(const GroupRow
     }
 }
 
-template <int TRIPS> __global__ __launch_bounds__(ROWS_MOST) void group_hist_kernel(GroupRowsArgs a)
+__global__ __launch_bounds__(ROWS_MOST) void group_hist_kernel(GroupRowsArgs a)
 {
     extern __shared__ int rows_lds[];
-    const int threads = blockDim.x, waves = threads >> 6;
-    for (int i = threadIdx.x; i < waves * a.groups; i += threads) rows_lds[i] = 0;
+    constexpr int THREADS = ROWS_MOST, WAVES = THREADS / 64;
+    for (int i = threadIdx.x; i < WAVES * a.groups; i += THREADS) rows_lds[i] = 0;
     __syncthreads();
-    int e[TRIPS], rank[TRIPS];
-    count_groups(a, rows_lds, e, rank);
+    for (int it = 0; it < a.iters; ++it) {
+        int e[1], rank[1];
+        count_groups<1>(a, rows_lds, ((long)blockIdx.x * a.iters + it) * THREADS + (threadIdx.x & ~63), e, rank);
+    }
     __syncthreads();
-    for (int g = threadIdx.x; g < a.groups; g += threads) {
+    for (int g = threadIdx.x; g < a.groups; g += THREADS) {
         int s = 0;
-        for (int w = 0; w < waves; ++w) s += rows_lds[w * a.groups + g];
+        for (int w = 0; w < WAVES; ++w) s += rows_lds[w * a.groups + g];
         a.hist[(long)blockIdx.x * a.groups + g] = (uint32_t)s;
     }
 }
@@ -82,8 +83,9 @@ template <int TRIPS> __global__ __launch_bounds__(ROWS_MOST) void group_place_ke
     int *const cnt = rows_lds, *const sums = cnt + waves * a.groups, *const totals = sums + 16;        // totals: [2][groups]
     for (int i = tid; i < (waves + 2) * a.groups + 16; i += threads) cnt[i] = 0;
     __syncthreads();
+    const long block0 = (long)blockIdx.x * a.iters * threads * TRIPS;
     int e[TRIPS], rank[TRIPS];
-    count_groups(a, cnt, e, rank);
+    count_groups<TRIPS>(a, cnt, block0 + wave * 64 * TRIPS, e, rank);
     // entries of each group in all workgroups, and in those ahead: the threads share out the workgroups
     if (a.blocks > 1) {
         const int parts = threads / a.groups, part = tid / a.groups, g = tid - part * a.groups;
@@ -123,65 +125,68 @@ template <int TRIPS> __global__ __launch_bounds__(ROWS_MOST) void group_place_ke
         ahead += w < wave ? s : 0;
         all += s;
     }
-    if (tid < a.groups) {
-        const int first = ahead + upto - total;
-        if (blockIdx.x == 0) {
-            a.offsets[tid] = first;
-            if (tid == a.groups - 1) a.offsets[a.groups] = all;
-        }
-        int at = first + before;
-        for (int w = 0; w < waves; ++w) {
-            const int c = cnt[w * a.groups + tid];
-            cnt[w * a.groups + tid] = at;
-            at += c;
-        }
+    int at = ahead + upto - total;                               // the group's next row
+    if (blockIdx.x == 0 && tid < a.groups) {
+        a.offsets[tid] = at;
+        if (tid == a.groups - 1) a.offsets[a.groups] = all;
     }
-    __syncthreads();
-    const long i0 = (long)blockIdx.x * (threads * TRIPS) + wave * 64 * TRIPS + lane;
+    at += before;
+    for (int it = 0;;) {
+        if (tid < a.groups)
+            for (int w = 0; w < waves; ++w) {
+                const int c = cnt[w * a.groups + tid];
+                cnt[w * a.groups + tid] = at;
+                at += c;
+            }
+        __syncthreads();
+        const long i0 = block0 + (long)it * threads * TRIPS + wave * 64 * TRIPS + lane;
 #pragma unroll
-    for (int j = 0; j < TRIPS; ++j) {
-        const long i = i0 + 64 * j;
-        if (i >= a.n) break;
-        const int r = e[j] >= 0 ? cnt[wave * a.groups + e[j]] + rank[j] : -1;
-        a.place[i] = r;
-        if (r >= 0) a.order[r] = (int)i;
-        if (i >= all) a.order[i] = -1;                           // rows behind the last group
+        for (int j = 0; j < TRIPS; ++j) {
+            const long i = i0 + 64 * j;
+            if (i >= a.n) break;
+            const int r = e[j] >= 0 ? cnt[wave * a.groups + e[j]] + rank[j] : -1;
+            a.place[i] = r;
+            if (r >= 0) a.order[r] = (int)i;
+            if (i >= all) a.order[i] = -1;                       // rows behind the last group
+        }
+        if (++it == a.iters) break;
+        __syncthreads();
+        for (int i = tid; i < waves * a.groups; i += threads) cnt[i] = 0;
+        __syncthreads();
+        count_groups<TRIPS>(a, cnt, i0 - lane + threads * TRIPS, e, rank);
+        __syncthreads();
     }
 }
 
-// One workgroup for up to 2048 entries, of 64 threads or as many as there are groups, and four entries to a thread; of more entries, 1024 threads with one each.
-constexpr int ROWS_ONE = 2048;
-static int rows_blocks(long n) { return n <= ROWS_ONE ? 1 : (int)((n + ROWS_MOST - 1) / ROWS_MOST); }
-size_t group_rows_words(long n, int groups) { return n <= ROWS_ONE ? 0 : (size_t)rows_blocks(n) * groups; }
-
-template <int TRIPS> static hipError_t launch_group_trips(const GroupRowsArgs &a, int threads, hipStream_t st)
-{
-    const int lds = ((threads / 64 + 2) * a.groups + 16) * 4;
-    constexpr int MOST = ((ROWS_MOST / 64 + 2) * GROUP_ROWS_MAX + 16) * 4;
-    auto hist = group_hist_kernel<TRIPS>;
-    auto place = group_place_kernel<TRIPS>;
-    if (lds > 64 * 1024) {
-        hipError_t e = ensure_max_lds(reinterpret_cast<const void *>(place), MOST);
-        if (e == hipSuccess) e = ensure_max_lds(reinterpret_cast<const void *>(hist), MOST);
-        if (e != hipSuccess) return e;
-    }
-    if (a.blocks > 1) {
-        hipLaunchKernelGGL(hist, dim3((unsigned)a.blocks), dim3((unsigned)threads), lds, st, a);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL(place, dim3((unsigned)a.blocks), dim3((unsigned)threads), lds, st, a);
-    return hipGetLastError();
-}
+// One workgroup for up to 2048 entries, of 64 threads or as many as there are groups, and four entries to a thread.  Of more entries, 1024 threads with one each, and up to 512
+// workgroups, which go through theirs one thousand at a time: each of them reads the counts of all.
+constexpr int ROWS_ONE = 2048, ROWS_BLOCKS = 512;
+static int rows_iters(long n) { return n <= ROWS_ONE ? 1 : (int)((n + (long)ROWS_MOST * ROWS_BLOCKS - 1) / ((long)ROWS_MOST * ROWS_BLOCKS)); }
+static int rows_blocks(long n) { return n <= ROWS_ONE ? 1 : (int)((n + (long)ROWS_MOST * rows_iters(n) - 1) / ((long)ROWS_MOST * rows_iters(n))); }
+size_t group_rows_words(long n, int groups) { return n <= ROWS_ONE ? 0 : (size_t)(n < (long)ROWS_MOST * ROWS_BLOCKS ? rows_blocks(n) : ROWS_BLOCKS) * groups; }
 
 hipError_t launch_group_rows(const int *group, int n, int groups, int *offsets, int *order, int *place, uint32_t *hist, hipStream_t st)
 {
     int bits = 0;
     while ((1 << bits) < groups) ++bits;
-    const GroupRowsArgs a = {group, n, groups, bits, rows_blocks(n), offsets, order, place, hist};
-    if (a.blocks > 1) return launch_group_trips<1>(a, ROWS_MOST, st);
+    const GroupRowsArgs a = {group, n, groups, bits, rows_blocks(n), rows_iters(n), offsets, order, place, hist};
     const int least = (groups + 63) / 64 * 64, whole = (n + 255) / 256 * 64;
-    return launch_group_trips<4>(a, least > whole ? least : whole, st);
+    const int threads = n > ROWS_ONE ? ROWS_MOST : least > whole ? least : whole;
+    const int lds = ((threads / 64 + 2) * groups + 16) * 4;
+    constexpr int MOST = ((ROWS_MOST / 64 + 2) * GROUP_ROWS_MAX + 16) * 4;
+    auto place_kernel = n > ROWS_ONE ? group_place_kernel<1> : group_place_kernel<4>;
+    hipError_t e = hipSuccess;
+    if (lds > 64 * 1024) {
+        e = ensure_max_lds(reinterpret_cast<const void *>(place_kernel), MOST);
+        if (e == hipSuccess) e = ensure_max_lds(reinterpret_cast<const void *>(group_hist_kernel), MOST);
+        if (e != hipSuccess) return e;
+    }
+    if (n > ROWS_ONE) {
+        hipLaunchKernelGGL(group_hist_kernel, dim3((unsigned)a.blocks), dim3((unsigned)threads), lds, st, a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(place_kernel, dim3((unsigned)a.blocks), dim3((unsigned)threads), lds, st, a);
+    return hipGetLastError();
 }
 
 // ---------------------------------------------------------------- rows in the order of their groups

@@ -349,6 +349,54 @@ def test_entries_by_group(n, groups):
         ab.abft_destroy(ctx)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,groups", [(524288, 3), (524289, 64), (1300001, 1024), (2100000, 5)])
+def test_many_entries_by_group(n, groups):
+    """More than the workgroups take at once."""
+    rng = np.random.default_rng(n)
+    ctx = ab.abft_create(n, 1024, 128, groups)
+    try:
+        g = (groups * rng.random(n) ** 3).astype(np.int32)
+        g[rng.random(n) < 0.05] = -1
+        same_rows(group_rows(ctx, torch.from_numpy(g).cuda(), groups), g, groups)
+    finally:
+        torch.cuda.synchronize()
+        ab.abft_destroy(ctx)
+
+
+@pytest.mark.gpu
+def test_many_entries_in_two_graphs_of_a_context():
+    rng = np.random.default_rng(5)
+    n, groups = 30000, 48
+    ctx = ab.abft_create(n, 1024, 128, groups)
+    try:
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            inputs = [torch.zeros(n, dtype=torch.int32, device="cuda") for _ in range(2)]
+            outs = [group_rows(ctx, x, groups) for x in inputs]
+            s.synchronize()
+            graphs = []
+            for x, out in zip(inputs, outs):
+                g = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(g, stream=s):
+                    ok(ab.abft_group_rows(ctx, x, n, groups, *out))
+                graphs.append(g)
+            for i in range(6):
+                host = [rng.integers(-1, groups, n).astype(np.int32) for _ in range(2)]
+                for x, h in zip(inputs, host):
+                    x.copy_(torch.from_numpy(h))
+                for k in ((0, 1), (1, 0))[i & 1]:
+                    graphs[k].replay()
+                s.synchronize()
+                for out, h in zip(outs, host):
+                    same_rows(out, h, groups)
+                other = torch.from_numpy(host[0][::-1].copy()).cuda()
+                same_rows(group_rows(ctx, other, groups), host[0][::-1], groups)
+    finally:
+        torch.cuda.synchronize()
+        ab.abft_destroy(ctx)
+
+
 # ------------------------------------------------------------------------------------------ rows there and back
 def rows_of(gen, dtype, rows, cols, spare=0):
     ld = pad(cols, 1 if dtype == "i8" else 2) + spare
