@@ -2,6 +2,9 @@
 //
 // A token is LPT lanes of a wave, EPL neighbouring experts to each.  The order of experts is that of score + bias (of the logits, where scores grow with them and
 // nothing is added), equal ones by index; a round takes the best that is left.
+//
+// Bound by the latency of a token's rounds, each a maximum over its lanes and one removed, and of many tokens by their instructions; the logits are read once (12608 x 128 of fp32, 6.5 MB, 1.3 us at
+// 5 TB/s; 6.2 us, all keys in 64 bits 8.9; the gradient 4.0).
 #include "abft_device.h"
 #include "gemm_epilogue.h"
 #include "route_args.h"
@@ -85,14 +88,34 @@ template <int CTRL> __device__ __forceinline__ double dpp_get64(double v)
 template <int CTRL> __device__ __forceinline__ float other(float v) { return dpp_get<CTRL>(v); }
 template <int CTRL> __device__ __forceinline__ int other(int v) { return dpp_mov<CTRL>(v); }
 template <int CTRL> __device__ __forceinline__ double other(double v) { return dpp_get64<CTRL>(v); }
-template <int D> __device__ __forceinline__ float far_other(float v) { return __shfl_xor(v, D); }
-template <int D> __device__ __forceinline__ int far_other(int v) { return __shfl_xor(v, D); }
-template <int D> __device__ __forceinline__ double far_other(double v) { return __shfl_xor(v, D); }
+// Across the rows of 16 lanes and the halves of a wave: the row-swap instructions, whose two results are the lane's own value and the other's, in either order.
+template <int D> __device__ __forceinline__ void far_pair(uint32_t v, uint32_t (&p)[2])
+{
+    if constexpr (D == 16) {
+        auto q = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        p[0] = q[0]; p[1] = q[1];
+    } else {
+        auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        p[0] = q[0]; p[1] = q[1];
+    }
+}
+template <int D, typename V, typename OP> __device__ __forceinline__ V with_far(V v, const OP &op)
+{
+    uint32_t p[2], q[2];
+    if constexpr (sizeof(V) == 4) {
+        far_pair<D>(__builtin_bit_cast(uint32_t, v), p);
+        return op(__builtin_bit_cast(V, p[0]), __builtin_bit_cast(V, p[1]));
+    } else {
+        const uint64_t u = __builtin_bit_cast(uint64_t, v);
+        far_pair<D>((uint32_t)u, p);
+        far_pair<D>((uint32_t)(u >> 32), q);
+        return op(__builtin_bit_cast(V, (uint64_t)q[0] << 32 | p[0]), __builtin_bit_cast(V, (uint64_t)q[1] << 32 | p[1]));
+    }
+}
 template <int CTRL> __device__ __forceinline__ long long other(long long v)
 {
     return __builtin_bit_cast(long long, dpp_get64<CTRL>(__builtin_bit_cast(double, v)));
 }
-template <int D> __device__ __forceinline__ long long far_other(long long v) { return __shfl_xor(v, D); }
 template <int LPT, typename V, typename OP> __device__ __forceinline__ V over_token(V v, const OP &op)
 {
     v = op(v, other<0xB1>(v));     // lane ^ 1
@@ -100,8 +123,8 @@ template <int LPT, typename V, typename OP> __device__ __forceinline__ V over_to
     v = op(v, other<0x141>(v));    // i <-> 7 - i inside 8 lanes
     v = op(v, other<0x140>(v));    // i <-> 15 - i inside 16 lanes
     if constexpr (LPT == 64) {
-        v = op(v, far_other<16>(v));
-        v = op(v, far_other<32>(v));
+        v = with_far<16>(v, op);
+        v = with_far<32>(v, op);
     }
     return v;
 }
@@ -138,9 +161,12 @@ template <> struct Order<double> {
     }
 };
 
-// Scores, off by some 2^-20 at most where they are computed in fp32.
-template <typename KEY, int LPT, int EPL> __device__ __forceinline__ void scores(bool sigmoid, const float (&x)[EPL], float top, KEY (&s)[EPL])
+// Scores, and the largest there can be.  In fp32, with d = x - max x, a softmax's exponential is off by (2 |d| + 2) 2^-24 of itself (d, its multiple and the instruction are each
+// rounded), their sum by as much of its terms and by up to 22 2^-24 for its additions, the quotient by 3 2^-24: with |d| of up to 20 where it counts (a term of a larger one is below 2^-28 of
+// the sum) below 2^-17 s.  A sigmoid is off by 2^-23 (1 + (1 - s)(|x| + 2) / 2) s or less, below 2^-22.
+template <typename KEY, int LPT, int EPL> __device__ __forceinline__ void scores(bool sigmoid, const float (&x)[EPL], float top, KEY (&s)[EPL], float *largest)
 {
+    *largest = 1.f;
     if (sigmoid) {
 #pragma unroll
         for (int i = 0; i < EPL; ++i) {
@@ -163,6 +189,7 @@ template <typename KEY, int LPT, int EPL> __device__ __forceinline__ void scores
         for (int i = 0; i < EPL; ++i) s[i] /= sum;
     } else {
         const float inv = __builtin_amdgcn_rcpf(sum);
+        *largest = inv;
 #pragma unroll
         for (int i = 0; i < EPL; ++i) s[i] *= inv;
     }
@@ -175,7 +202,7 @@ template <int LPT, int EPL, bool GROUPED> struct RouteLds {
 };
 
 // The experts of a token: lane j gets the j-th, -1 where none is left.  False in fp32: keys are so near each other that fp32 may have their order, or what is chosen, wrong; 64 bits then
-// tell (some 1 of 300 tokens with random biases).  Told apart are neighbours among the chosen and the first that is not, and the last group that stays and the first that
+// tell.  Told apart are neighbours among the chosen and the first that is not, and the last group that stays and the first that
 // does not.  Keys of fp32 logits are exact.
 template <typename KEY, int LPT, int EPL, bool GROUPED>
 __device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL], float top, RouteLds<LPT, EPL, GROUPED> &lds, int l, int *mine)
@@ -189,8 +216,9 @@ __device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL]
     KEY s[EPL];
     bool sure = true;
     const bool scored = !a.by_logit;
+    float largest = 1.f;
     if (scored) {
-        scores<KEY, LPT, EPL>(a.sigmoid, x, top, s);
+        scores<KEY, LPT, EPL>(a.sigmoid, x, top, s, &largest);
 #pragma unroll
         for (int i = 0; i < EPL; ++i) {
             const KEY k = a.bias ? s[i] + (KEY)a.bias[min(e0 + i, E - 1)] : s[i];
@@ -211,6 +239,7 @@ __device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL]
         wave_lds_fence();
         for (int g = l; g < G; g += LPT) {
             KEY b0 = -(KEY)inf, b1 = -(KEY)inf;
+#pragma unroll 8
             for (int i = 0; i < per; ++i) {
                 const KEY k = keys[g * per + i];
                 b1 = k > b0 ? b0 : k > b1 ? k : b1;
@@ -225,6 +254,7 @@ __device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL]
             const int g = g0 + l;
             int rank = 0;
             const KEY v = values[min(g, G - 1)];
+#pragma unroll 8
             for (int h = 0; h < G; ++h) {
                 const KEY w = values[h];
                 rank += w > v || (w == v && h < g) ? 1 : 0;
@@ -238,8 +268,9 @@ __device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL]
         if (ROUNDED && scored) {
             in_min = over_token<LPT>(in_min, Smaller{});
             out_max = over_token<LPT>(out_max, Larger{});
-            // (groups without an expert are the last in any arithmetic)
-            sure = out_max == -(KEY)inf || in_min - out_max > (KEY)0x1p-17f * (1 + fabsf((float)out_max));
+            // two sums of two, twice over; with biases, their roundings.  (Groups without an expert are the last in any arithmetic.)
+            const float far = (a.sigmoid ? 0x1p-19f : 0x1p-14f * largest) + 0x1p-20f * fabsf((float)out_max);
+            sure = out_max == -(KEY)inf || (float)(in_min - out_max) > far;
         }
 #pragma unroll
         for (int i = 0; i < EPL; ++i) key[i] = stay >> (min(e0 + i, E - 1) / per) & 1 ? key[i] : O::NONE;
@@ -271,7 +302,12 @@ __device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL]
         if (check) {
             const int next = l < a.topk ? lds.chosen[l + 1] : -1;
             const float next_key = __shfl_down(my_key, 1);
-            if (next >= 0 && !(my_key - next_key > 0x1p-18f * (1.f + fabsf(my_key)))) sure = false;
+            // twice what two keys are off, twice over; of a softmax by the larger of the two scores
+            if (next >= 0) {
+                const float score = fmaxf(my_key - a.bias[lds.chosen[l]], next_key - a.bias[next]);
+                const float far = (a.sigmoid ? 0x1p-20f : 0x1p-15f * fabsf(score)) + 0x1p-21f * fmaxf(fabsf(my_key), fabsf(next_key));
+                if (!(my_key - next_key > far)) sure = false;
+            }
         }
         return over_token<LPT>((int)sure, Smaller{}) != 0;
     }
@@ -400,30 +436,50 @@ template <int DT, int LPT, int EPL> __global__ __launch_bounds__(256) void route
 }
 
 // ------------------------------------------------------------------------------------------
-template <int DT, int LPT, int EPL> static hipError_t launch_one(bool grad, const RouteArgs &a, hipStream_t st)
+template <int DT, int LPT, int EPL> static hipError_t launch_one(const RouteArgs &a, hipStream_t st)
 {
     const dim3 grid((unsigned)(((long)a.tokens + 256 / LPT - 1) / (256 / LPT)));
-    if (grad)              hipLaunchKernelGGL((route_grad_kernel<DT, LPT, EPL>), grid, dim3(256), 0, st, a);
-    else if (a.groups > 1) hipLaunchKernelGGL((route_kernel<DT, LPT, EPL, true>), grid, dim3(256), 0, st, a);
-    else                   hipLaunchKernelGGL((route_kernel<DT, LPT, EPL, false>), grid, dim3(256), 0, st, a);
+    if (a.groups > 1) hipLaunchKernelGGL((route_kernel<DT, LPT, EPL, true>), grid, dim3(256), 0, st, a);
+    else              hipLaunchKernelGGL((route_kernel<DT, LPT, EPL, false>), grid, dim3(256), 0, st, a);
     return hipGetLastError();
 }
-template <int DT> static hipError_t launch_type(bool grad, const RouteArgs &a, hipStream_t st)
+template <int DT, int LPT, int EPL> static hipError_t launch_grad(const RouteArgs &a, hipStream_t st)
 {
-    // sixteen lanes to a token where they do: four tokens then share a wave's instructions
-    if (a.experts <= 256 && a.topk < 16) {
-        if (a.experts <= 32)  return launch_one<DT, 16, 2>(grad, a, st);
-        if (a.experts <= 64)  return launch_one<DT, 16, 4>(grad, a, st);
-        if (a.experts <= 128) return launch_one<DT, 16, 8>(grad, a, st);
-        return launch_one<DT, 16, 16>(grad, a, st);
-    }
-    if (a.experts <= 256) return launch_one<DT, 64, 4>(grad, a, st);
-    if (a.experts <= 512) return launch_one<DT, 64, 8>(grad, a, st);
-    return launch_one<DT, 64, 16>(grad, a, st);
+    hipLaunchKernelGGL((route_grad_kernel<DT, LPT, EPL>), dim3((unsigned)(((long)a.tokens + 256 / LPT - 1) / (256 / LPT))), dim3(256), 0, st, a);
+    return hipGetLastError();
 }
+template <int DT> static hipError_t launch_type(const RouteArgs &a, hipStream_t st)
+{
+    // Many tokens of few experts: sixteen lanes to a token, four of which share a wave's instructions.  Else a wave, with shorter lists in its lanes.  (us, 8 choices, sixteen lanes / a wave: softmax,
+    // 12608 tokens 64 experts in 8 groups 9.7 / 14.8, 128 experts 6.2 / 9.5, 256 in 8 groups 22.6 / 22.8; sigmoid with bias, 12608 x 256 28.1 / 24.4, 4096 x 64 8.6 / 8.2, 4096 x 128 9.5 / 6.7,
+    // 2048 x 256 20.0 / 11.0; a second look in 64 bits by a few tokens is in those of the bias.)
+    if (a.experts <= 128 && a.topk < 16 && a.tokens > 4096) {
+        if (a.experts <= 32)  return launch_one<DT, 16, 2>(a, st);
+        if (a.experts <= 64)  return launch_one<DT, 16, 4>(a, st);
+        return launch_one<DT, 16, 8>(a, st);
+    }
+    if (a.experts <= 64)  return launch_one<DT, 64, 1>(a, st);
+    if (a.experts <= 128) return launch_one<DT, 64, 2>(a, st);
+    if (a.experts <= 256) return launch_one<DT, 64, 4>(a, st);
+    if (a.experts <= 512) return launch_one<DT, 64, 8>(a, st);
+    return launch_one<DT, 64, 16>(a, st);
+}
+template <int DT> static hipError_t launch_grad_type(const RouteArgs &a, hipStream_t st)
+{
+    if (a.experts <= 256 && a.topk <= 16) {
+        if (a.experts <= 32)  return launch_grad<DT, 16, 2>(a, st);
+        if (a.experts <= 64)  return launch_grad<DT, 16, 4>(a, st);
+        if (a.experts <= 128) return launch_grad<DT, 16, 8>(a, st);
+        return launch_grad<DT, 16, 16>(a, st);
+    }
+    if (a.experts <= 256) return launch_grad<DT, 64, 4>(a, st);
+    if (a.experts <= 512) return launch_grad<DT, 64, 8>(a, st);
+    return launch_grad<DT, 64, 16>(a, st);
+}
+template <int DT> static hipError_t launch_either(bool grad, const RouteArgs &a, hipStream_t st) { return grad ? launch_grad_type<DT>(a, st) : launch_type<DT>(a, st); }
 hipError_t launch_route(int dt, bool grad, const RouteArgs &a, hipStream_t st)
 {
-    return dt == DT_F32 ? launch_type<DT_F32>(grad, a, st) : dt == DT_BF16 ? launch_type<DT_BF16>(grad, a, st) : launch_type<DT_F16>(grad, a, st);
+    return dt == DT_F32 ? launch_either<DT_F32>(grad, a, st) : dt == DT_BF16 ? launch_either<DT_BF16>(grad, a, st) : launch_either<DT_F16>(grad, a, st);
 }
 
 }  // namespace abft
