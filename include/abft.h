@@ -311,7 +311,8 @@ typedef struct {
 int abft_route(const void *logits, abft_dtype dtype, const abft_routing *q, int32_t *expert, float *weight, void *stream);
 
 /* Its backward pass: dlogits (type of logits, rows ldd apart) from dweight [tokens][topk], for the choices expert as abft_route wrote them (entries outside
- * [0, experts), and of masked logits, have no part; of an expert named twice by a token one counts).  Choices are constants, as is the bias.  All of a token's row is
+ * [0, experts), and of masked logits, have no part; an expert named twice by a token
+ * counts twice, in the sums too).  Choices are constants, as is the bias.  All of a token's row is
  * written, zeros included; what lies between experts and ldd stays.  A token with a logit that is NaN or +Inf gets NaN. */
 int abft_route_grad(const void *logits, abft_dtype dtype, const abft_routing *q, const int32_t *expert, const float *dweight, void *dlogits,
                     int64_t ldd, void *stream);
@@ -329,12 +330,12 @@ int abft_gather_rows(const void *X, abft_dtype dtype, int64_t tokens, int64_t co
 
 /* out[t] = base[t] + the sum over j of weight[t][j] Y[place[t][j]], in fp32, j rising, rounded once; places outside [0, rows) have no part, whatever
  * their weight.  base: NULL, or added first (may be out itself, of the same pitch); weight: NULL, or [tokens][topk]: ones.  ABFT_BF16 or ABFT_F16.  What lies
- * between cols and ldo stays.  tokens * topk <= 2^30. */
+ * between cols and ldo stays.  tokens * topk <= 2^30, cols <= 2^24. */
 int abft_combine_rows(const void *Y, abft_dtype dtype, int64_t rows, int64_t cols, int64_t ldy, const int32_t *place, const float *weight,
                       int64_t tokens, int32_t topk, const void *base, int64_t ldb, void *out, int64_t ldo, void *stream);
 
 /* Its backward pass: dY[place[t][j]] = weight[t][j] dout[t], rounded once, and dweight[t][j] = the dot of dout[t] and Y[place[t][j]], in fp32, 0 where the place is
- * outside [0, rows).  Rows of dY that no place names stay as they are; a row named twice holds one of the two.  dY or dweight (then Y too) may be NULL.  (base's
+ * outside [0, rows).  Rows of dY that no place names stay as they are; each element of a row named twice is one of the two's.  dY or dweight (then Y too) may be NULL.  (base's
  * gradient is dout.) */
 int abft_combine_rows_grad(const void *dout, abft_dtype dtype, int64_t tokens, int64_t cols, int64_t ldd, const int32_t *place, const float *weight,
                            int32_t topk, const void *Y, int64_t rows, int64_t ldy, void *dY, int64_t lddy, float *dweight, void *stream);

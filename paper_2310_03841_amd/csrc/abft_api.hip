@@ -1126,7 +1126,7 @@ static int combine_args(int dtype, const void *Y, int64_t rows, int64_t cols, in
 {
     if (!is_half(dtype) || topk < 1) return ABFT_EINVAL;
     const int rc = check_rows(rows, cols, Y ? ldy : cols, 1);
-    if (rc == ABFT_ESHAPE || tokens < 1 || tokens > (1 << 30) || tokens * (int64_t)topk > (1 << 30)) return ABFT_ESHAPE;
+    if (rc == ABFT_ESHAPE || cols > (1 << 24) || tokens < 1 || tokens > (1 << 30) || tokens * (int64_t)topk > (1 << 30)) return ABFT_ESHAPE;
     if (!place) return ABFT_EINVAL;
     if ((Y && (!aligned16(Y) || (ldy * 2) % 16)) || ((uintptr_t)place & 3u) || ((uintptr_t)weight & 3u)) return ABFT_EALIGN;
     memset(a, 0, sizeof(*a));

@@ -421,7 +421,7 @@ template <int DT, int LPT, int EPL> __global__ __launch_bounds__(256) void route
     } else {
         d = dw;
     }
-    if (there) g[e] = d;
+    if (there) atomicAdd(g + e, d);                              // (in LDS: each has its own place, unless a token names an expert twice)
     wave_lds_fence();
     const float D = spread ? over_token<LPT>(there ? dw * expf(xe - m) / sum : 0.f, Plus{}) : 0.f;
     if (t >= a.tokens) return;

@@ -317,6 +317,28 @@ def test_gradient_takes_no_part_of_choices_outside():
         assert np.allclose(got[t], want, rtol=0, atol=64 * U32 * 8)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("score", [ab.ABFT_SOFTMAX, ab.ABFT_SIGMOID])
+@pytest.mark.parametrize("normalise", [True, False])
+@pytest.mark.parametrize("E,topk", [(20, 4), (300, 20)])
+def test_gradient_of_an_expert_named_twice(score, normalise, E, topk):
+    """Its choices count one by one, as differentiating the weights with the choices held says.  A share is off by 4 rel (as above) of at most twice the largest gradient of a
+    weight, topk of them add up at most."""
+    r = Route("f32", 9, E, topk, score=score, normalise=normalise, scale=1.5, seed=E)
+    r.forward()
+    r.ids[1, 2] = r.ids[1, 0]
+    r.ids[2, :] = r.ids[2, topk - 1]
+    r.ids[3, 1:4] = 7
+    r.backward()
+    x = torch.tensor(r.x, requires_grad=True)
+    s = torch.sigmoid(x) if score else torch.softmax(x, dim=1)
+    w = s.gather(1, r.ids.cpu().long())
+    (1.5 * (w / w.sum(dim=1, keepdim=True) if normalise else w) * r.dw.double().cpu()).sum().backward()
+    rel = (4 * np.abs(r.x).max() + E + 16) * U32
+    tol = 4 * rel * 2 * 1.5 * float(r.dw.abs().max()) * topk
+    assert np.abs(r.dx[:, :E].double().cpu().numpy() - x.grad.numpy()).max() <= tol
+
+
 # ------------------------------------------------------------------------------------------ entries by group
 def plain_group_rows(group, groups):
     inside = (group >= 0) & (group < groups)
@@ -767,10 +789,11 @@ def test_refusals_of_rows_need_no_gpu():
     good = dict(Y=P, dtype=ab.ABFT_BF16, rows=8, cols=8, ldy=8, place=P, weight=P, tokens=4, topk=2, base=P, ldb=8, out=P, ldo=8, stream=0)
     common = [(dict(dtype=ab.ABFT_I8), E), (dict(topk=0), E), (dict(tokens=0), S), (dict(rows=0), S), (dict(cols=0), S), (dict(tokens=1 << 29, topk=3), S), (dict(place=None), E), (dict(place=P + 2), A),
               (dict(weight=P + 2), A), (dict(Y=P + 8), A), (dict(ldy=4), S), (dict(ldy=12), A)]
-    expect(ab.abft_combine_rows, good, common + [(dict(Y=None), E), (dict(out=None), E), (dict(ldo=4), S), (dict(ldo=12), A), (dict(ldb=4), S), (dict(ldb=12), A), (dict(base=P + 8), A), (dict(out=P + 8), A)])
+    expect(ab.abft_combine_rows, good, common + [(dict(Y=None), E), (dict(out=None), E), (dict(cols=(1 << 24) + 1, ldy=1 << 25, ldo=1 << 25, ldb=1 << 25), S), (dict(ldo=4), S), (dict(ldo=12), A), (dict(ldb=4), S), (dict(ldb=12), A), (dict(base=P + 8), A), (dict(out=P + 8), A)])
     good = dict(dout=P, dtype=ab.ABFT_BF16, tokens=4, cols=8, ldd=8, place=P, weight=P, topk=2, Y=P, rows=8, ldy=8, dY=P, lddy=8, dweight=P, stream=0)
     expect(ab.abft_combine_rows_grad, good, common + [(dict(dout=None), E), (dict(dY=None, dweight=None), E), (dict(Y=None), E), (dict(ldd=4), S), (dict(ldd=12), A), (dict(lddy=4), S), (dict(lddy=12), A),
-                                                      (dict(dY=P + 8), A), (dict(dout=P + 8), A), (dict(dweight=P + 2), A)])
+                                                      (dict(dY=P + 8), A), (dict(dout=P + 8), A), (dict(dweight=P + 2), A),
+                                                      (dict(cols=(1 << 24) + 1, ldy=1 << 25, ldd=1 << 25, lddy=1 << 25), S)])
 
 
 @pytest.mark.gpu
