@@ -1006,7 +1006,7 @@ extern "C" int abft_mx4_tile_shape(int mode, const abft_shape *s, int *tile_m, i
     Mx4Args g = mx4_args(nullptr, nullptr, nullptr, nullptr, &q, sh);
     GroupKernel k;
     if (!mx4_plan(mode != ABFT_OFF, g, &k)) return ABFT_ESHAPE;
-    mx4_tile_shape(k, g, tile_m, tile_n);
+    mx4_tile_shape(mode != ABFT_OFF, k, g, tile_m, tile_n);
     return ABFT_OK;
 }
 

@@ -46,10 +46,10 @@ static double mx4_few_us(const Mx4Problem &p)
     return 5.1 + (p.protect ? 5.2 + 1e-3 * tiles : 0.0) + std::max(tiles * 48 * p.row / 14.6e6, p.groups * p.N * p.row / 15.2e6);
 }
 
-void mx4_tile_shape(const GroupKernel &k, const Mx4Args &g, int *rows, int *columns)
+void mx4_tile_shape(bool protect, const GroupKernel &k, const Mx4Args &g, int *rows, int *columns)
 {
     *rows = k.kind == GROUP_KERNEL_BIG ? 256 : k.kind == GROUP_KERNEL_FEW ? 16 : 64;
-    *columns = k.kind == GROUP_KERNEL_BIG ? 256 : k.kind == GROUP_KERNEL_FEW ? mx4_few_columns(g) : k.tiles == TILE_64_128 ? 128 : 64;
+    *columns = k.kind == GROUP_KERNEL_BIG ? 256 : k.kind == GROUP_KERNEL_FEW ? mx4_few_columns(protect, g) : k.tiles == TILE_64_128 ? 128 : 64;
 }
 
 bool mx4_plan(bool protect, Mx4Args &g, GroupKernel *k)
@@ -78,8 +78,8 @@ bool mx4_plan(bool protect, Mx4Args &g, GroupKernel *k)
     if (mx4_few_fits(protect, g) && mx4_few_us(p) < us) k->kind = GROUP_KERNEL_FEW;
     if (k->kind == GROUP_KERNEL_BIG) return row_tiles(g.M, g.groups, 128) * ceil_div(g.N, 256) < 1L << 31;      // (a list that its workgroups walk)
     int rows, columns;
-    mx4_tile_shape(*k, g, &rows, &columns);
-    const long wgs = k->kind == GROUP_KERNEL_FEW ? mx4_few_workgroups(g) : ceil_div(row_tiles(g.M, g.groups, rows) * ceil_div(g.N, columns), 8) * 8;
+    mx4_tile_shape(protect, *k, g, &rows, &columns);
+    const long wgs = k->kind == GROUP_KERNEL_FEW ? mx4_few_workgroups(protect, g) : ceil_div(row_tiles(g.M, g.groups, rows) * ceil_div(g.N, columns), 8) * 8;
     return n_pass + wgs <= MAX_GRID_X;
 }
 

@@ -5,8 +5,9 @@
 // bytes (eight blocks) of each of their rows of B at a time, straight into the registers of 16 x 16 MFMAs, whose lanes each take a block and its power
 // of two.  The waves' sums meet in LDS, in a fixed order.
 //
-// Protected, a workgroup sums its rows of A first and multiplies that vector with the elements of B it holds, by vector instructions beside the MFMAs, so that B
-// is read once.  A column that disagrees leaves a mark in cc_obs for the check kernel; the workgroups' shares of the rows' sums lie side by side
+// Protected, a workgroup sums its rows of A first and multiplies that vector with the elements of B it holds, so that B is read once.  MFMAs do it too: a block
+// of the vector is split into five terms of 8 bits (e4m3), a power of two each, 2^-5 of the one before it, and a term is a row of the other operand.  The first takes the
+// block's largest sum, below 2^8 of its power, to within 2^3 of that, and each the rest of the one before in the same way, so what is left behind is below 2^-25 of the largest.  A column that disagrees leaves a mark in cc_obs for the check kernel; the workgroups' shares of the rows' sums lie side by side
 // for it.
 #include <algorithm>
 
@@ -21,13 +22,20 @@ struct Mx4FewArgs {
     const uint32_t *b_max;
     float tau_k, tau_cols;                  // 1e-3 K; > 0: instead of tau_k max|A| max|B|
     uint32_t *shares;                       // [tiles_n * NB][M]
-    int sums_off;                           // where the column sums of A lie in LDS, behind what the waves exchange
+    int sums_off;                           // where the terms of the column sums of A lie in LDS, behind what the waves exchange
 };
+
+// of a block of e^T A
+constexpr int TERMS = 5;
+constexpr int mx4_few_term_bytes(int K) { return K / 16 * (TERMS * 32 + 8); }          // K: bytes
 
 template <int NB> constexpr int mx4_few_part_bytes() { return 4 * NB * 64 * 16 + 4 * NB * 16 * 4 + 16; }
 
+// Waves of a SIMD that there are to be registers for.
+constexpr int few_waves(bool protect, int nb, int u) { return !protect || u == 4 ? 1 : nb == 4 ? 4 : u == 1 ? 5 : 4; }
+
 // U: pieces of 128 bytes of a row that a wave has on their way
-template <int OT, bool PROT, int NB, int U> __global__ __launch_bounds__(256) void gemm_mx4_few_kernel(Mx4FewArgs f)
+template <int OT, bool PROT, int NB, int U> __global__ __launch_bounds__(256, few_waves(PROT, NB, U)) void gemm_mx4_few_kernel(Mx4FewArgs f)
 {
     constexpr int BN = 16 * NB;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
@@ -40,7 +48,7 @@ template <int OT, bool PROT, int NB, int U> __global__ __launch_bounds__(256) vo
         if ((int)blockIdx.x < g.n_pass) {
             GroupTile t;
             if (find_tile<4 * PASS_ROWS>(g, g.pass_win, g.pass_inv, (int)blockIdx.x, &t, g.pass_log2))
-                mx4_pass<4, false>(g, t.e, t.first, t.rows, t.tm * 4 * PASS_ROWS << g.pass_log2, g.pass_log2, t.tn, smem);
+                mx4_pass<4, false, 2>(g, t.e, t.first, t.rows, t.tm * 4 * PASS_ROWS << g.pass_log2, g.pass_log2, t.tn, smem);
             return;
         }
     }
@@ -61,10 +69,9 @@ template <int OT, bool PROT, int NB, int U> __global__ __launch_bounds__(256) vo
     }
 
     // ---- this wave's pieces: every fourth
-    f32x4 acc[NB];
-    float pred[NB];
+    f32x4 acc[NB], pred[NB];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) { acc[nb] = f32x4{0.f, 0.f, 0.f, 0.f}; pred[nb] = 0.f; }
+    for (int nb = 0; nb < NB; ++nb) { acc[nb] = pred[nb] = f32x4{0.f, 0.f, 0.f, 0.f}; }
     i32x4 a[U][2], b[U][2][NB];
     uint2 as[U], bs[U][NB];
     auto load = [&](int p0) __attribute__((always_inline)) {
@@ -84,42 +91,69 @@ template <int OT, bool PROT, int NB, int U> __global__ __launch_bounds__(256) vo
             as[u] = *reinterpret_cast<const uint2 *>(asc + (p0 + 4 * u) * 8);
         }
     };
+    // (what the sums of A below begin with is asked for first: loads come back in the order they were asked for)
+    uint32_t ax[4], as4[4];
+    auto load_rows = [&](int i, int r0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const long r = min(r0 + j, rows - 1);
+            ax[j] = *reinterpret_cast<const uint32_t *>(At + r * g.lda + (i >> 3) * 16 + ((i & 7) >> 1) * 4);
+            as4[j] = St[r * g.ld_sa + (i >> 3)];
+        }
+    };
+    if (PROT && tid < nch * 8) load_rows(tid, 0);
+    const float b_top = PROT && f.tau_cols <= 0.f ? __uint_as_float(f.b_max[t.e]) : 0.f;
     if (wave < pairs) load(wave);
 
-    // ---- e^T A of the tile's rows, in fp32, a block's 32 side by side: a thread to four columns of a block
-    float *const sums = reinterpret_cast<float *>(smem + f.sums_off);
+    // ---- e^T A of the tile's rows, in fp32, as eight-bit terms: a thread to four columns of a block
+    uint8_t *const terms = smem + f.sums_off, *const powers = terms + nch * TERMS * 32;
     float *const tops = reinterpret_cast<float *>(smem + mx4_few_part_bytes<NB>() - 16);
     if constexpr (PROT) {
         float top = 0.f;
         for (int i = tid; i < nch * 8; i += 256) {
-            const int c = i >> 3, w = (i & 7) >> 1, half = i & 1;
+            const int c = i >> 3, half = i & 1;
             f32x4 sum = {0.f, 0.f, 0.f, 0.f};
             for (int r0 = 0; r0 < rows; r0 += 4) {
-                uint32_t x[4], s[4];
+                if (i != tid || r0) load_rows(i, r0);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const long r = min(r0 + j, rows - 1);
-                    x[j] = *reinterpret_cast<const uint32_t *>(At + r * g.lda + c * 16 + 4 * w);
-                    s[j] = St[r * g.ld_sa + c];
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t v = half ? x[j] >> 16 : x[j];
-                    const f32x2 p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, mx4_unit(s[j]), 0), q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, mx4_unit(s[j]), 1);
+                    const uint32_t v = half ? ax[j] >> 16 : ax[j];
+                    const f32x2 p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, mx4_unit(as4[j]), 0), q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, mx4_unit(as4[j]), 1);
                     if (r0 + j < rows) {
                         sum += f32x4{p[0], p[1], q[0], q[1]};
                         top = fmaxf(fmaxf(fmaxf(top, fabsf(p[0])), fmaxf(fabsf(p[1]), fabsf(q[0]))), fabsf(q[1]));
                     }
                 }
             }
-            *reinterpret_cast<f32x4 *>(sums + 4 * i) = sum;
+            // the exponent of the block's largest: over the eight threads of a block
+            uint32_t most = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) most = max(most, __float_as_uint(sum[j]) & 0x7FFFFFFFu);
+            most = max(most, (uint32_t)dpp_mov<0xB1>((int)most));            // lane ^ 1
+            most = max(most, (uint32_t)dpp_mov<0x4E>((int)most));            // lane ^ 2
+            most = max(most, (uint32_t)dpp_mov<0x141>((int)most));           // i <-> 7 - i inside 8 lanes
+            const int field = (int)(most >> 23);
+#pragma unroll
+            for (int p = 0; p < TERMS; ++p) {
+                const uint32_t power = field == 255 ? 255u : (uint32_t)max(field - 7 - 5 * p, 0);
+                const float unit = mx4_unit(power);
+                s16x2 o = {0, 0};
+                o = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(o, sum[0], sum[1], unit, false);
+                o = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(o, sum[2], sum[3], unit, true);
+                const int word = __builtin_bit_cast(int, o);
+                *reinterpret_cast<int *>(terms + (c * TERMS + p) * 32 + (i & 7) * 4) = word;
+                if ((i & 7) == p) powers[c * 8 + p] = (uint8_t)power;
+                const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, unit, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, unit, true);
+                sum -= f32x4{lo[0], lo[1], hi[0], hi[1]};
+            }
         }
         top = wave_max(top);
         if (lane == 0) tops[wave] = top;
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
     for (int p0 = wave; p0 < pairs; p0 += 4 * U) {
-        if (p0 != wave) load(p0);
+        if constexpr (U > 1)                                     // (one piece is all there is for U = 1)
+            if (p0 != wave) load(p0);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (u && p0 + 4 * u >= pairs) break;
@@ -130,22 +164,23 @@ template <int OT, bool PROT, int NB, int U> __global__ __launch_bounds__(256) vo
                 const bool in = ch < nch;
                 const i32x4 av = in ? a[u][h] : i32x4{0, 0, 0, 0};
                 const uint32_t asv = in ? ((h ? as[u].y : as[u].x) >> (8 * piece)) & 0xFFu : 0u;
-                const float *s = sums + (in ? ch : nch - 1) * 32;
+                i32x8 ev = {0, 0, 0, 0, 0, 0, 0, 0};
+                uint32_t esv = 0;
+                if (PROT && i16 < TERMS) {
+                    const int c = ch - piece + (piece >> 1);
+                    const uint8_t *at = terms + (c * TERMS + i16) * 32 + (piece & 1) * 16;
+                    i32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+                    if (c < nch) lo = *reinterpret_cast<const i32x4 *>(at);
+                    if (c + 2 < nch) hi = *reinterpret_cast<const i32x4 *>(at + 2 * TERMS * 32);
+                    ev = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    if (in) esv = powers[ch * 8 + i16];
+                }
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
                     const i32x4 bv = in ? b[u][h][nb] : i32x4{0, 0, 0, 0};
                     const uint32_t bsv = in ? ((h ? bs[u][nb].y : bs[u][nb].x) >> (8 * piece)) & 0xFFu : 0u;
                     acc[nb] = mfma16_mx4<0>(bv, av, acc[nb], bsv, asv);
-                    if constexpr (PROT) {
-                        float v[32];
-                        mx4_values(bv, mx4_unit(bsv), v);
-#pragma unroll
-                        for (int q4 = 0; q4 < 8; ++q4) {
-                            const f32x4 sv = *reinterpret_cast<const f32x4 *>(s + 4 * q4);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) pred[nb] = __builtin_fmaf(v[4 * q4 + i], sv[i], pred[nb]);
-                        }
-                    }
+                    if constexpr (PROT) pred[nb] = mfma16_mx4_f8(bv, ev, pred[nb], bsv, esv);
                 }
             }
         }
@@ -157,8 +192,10 @@ template <int OT, bool PROT, int NB, int U> __global__ __launch_bounds__(256) vo
     for (int nb = 0; nb < NB; ++nb) {
         *reinterpret_cast<f32x4 *>(smem + ((wave * NB + nb) * 64 + lane) * 16) = acc[nb];
         if constexpr (PROT) {
-            const float s = add_xor32(add_xor16(pred[nb]));
-            if (lane < 16) ppart[(wave * NB + nb) * 16 + lane] = s;
+            f32x4 p;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = row16_sum(pred[nb][i]);           // (of the terms)
+            if (i16 == 0) *reinterpret_cast<f32x4 *>(ppart + (wave * NB + nb) * 16 + 4 * piece) = p;
         }
     }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -201,7 +238,7 @@ template <int OT, bool PROT, int NB, int U> __global__ __launch_bounds__(256) vo
         if (lane < rows && 16 * nb + n0 < N) f.shares[(long)(t.tn * NB + nb) * g.M + t.first + m0 + lane] = as_word(rsum);
         // a column's sum over the sixteen lanes of its rows, against its prediction
         const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-        const float tol = f.tau_cols > 0.f ? f.tau_cols : f.tau_k * top * __uint_as_float(f.b_max[t.e]);
+        const float tol = f.tau_cols > 0.f ? f.tau_cols : f.tau_k * top * b_top;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float obs = row16_sum(v[i]);
@@ -214,20 +251,23 @@ template <int OT, bool PROT, int NB, int U> __global__ __launch_bounds__(256) vo
 }
 
 // ------------------------------------------------------------------------------------------
-constexpr int MX4_FEW_MAX_SUMS = 64 * 1024;      // bytes of LDS for the column sums of A
+constexpr int MX4_FEW_MAX_K = 8 * 1024;           // bytes of a row, protected: the column sums of A are kept in LDS
 
-bool mx4_few_fits(bool protect, const Mx4Args &g) { return !protect || (g.M <= 32L * g.groups && g.K * 8L <= MX4_FEW_MAX_SUMS); }
+bool mx4_few_fits(bool protect, const Mx4Args &g) { return !protect || (g.M <= 32L * g.groups && g.K <= MX4_FEW_MAX_K); }
 
-// 32 columns to a workgroup, which reads its rows of A once for both halves, unless that leaves compute units without one.
-int mx4_few_columns(const Mx4Args &g)
+static int few_pieces(const Mx4Args &g) { return (g.K + 4 * SLAB_BYTES - 1) / (4 * SLAB_BYTES); }       // of a wave
+// 32 columns to a workgroup, which reads its rows of A once for both halves, unless that leaves compute units without one; protected 64, while their
+// registers leave room for several workgroups on a compute unit.
+int mx4_few_columns(bool protect, const Mx4Args &g)
 {
-    const long rows = ((long)g.M + g.groups - 1) / g.groups;                 // of a group on average
-    return std::min(g.M, g.groups) * ((rows + 15) / 16) * ((g.N + 31) / 32) >= 512 ? 32 : 16;
+    const long rows = ((long)g.M + g.groups - 1) / g.groups, tiles = std::min(g.M, g.groups) * ((rows + 15) / 16);     // rows: of a group on average
+    if (protect && few_pieces(g) == 1 && tiles * ((g.N + 63) / 64) >= 512) return 64;
+    return tiles * ((g.N + 31) / 32) >= 512 ? 32 : 16;
 }
 
-long mx4_few_workgroups(const Mx4Args &g)
+long mx4_few_workgroups(bool protect, const Mx4Args &g)
 {
-    const int bn = mx4_few_columns(g);
+    const int bn = mx4_few_columns(protect, g);
     return ((g.groups == 1 ? (g.M + 15) / 16 : g.M / 16 + std::min(g.M, g.groups)) * (long)((g.N + bn - 1) / bn) + 7) / 8 * 8;
 }
 
@@ -237,12 +277,12 @@ template <int OT, bool PROT, int NB, int U> static hipError_t launch_few_of(Mx4F
     auto kern = gemm_mx4_few_kernel<OT, PROT, NB, U>;
     f.sums_off = (mx4_few_part_bytes<NB>() + 15) & ~15;
     int smem = f.sums_off;
-    if (PROT) smem = std::max(smem + g.K * 8, mx4_pass_lds<4, false>());
-    const hipError_t e = ensure_max_lds(reinterpret_cast<const void *>(kern), MX4_FEW_MAX_SUMS + 32 * 1024);
+    if (PROT) smem = std::max(smem + mx4_few_term_bytes(g.K), mx4_pass_lds<4, false>());
+    const hipError_t e = ensure_max_lds(reinterpret_cast<const void *>(kern), mx4_few_term_bytes(MX4_FEW_MAX_K) + 32 * 1024);
     if (e != hipSuccess) return e;
     g.tiles_n = (g.N + 16 * NB - 1) / (16 * NB);
     g.group_inv = map_inverse(g.tiles_n);
-    const long wgs = (PROT ? g.n_pass : 0) + mx4_few_workgroups(g);
+    const long wgs = (PROT ? g.n_pass : 0) + mx4_few_workgroups(PROT, g);
     hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), smem, st, f);
     return hipGetLastError();
 }
@@ -250,15 +290,16 @@ template <int OT, bool PROT, int NB, int U> static hipError_t launch_few_of(Mx4F
 // Registers for no more pieces than a wave has: with few, more waves share a SIMD, and they have more on their way together.
 template <int OT, bool PROT, int NB> static hipError_t launch_few_one(Mx4FewArgs &f, hipStream_t st)
 {
-    const int pieces = (f.g.K + 4 * SLAB_BYTES - 1) / (4 * SLAB_BYTES);      // of a wave
+    const int pieces = few_pieces(f.g);
     return pieces <= 1 ? launch_few_of<OT, PROT, NB, 1>(f, st) : pieces <= 2 ? launch_few_of<OT, PROT, NB, 2>(f, st) : launch_few_of<OT, PROT, NB, 4>(f, st);
 }
 
 template <int OT> static hipError_t launch_few_type(bool protect, Mx4FewArgs &f, hipStream_t st)
 {
-    const bool wide = mx4_few_columns(f.g) == 32;
-    if (protect) return wide ? launch_few_one<OT, true, 2>(f, st) : launch_few_one<OT, true, 1>(f, st);
-    return wide ? launch_few_one<OT, false, 2>(f, st) : launch_few_one<OT, false, 1>(f, st);
+    const int columns = mx4_few_columns(protect, f.g);
+    if (!protect) return columns == 32 ? launch_few_one<OT, false, 2>(f, st) : launch_few_one<OT, false, 1>(f, st);
+    if (columns == 64) return launch_few_of<OT, true, 4, 1>(f, st);
+    return columns == 32 ? launch_few_one<OT, true, 2>(f, st) : launch_few_one<OT, true, 1>(f, st);
 }
 
 hipError_t launch_mx4_few(int ot, bool protect, Mx4Args &g, const uint32_t *b_max, float tau_k, float tau_cols, hipStream_t st)

@@ -10,6 +10,7 @@ namespace abft {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 template <> struct Traits<DT_MX4> {
@@ -30,6 +31,13 @@ template <int BYTE> __device__ __forceinline__ f32x16 mfma_mx4(const i32x4 &a, c
 template <int BYTE> __device__ __forceinline__ f32x4 mfma16_mx4(const i32x4 &a, const i32x4 &b, const f32x4 &c, uint32_t sa, uint32_t sb)
 {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx4_operand(a), mx4_operand(b), c, 4, 4, BYTE, (int)sa, BYTE, (int)sb);
+}
+
+// b: of 8 bits (e4m3); a lane's first sixteen are those of half a block and its others of the block two on (lane 16 q + i: half q % 2 of block q / 2), its power of two that of
+// block q all the same
+__device__ __forceinline__ f32x4 mfma16_mx4_f8(const i32x4 &a, const i32x8 &b, const f32x4 &c, uint32_t sa, uint32_t sb)
+{
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx4_operand(a), b, c, 4, 0, 0, (int)sa, 0, (int)sb);
 }
 
 // 2^(s - 127) as the conversions take it (they look at its exponent alone).

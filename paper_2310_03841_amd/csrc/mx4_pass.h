@@ -14,8 +14,8 @@ namespace abft {
 // LDS: each wave's sums of the window's columns (SUMS: e^T A is wanted too), and a maximum to a wave
 template <int WAVES, bool SUMS = true> constexpr int mx4_pass_lds() { return (SUMS ? WAVES * PASS_BYTES * 2 * 4 : 0) + WAVES * 4; }
 
-// Rows row0 .. of group e (which has `rows` from `first` on), 2^log2 trips of WAVES * PASS_ROWS of them at most.
-template <int WAVES, bool SUMS = true> __device__ __forceinline__ void mx4_pass(const Mx4Args &g, int e, int first, int rows, int row0, int log2, int win, uint8_t *smem)
+// Rows row0 .. of group e (which has `rows` from `first` on), 2^log2 times WAVES * PASS_ROWS of them at most, ROWS of a wave on their way together.
+template <int WAVES, bool SUMS = true, int ROWS = PASS_ROWS> __device__ __forceinline__ void mx4_pass(const Mx4Args &g, int e, int first, int rows, int row0, int log2, int win, uint8_t *smem)
 {
     constexpr int COLS = PASS_BYTES * 2;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -35,19 +35,19 @@ template <int WAVES, bool SUMS = true> __device__ __forceinline__ void mx4_pass(
 #pragma unroll
         for (int i = 0; i < 4; ++i) b[4 * q4 + i] = __uint_as_float((uint32_t)v[i]);
     }
-    for (int r0 = row0 + wave * PASS_ROWS; r0 < upto; r0 += WAVES * PASS_ROWS) {
-        i32x4 x[PASS_ROWS];
-        uint32_t s[PASS_ROWS];
-        float dot[PASS_ROWS];
+    for (int r0 = row0 + wave * ROWS; r0 < upto; r0 += WAVES * ROWS) {
+        i32x4 x[ROWS];
+        uint32_t s[ROWS];
+        float dot[ROWS];
 #pragma unroll
-        for (int u = 0; u < PASS_ROWS; ++u) {
+        for (int u = 0; u < ROWS; ++u) {
             const long r = first + min(r0 + u, rows - 1);
             x[u] = *reinterpret_cast<const i32x4 *>(g.A + r * g.lda + at * 16);
             s[u] = g.sa[r * g.ld_sa + at];
             dot[u] = 0.f;
         }
 #pragma unroll
-        for (int u = 0; u < PASS_ROWS; ++u) {
+        for (int u = 0; u < ROWS; ++u) {
             if (!in || r0 + u >= rows) continue;
             float v[32];
             mx4_values(x[u], mx4_unit(s[u]), v);
@@ -61,11 +61,11 @@ template <int WAVES, bool SUMS = true> __device__ __forceinline__ void mx4_pass(
         }
         float mine = 0.f;
 #pragma unroll
-        for (int u = 0; u < PASS_ROWS; ++u) {
+        for (int u = 0; u < ROWS; ++u) {
             const float t = wave_sum(dot[u]);
             mine = lane == u ? t : mine;
         }
-        if (lane < PASS_ROWS && r0 + lane < rows) atomic_add_word(g.rc_pred + first + r0 + lane, mine);
+        if (lane < ROWS && r0 + lane < rows) atomic_add_word(g.rc_pred + first + r0 + lane, mine);
     }
 #pragma unroll
     for (int q4 = 0; q4 < 8 && SUMS; ++q4)

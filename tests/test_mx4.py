@@ -266,11 +266,12 @@ def test_product_matches_plain(out, ends, N, K):
 # each kernel by name, unprotected and protected: which tiles a problem takes
 KERNELS = {
     (16, 16): ([0, 1, 4, 9], 200, 520),
-    (16, 32): ([0, 2, 2, 22, 24] + list(range(25, 61)), 1030, 264),
+    (16, 32): ([0, 2, 2, 22, 24] + list(range(25, 61)), 1030, 1300),
     (64, 64): ([0, 150, 150, 1201], 200, 1000),
     (64, 128): ([0, 1000, 1530, 2311], 1100, 168),
     (256, 256): ([0, 257, 257, 2900, 3029, 5000], 1546, 768),
 }
+WIDE = ([0, 2, 2, 22, 24] + list(range(25, 61)), 1030, 264)     # protected by 64 columns, else by 32
 DEEP = ([0, 255, 4400], 1090, 2304)                             # tiles of 256 x 256 of more slabs than three, and a last round of halves
 
 
@@ -284,6 +285,7 @@ def test_which_kernel_a_problem_takes():
         for tile, (ends, N, K) in KERNELS.items():
             assert tile_of(ends, N, K, mode) == tile, (tile, mode)
         assert tile_of(*DEEP, mode) == (256, 256)
+        assert tile_of(*WIDE, mode) == (16, 64 if mode else 32)
         # not whole slabs of 256 elements (as blocks of 32 cover them), or fewer than three of them
         for K in (736, 769, 512, 3000):
             assert tile_of(KERNELS[256, 256][0], 1546, K, mode) != (256, 256)
@@ -293,7 +295,7 @@ def test_which_kernel_a_problem_takes():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("out", ["bf16", "f16"])
-@pytest.mark.parametrize("ends,N,K", list(KERNELS.values()) + [DEEP])
+@pytest.mark.parametrize("ends,N,K", list(KERNELS.values()) + [WIDE, DEEP])
 def test_each_kernel(out, ends, N, K):
     """Clean, with a bias; flips all over its tiles; blocks of NaN."""
     p = Product(ends, N, K, M=ends[-1] + 2, out=out, bias=True, seed=K)
@@ -324,6 +326,28 @@ def test_each_kernel(out, ends, N, K):
         p.check(clean=False)
         rf, cf = p.row_flag.cpu().numpy(), p.col_flag.cpu().numpy()
         assert rf[r] == 1 and cf[c] == 1 and rf[:ends[g]].sum() == 0 and cf[:g * N].sum() == 0
+    finally:
+        p.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("spread", [3, 40])
+@pytest.mark.parametrize("ends,N,K", [([0, 1], 40, 31), ([0, 5, 16], 100, 520), ([0, 3, 24, 40], 70, 1300), ([0, 2], 16, 9000), WIDE, KERNELS[16, 32]])
+def test_predictions_of_few_rows_are_as_near_as_fp32(ends, N, K, spread):
+    """A tile's e^T A is taken as terms of 8 bits, of which 2^-25 of a block's largest sum is left behind: as fp32 does.  With R rows to a tile, every product of a prediction or a sum is at
+    most R max|A| max|B|; the additions of a wave's K / 512 MFMAs, those inside one (to some 2^-17 of its largest product), and the last ones over waves and rows stay
+    below n = K / 512 + 8 steps of 2^-20 K R max|A| max|B|.  Tolerances of 1e-3 K max|A| max|B| lie 5 times and more above."""
+    assert tile_of(ends, N, K, ab.ABFT_DETECT)[0] == 16
+    p = Product(ends, N, K, seed=K + spread)
+    try:
+        rng = np.random.default_rng(1)
+        p.sA[:, :(K + 31) // 32] = rng.integers(127 - spread, 128 + spread, (p.M, (K + 31) // 32))
+        p.upload()
+        R = min(16, int(np.diff(ends).max()))
+        a, b = values(p.A, p.sA, K), values(p.B, p.sB, K)
+        tau_cols = (K / 512 + 8) * 2.0 ** -20 * K * R * np.abs(a).max() * np.abs(b).max()
+        p.run(ab.ABFT_DETECT, tau_cols=tau_cols)
+        p.check()
     finally:
         p.close()
 
