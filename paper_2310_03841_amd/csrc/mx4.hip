@@ -3,7 +3,9 @@
 // A block's power of two is 2^e, e the exponent of its largest magnitude less 2, that of the largest element 6 = 1.5 2^2 (not below -127); x 2^-e goes to
 // the nearest element, ties to the even code, and what lies above 6 (up to 8) to 6.  x 2^-e is exact, so one rounding is all there is.
 //
-// Bound by memory: two bytes read and about half a byte written per element, and the other way round.  Four lanes to a block, 16 bytes of the 16-bit row each.
+// Bound by memory: two bytes read and about half a byte written per element, and the other way round.  Four lanes to a block, 16 bytes of the 16-bit row each, all of a row's loads
+// ahead.  12608 rows of 4096 bf16, gathered from 6304 tokens: 28 us (52 MB read, most of it twice, 27 written), and back 22 us (131 MB, 6.0 TB/s); both in turn
+// 50 us, with elements found by comparisons and fewer loads on their way 75.  Stores past the caches gain nothing.
 #include "abft_device.h"
 #include "gemm_epilogue.h"
 #include "mx4_device.h"
