@@ -6,8 +6,7 @@
 // of two.  The waves' sums meet in LDS, in a fixed order.
 //
 // Protected, a workgroup sums its rows of A first and multiplies that vector with the elements of B it holds, so that B is read once.  MFMAs do it too: a block
-// of the vector is split into five terms of 8 bits (e4m3), a power of two each, 2^-5 of the one before it, and a term is a row of the other operand.  The first takes the
-// block's largest sum, below 2^8 of its power, to within 2^3 of that, and each the rest of the one before in the same way, so what is left behind is below 2^-25 of the largest.  A
+// of the vector is split into five terms of 8 bits (mx4_put_terms), and a term is a row of the other operand.  A
 // column that disagrees leaves a mark in cc_obs for the check kernel; the workgroups' shares of the rows' sums lie side by side for it.
 //
 // 32 tokens, 32 experts of 4096 x 1024 (us on the card): 10.1, protected 12.9 by 64 columns, for fewer of those sums, and 13.2 by 32; with the vector multiplied by vector instructions
@@ -28,10 +27,6 @@ struct Mx4FewArgs {
     uint32_t *shares;                       // [tiles_n * NB][M]
     int sums_off;                           // where the terms of the column sums of A lie in LDS, behind what the waves exchange
 };
-
-// of a block of e^T A
-constexpr int TERMS = 5;
-constexpr int mx4_few_term_bytes(int K) { return K / 16 * (TERMS * 32 + 8); }          // K: bytes
 
 template <int NB> constexpr int mx4_few_part_bytes() { return 4 * NB * 64 * 16 + 4 * NB * 16 * 4 + 16; }
 
@@ -129,27 +124,7 @@ template <int OT, bool PROT, int NB, int U> __global__ __launch_bounds__(256, fe
                     }
                 }
             }
-            // the exponent of the block's largest: over the eight threads of a block
-            uint32_t most = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) most = max(most, __float_as_uint(sum[j]) & 0x7FFFFFFFu);
-            most = max(most, (uint32_t)dpp_mov<0xB1>((int)most));            // lane ^ 1
-            most = max(most, (uint32_t)dpp_mov<0x4E>((int)most));            // lane ^ 2
-            most = max(most, (uint32_t)dpp_mov<0x141>((int)most));           // i <-> 7 - i inside 8 lanes
-            const int field = (int)(most >> 23);
-#pragma unroll
-            for (int p = 0; p < TERMS; ++p) {
-                const uint32_t power = field == 255 ? 255u : (uint32_t)max(field - 7 - 5 * p, 0);
-                const float unit = mx4_unit(power);
-                s16x2 o = {0, 0};
-                o = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(o, sum[0], sum[1], unit, false);
-                o = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(o, sum[2], sum[3], unit, true);
-                const int word = __builtin_bit_cast(int, o);
-                *reinterpret_cast<int *>(terms + (c * TERMS + p) * 32 + (i & 7) * 4) = word;
-                if ((i & 7) == p) powers[c * 8 + p] = (uint8_t)power;
-                const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, unit, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, unit, true);
-                sum -= f32x4{lo[0], lo[1], hi[0], hi[1]};
-            }
+            mx4_put_terms(sum, i & 7, terms + c * TERMS * 32, powers + c * 8);
         }
         top = wave_max(top);
         if (lane == 0) tops[wave] = top;
@@ -168,17 +143,9 @@ template <int OT, bool PROT, int NB, int U> __global__ __launch_bounds__(256, fe
                 const bool in = ch < nch;
                 const i32x4 av = in ? a[u][h] : i32x4{0, 0, 0, 0};
                 const uint32_t asv = in ? ((h ? as[u].y : as[u].x) >> (8 * piece)) & 0xFFu : 0u;
-                i32x8 ev = {0, 0, 0, 0, 0, 0, 0, 0};
-                uint32_t esv = 0;
-                if (PROT && i16 < TERMS) {
-                    const int c = ch - piece + (piece >> 1);
-                    const uint8_t *at = terms + (c * TERMS + i16) * 32 + (piece & 1) * 16;
-                    i32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
-                    if (c < nch) lo = *reinterpret_cast<const i32x4 *>(at);
-                    if (c + 2 < nch) hi = *reinterpret_cast<const i32x4 *>(at + 2 * TERMS * 32);
-                    ev = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    if (in) esv = powers[ch * 8 + i16];
-                }
+                i32x8 ev;
+                uint32_t esv;
+                if constexpr (PROT) mx4_get_terms(terms, powers, ch - piece, nch, lane, ev, esv);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
                     const i32x4 bv = in ? b[u][h][nb] : i32x4{0, 0, 0, 0};
@@ -281,8 +248,8 @@ template <int OT, bool PROT, int NB, int U> static hipError_t launch_few_of(Mx4F
     auto kern = gemm_mx4_few_kernel<OT, PROT, NB, U>;
     f.sums_off = (mx4_few_part_bytes<NB>() + 15) & ~15;
     int smem = f.sums_off;
-    if (PROT) smem = std::max(smem + mx4_few_term_bytes(g.K), mx4_pass_lds<4, false>());
-    const hipError_t e = ensure_max_lds(reinterpret_cast<const void *>(kern), mx4_few_term_bytes(MX4_FEW_MAX_K) + 32 * 1024);
+    if (PROT) smem = std::max(smem + g.K / 16 * TERM_BYTES, mx4_pass_lds<4, false>());
+    const hipError_t e = ensure_max_lds(reinterpret_cast<const void *>(kern), MX4_FEW_MAX_K / 16 * TERM_BYTES + 32 * 1024);
     if (e != hipSuccess) return e;
     g.tiles_n = (g.N + 16 * NB - 1) / (16 * NB);
     g.group_inv = map_inverse(g.tiles_n);

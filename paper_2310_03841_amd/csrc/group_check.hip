@@ -36,20 +36,19 @@ struct Mx4CheckArgs : GroupCheckArgs {
 template <int DT> struct GroupCheckArgsOf { typedef GroupCheckArgs type; };
 template <> struct GroupCheckArgsOf<DT_MX4> { typedef Mx4CheckArgs type; };
 
-// Dots of RW rows of 4-bit B with a vector of 2 K terms, the vector's 32 terms of a lane's block in registers.  LPR lanes to a row, as many as a row has blocks (or 64, and the
-// vector in pieces): 64 / LPR rows at a time, each one's loads ahead of the sums of the one before.  dot[j] belongs to row row0 + j * (64 / LPR) + lane / LPR.
-template <int RW, int LPR> __device__ __forceinline__ void mx4_row_dots(const uint8_t *X, long ld, const uint8_t *S, long lds, int row0, int rows, int K, const uint32_t *vec, float (&dot)[RW])
+// Dots of RW rows of 4-bit B with a vector of 2 K terms, by vector instructions: a block of a row to a lane, and the vector's 32 terms of it in registers, 64 blocks at a time.
+template <int RW> __device__ __forceinline__ void mx4_row_dots(const uint8_t *X, long ld, const uint8_t *S, long lds, int row0, int rows, int K, const uint32_t *vec, float (&dot)[RW])
 {
-    const int lane = threadIdx.x & 63, l = lane % LPR, nb = K / 16;
+    const int lane = threadIdx.x & 63, nb = K / 16;
 #pragma unroll
     for (int j = 0; j < RW; ++j) dot[j] = 0.f;
-    for (int b0 = 0; b0 < nb; b0 += LPR) {
-        const int at = min(b0 + l, nb - 1);
+    for (int b0 = 0; b0 < nb; b0 += 64) {
+        const int at = min(b0 + lane, nb - 1);
         i32x4 v[RW];
         uint32_t s[RW];
 #pragma unroll
         for (int j = 0; j < RW; ++j) {
-            const long r = min(row0 + j * (64 / LPR) + lane / LPR, rows - 1);
+            const long r = min(row0 + j, rows - 1);
             v[j] = *reinterpret_cast<const i32x4 *>(X + r * ld + at * 16);
             s[j] = S[r * lds + at];
         }
@@ -58,7 +57,7 @@ template <int RW, int LPR> __device__ __forceinline__ void mx4_row_dots(const ui
         for (int q4 = 0; q4 < 8; ++q4) {
             const i32x4_word w = *reinterpret_cast<const i32x4_word *>(vec + at * 32 + 4 * q4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) a[4 * q4 + i] = b0 + l < nb ? __uint_as_float((uint32_t)w[i]) : 0.f;
+            for (int i = 0; i < 4; ++i) a[4 * q4 + i] = b0 + lane < nb ? __uint_as_float((uint32_t)w[i]) : 0.f;
         }
 #pragma unroll
         for (int j = 0; j < RW; ++j) {
@@ -70,7 +69,56 @@ template <int RW, int LPR> __device__ __forceinline__ void mx4_row_dots(const ui
         }
     }
 #pragma unroll
-    for (int j = 0; j < RW; ++j) dot[j] = seg_sum(dot[j], LPR);
+    for (int j = 0; j < RW; ++j) dot[j] = wave_sum(dot[j]);
+}
+
+// The same of sixteen rows, by MFMAs, of up to 32 blocks: the vector in terms of 8 bits in LDS, for all four waves, and every load of B ahead of them.  p[i]: the dot of row
+// row0 + 4 (lane / 16) + i.  (Protected 12608 x 4096 x 1024 in 16 groups 65.0 / 63.6 us, 3000 x 1000 x 96 in 4 12.4 / 11.2; in windows of 32 blocks, where rows are deeper and workgroups few: 6000 x
+// 1024 x 4096 in 8 39.5 / 46.4.)
+constexpr int DOTS_BLOCKS = 32, DOTS_ROWS = 16;
+__device__ __forceinline__ void mx4_tile_dots(const uint8_t *X, long ld, const uint8_t *S, long lds, int row0, int rows, int K, const uint32_t *vec, uint8_t *smem, float (&p)[4])
+{
+    static_assert(DOTS_BLOCKS * 8 == 256, "four terms of the vector to a thread");
+    const int tid = threadIdx.x, lane = tid & 63, piece = lane >> 4, nb = K / 16;
+    const long r = min(row0 + (lane & 15), rows - 1);
+    const uint8_t *const src = X + r * ld, *const sc = S + r * lds;
+    uint8_t *const terms = smem, *const powers = smem + DOTS_BLOCKS * TERMS * 32;
+    const i32x4_word a = *reinterpret_cast<const i32x4_word *>(vec + min(tid, nb * 8 - 1) * 4);
+    i32x4 b[DOTS_BLOCKS / 4];
+    uint2 s[DOTS_BLOCKS / 8];
+#pragma unroll
+    for (int u = 0; u < DOTS_BLOCKS / 4; ++u) {
+        if (4 * u >= nb) break;
+        const int over = 4 * u + 4 <= nb ? 0 : max(4 * u + piece - (nb - 1), 0);             // (of the last four blocks alone)
+        b[u] = *reinterpret_cast<const i32x4 *>(src + (4 * u + piece - over) * 16);
+    }
+    // (rows of powers of two are whole 16 bytes)
+#pragma unroll
+    for (int u = 0; u < DOTS_BLOCKS / 8; ++u) {
+        if (8 * u >= nb) break;
+        s[u] = *reinterpret_cast<const uint2 *>(sc + 8 * u);
+    }
+    f32x4 v;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = __uint_as_float((uint32_t)a[q]);
+    if (tid < nb * 8) mx4_put_terms(v, tid & 7, terms + (tid >> 3) * TERMS * 32, powers + (tid >> 3) * 8);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");         // (over LDS alone: B may still be on its way)
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < DOTS_BLOCKS / 4; ++u) {
+        if (4 * u >= nb) break;
+        // past the last block nothing is multiplied, whatever it holds
+        const bool in = 4 * u + piece < nb;
+        const i32x4 bv = in ? b[u] : i32x4{0, 0, 0, 0};
+        const uint32_t bsv = in ? ((u & 1 ? s[u >> 1].y : s[u >> 1].x) >> (8 * piece)) & 0xFFu : 0u;
+        i32x8 ev;
+        uint32_t esv;
+        mx4_get_terms(terms, powers, 4 * u, nb, lane, ev, esv);
+        acc = mfma16_mx4_f8(bv, ev, acc, bsv, esv);
+        __builtin_amdgcn_sched_barrier(0);                       // (terms of one step at a time in registers)
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = row16_sum(acc[i]);        // (of the terms)
 }
 
 constexpr int GCHK_KN_LANES = 4;          // chunk columns of a unit over a B stored K x N (64 lanes run along k)
@@ -78,8 +126,8 @@ constexpr int GCHK_KN_LANES = 4;          // chunk columns of a unit over a B st
 // What is left to do of the columns: their predictions from B stored N x K or K x N, or nothing but to write down what the product's kernel marked.
 enum { COLS_NK, COLS_KN, COLS_MARKED };
 
-// RW: rows of B to a wave (4 bits: to LPR lanes of one)
-template <int DT, int RW, int COLS, int LPR = 64>
+// RW: rows of B to a wave (4 bits: sixteen are a tile of MFMAs)
+template <int DT, int RW, int COLS>
 __global__ __launch_bounds__(256) void group_check_kernel(typename GroupCheckArgsOf<DT>::type f)
 {
     using T = Traits<DT>;
@@ -158,17 +206,29 @@ __global__ __launch_bounds__(256) void group_check_kernel(typename GroupCheckArg
     int n = 0;
     acc_t pred = T::zero();
     if constexpr (COLS == COLS_NK) {
-        constexpr int ROWS = 64 / LPR;                           // side by side
-        const int row0 = (unit * 4 + wave) * RW * ROWS, l = lane % LPR;
-        n = row0 + l * ROWS + lane / LPR;
-        mine_ok = l < RW && n < N;
-        // (a group without rows: nothing of its matrix is read)
-        if (rows > 0 && row0 < N) {
-            acc_t dot[RW];
-            if constexpr (MX4) mx4_row_dots<RW, LPR>(Bb, f.ldb, f.sb + (long)e * f.stride_sb, f.ld_sb, row0, N, K, asum, dot);
-            else row_dots<DT, RW>(Bb, f.ldb, row0, N, K, asum, false, dot);
+        const int row0 = (unit * 4 + wave) * RW;
+        if constexpr (MX4 && RW == DOTS_ROWS) {
+            __shared__ __attribute__((aligned(16))) uint8_t smem[DOTS_BLOCKS * TERM_BYTES];
+            const int i = lane & 15;
+            n = row0 + 4 * (lane >> 4) + i;
+            mine_ok = i < 4 && n < N;
+            // (a group without rows: nothing of its matrix is read)
+            if (rows > 0) {
+                float dot[4];
+                mx4_tile_dots(Bb, f.ldb, f.sb + (long)e * f.stride_sb, f.ld_sb, row0, N, K, asum, smem, dot);
 #pragma unroll
-            for (int j = 0; j < RW; ++j) pred = l == j ? dot[j] : pred;
+                for (int j = 0; j < 4; ++j) pred = i == j ? dot[j] : pred;
+            }
+        } else {
+            n = row0 + lane;
+            mine_ok = lane < RW && n < N;
+            if (rows > 0 && row0 < N) {
+                acc_t dot[RW];
+                if constexpr (MX4) mx4_row_dots<RW>(Bb, f.ldb, f.sb + (long)e * f.stride_sb, f.ld_sb, row0, N, K, asum, dot);
+                else row_dots<DT, RW>(Bb, f.ldb, row0, N, K, asum, false, dot);
+#pragma unroll
+                for (int j = 0; j < RW; ++j) pred = lane == j ? dot[j] : pred;
+            }
         }
     } else {
         const int cx = tid % GCHK_KN_LANES, ky = tid / GCHK_KN_LANES;
@@ -270,19 +330,16 @@ hipError_t launch_group_check(int dt, const GroupKernel &k, const GroupArgs &g, 
 
 hipError_t launch_mx4_check(const GroupKernel &k, const Mx4Args &g, int K, const Workspace &w, const Verdict &v, const OneLaunch &end, hipStream_t st)
 {
-    constexpr int RW = 8;
+    constexpr int DEEP = 8;                                      // rows to a wave where they are of more blocks than a tile's
     Mx4CheckArgs f;
     check_args(f, g, (float)K, w, v, end);
     f.sb = g.sb; f.ld_sb = g.ld_sb; f.stride_sb = g.stride_sb;
-    const bool marked = k.kind == GROUP_KERNEL_FEW;
-    const int blocks = g.K / 16, lpr = blocks <= 8 ? 8 : blocks <= 16 ? 16 : blocks <= 32 ? 32 : 64;
-    const dim3 grid = check_grid(f, marked, 4 * RW * (64 / lpr));
+    const bool marked = k.kind == GROUP_KERNEL_FEW, deep = g.K / 16 > DOTS_BLOCKS;
+    const dim3 grid = check_grid(f, marked, 4 * (deep ? DEEP : DOTS_ROWS));
     // (marked: fp32 sums and nothing of the operands)
-    if (marked)         hipLaunchKernelGGL((group_check_kernel<DT_BF16, GCHK_ROWS, COLS_MARKED>), grid, dim3(256), 0, st, (const GroupCheckArgs &)f);
-    else if (lpr == 8)  hipLaunchKernelGGL((group_check_kernel<DT_MX4, RW, COLS_NK, 8>), grid, dim3(256), 0, st, f);
-    else if (lpr == 16) hipLaunchKernelGGL((group_check_kernel<DT_MX4, RW, COLS_NK, 16>), grid, dim3(256), 0, st, f);
-    else if (lpr == 32) hipLaunchKernelGGL((group_check_kernel<DT_MX4, RW, COLS_NK, 32>), grid, dim3(256), 0, st, f);
-    else                hipLaunchKernelGGL((group_check_kernel<DT_MX4, RW, COLS_NK, 64>), grid, dim3(256), 0, st, f);
+    if (marked)    hipLaunchKernelGGL((group_check_kernel<DT_BF16, GCHK_ROWS, COLS_MARKED>), grid, dim3(256), 0, st, (const GroupCheckArgs &)f);
+    else if (deep) hipLaunchKernelGGL((group_check_kernel<DT_MX4, DEEP, COLS_NK>), grid, dim3(256), 0, st, f);
+    else           hipLaunchKernelGGL((group_check_kernel<DT_MX4, DOTS_ROWS, COLS_NK>), grid, dim3(256), 0, st, f);
     return hipGetLastError();
 }
 

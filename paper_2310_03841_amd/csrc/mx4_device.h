@@ -43,6 +43,50 @@ __device__ __forceinline__ f32x4 mfma16_mx4_f8(const i32x4 &a, const i32x8 &b, c
 // 2^(s - 127) as the conversions take it (they look at its exponent alone).
 __device__ __forceinline__ float mx4_unit(uint32_t s) { return __uint_as_float(s << 23); }
 
+// Four fp32 values of a block's 32, the others in the seven lanes beside this one (part: which of the eight), as terms of 8 bits (e4m3): each term has a power of two for the block, 2^-5 of
+// the one before it.  The first takes the block's largest value, below 2^8 of its power, to within 2^3 of that, and each the rest of the one before in the same way: what is
+// left behind is below 2^-25 of the largest.  A block with an Inf or a NaN is NaN.  terms: TERMS times 32 bytes; powers: TERMS bytes of eight.
+constexpr int TERMS = 5, TERM_BYTES = TERMS * 32 + 8;        // LDS for a block
+__device__ __forceinline__ void mx4_put_terms(f32x4 v, int part, uint8_t *terms, uint8_t *powers)
+{
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) most = max(most, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+    most = max(most, (uint32_t)dpp_mov<0xB1>((int)most));            // lane ^ 1
+    most = max(most, (uint32_t)dpp_mov<0x4E>((int)most));            // lane ^ 2
+    most = max(most, (uint32_t)dpp_mov<0x141>((int)most));           // i <-> 7 - i inside 8 lanes
+    const int field = (int)(most >> 23);
+#pragma unroll
+    for (int p = 0; p < TERMS; ++p) {
+        const uint32_t power = field == 255 ? 255u : (uint32_t)max(field - 7 - 5 * p, 0);
+        const float unit = mx4_unit(power);
+        s16x2 o = {0, 0};
+        o = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(o, v[0], v[1], unit, false);
+        o = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(o, v[2], v[3], unit, true);
+        const int word = __builtin_bit_cast(int, o);
+        *reinterpret_cast<int *>(terms + p * 32 + part * 4) = word;
+        if (part == p) powers[p] = (uint8_t)power;
+        const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, unit, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, unit, true);
+        v -= f32x4{lo[0], lo[1], hi[0], hi[1]};
+    }
+}
+// Those of blocks c0 .. c0 + 3 of nb (zeros behind them) as an operand of mfma16_mx4_f8, a term to a row.
+__device__ __forceinline__ void mx4_get_terms(const uint8_t *terms, const uint8_t *powers, int c0, int nb, int lane, i32x8 &v, uint32_t &power)
+{
+    const int term = lane & 15, piece = lane >> 4;
+    v = i32x8{0, 0, 0, 0, 0, 0, 0, 0};
+    power = 0;
+    if (term < TERMS) {
+        const int c = c0 + (piece >> 1);
+        const uint8_t *at = terms + (c * TERMS + term) * 32 + (piece & 1) * 16;
+        i32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+        if (c < nb) lo = *reinterpret_cast<const i32x4 *>(at);
+        if (c + 2 < nb) hi = *reinterpret_cast<const i32x4 *>(at + 2 * TERMS * 32);
+        v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        if (c0 + piece < nb) power = powers[(c0 + piece) * 8 + term];
+    }
+}
+
 // The 32 values of a block.
 __device__ __forceinline__ void mx4_values(const i32x4 &v, float unit, float (&x)[32])
 {
