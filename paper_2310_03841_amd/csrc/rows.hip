@@ -257,7 +257,8 @@ hipError_t launch_gather_rows(int es, const void *X, int tokens, int cols, long 
 // ---------------------------------------------------------------- and back to their tokens
 // 16 bytes of a row to a lane.  Sums in fp32, in the order of a token's choices, the base first.
 // Bound by memory: rows of 2 KB in any order.  12608 tokens of 1001 fp16 columns, two choices and a base: 25.5 us for 101 MB, 4.0 TB/s (a token to half a wave, four chunks to a lane,
-// 26.3); the gradient 23.5 us for 126 MB, 5.4 TB/s.
+// 26.3); the gradient 23.5 us for 126 MB, 5.4 TB/s.  Stores past the caches would take both in turn from 48.9 to 41.4, and cost a product that reads what they wrote more than that: 12608 tokens, 1024
+// columns of bf16, two choices, with a product of 768 columns behind it: combine 41.0 / 42.8, gradient 65.9 / 71.1; four choices 49.4 / 50.4 and 118.7 / 125.8.
 __device__ __forceinline__ void put_chunk(uint8_t *dst, const uint32_t (&o)[4], int n)        // n: elements of the chunk inside the row
 {
     if (n >= 8) *reinterpret_cast<i32x4 *>(dst) = i32x4{(int)o[0], (int)o[1], (int)o[2], (int)o[3]};
