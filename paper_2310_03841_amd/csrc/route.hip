@@ -4,7 +4,7 @@
 // nothing is added), equal ones by index; a round takes the best that is left.
 //
 // Bound by the latency of a token's rounds, each a maximum over its lanes and one removed, and of many tokens by their instructions; the logits are read once (12608 x 128 of fp32, 6.5 MB, 1.3 us at
-// 5 TB/s; 7.2 us, both directions back to back 11.0).
+// 5 TB/s; 7.1 us, both directions back to back 10.2).
 #include "abft_device.h"
 #include "gemm_epilogue.h"
 #include "route_args.h"
@@ -277,7 +277,8 @@ __device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL]
     }
     // rounds: the best that is left, of equal ones that of the first lane, there the first.  Its lane writes it down.
     const bool check = ROUNDED && a.bias != nullptr;                         // then one round more, for the first that is not chosen
-    const int base = (threadIdx.x & 63) & ~(LPT - 1);
+    const int lane = threadIdx.x & 63;
+    [[maybe_unused]] const uint64_t below = ((1ull << lane) - 1) & ~((1ull << (lane & ~(LPT - 1))) - 1);         // the token's lanes ahead of this one
     float my_key = 0.f;
     for (int j = 0; j < a.topk + (check ? 1 : 0); ++j) {
         order_t best = O::NONE;
@@ -285,14 +286,17 @@ __device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL]
         for (int i = 0; i < EPL; ++i) best = key[i] > best ? key[i] : best;
         const order_t own = best;
         best = over_token<LPT>(best, Larger{});
-        const uint64_t who = __ballot(own == best) >> base;                  // (of the token's lanes, and others above them)
-        const bool owner = l == (int)__builtin_ctzll(who);
-        int slot = EPL;
+        const uint64_t who = __ballot(own == best);
+        const bool owner = LPT == 64 ? l == (int)__builtin_ctzll(who) : own == best && !(who & below);
+        int slot = 0;
+        bool left = owner;                                       // (masks: scalar instructions beside the vector ones)
 #pragma unroll
-        for (int i = EPL - 1; i >= 0; --i) slot = key[i] == best ? i : slot;
-        slot = owner ? slot : EPL;
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) key[i] = slot == i ? O::NONE : key[i];
+        for (int i = 0; i < EPL; ++i) {
+            const bool here = left && key[i] == best;
+            left = left && !here;
+            key[i] = here ? O::NONE : key[i];
+            slot = here ? i : slot;
+        }
         if (owner) lds.chosen[j] = best != O::NONE ? e0 + slot : -1;
         if constexpr (ROUNDED) my_key = l == j ? O::value(best) : my_key;
     }
@@ -434,7 +438,7 @@ template <int DT, int LPT, int EPL> __global__ __launch_bounds__(256) void route
         filled += __popcll(__ballot(full));
         v[i] = full ? v[i] : 0.f;
     }
-    // fewer places than choices: some token of the wave names an expert twice.  (Additions to begin with: 11.6 us for 11.0, both directions of 12608 x 128.)
+    // fewer places than choices: some token of the wave names an expert twice.  (Additions to begin with: 11.6 us for 10.9, both directions of 12608 x 128.)
     if (__builtin_expect(filled != __popcll(__ballot(there)), 0)) {
 #pragma unroll
         for (int i = 0; i < EPL; ++i) g[e0 + i] = 0.f;
