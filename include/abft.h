@@ -304,7 +304,8 @@ typedef struct {
 } abft_routing;
 
 /* The choices: expert and weight, DEVICE, [tokens][topk].  logits: ABFT_BF16, ABFT_F16 or ABFT_F32; pointer and rows as the matrices above (16 bytes).
- * Choices are those of exact arithmetic (two keys, or values of groups, that differ by less than 2^-50 of the larger aside); weights are computed in fp32.  Where fewer
+ * Choices are those of exact arithmetic, of scores below 2^-1000 taken as zeros, and two keys, or values of groups, that differ by less than 2^-40 of the largest score or
+ * bias that went into them aside (64 bits are what is nearest); weights are computed in fp32.  Where fewer
  * than topk experts are left the rest is expert -1, weight 0, so a token whose logits are all -Inf goes to no expert.  A token with a logit that is NaN or +Inf
  * has no scores: experts 0, 1, .. and weights NaN, so that nothing made of it looks sound.  Needs no context, nor do the
  * other calls of this section but abft_group_rows; they run on the current device.  Sizes beyond those above, or tokens > 2^24: ABFT_ESHAPE. */

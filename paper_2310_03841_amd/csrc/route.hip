@@ -234,10 +234,14 @@ __device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL]
     if constexpr (GROUPED) {
         const int G = a.groups, per = E / G;
         KEY *const keys = reinterpret_cast<KEY *>(lds.keys), *const values = reinterpret_cast<KEY *>(lds.values);
+        [[maybe_unused]] float margins[ROUTE_MAX_GROUPS / LPT];                  // of the lane's groups
 #pragma unroll
         for (int i = 0; i < EPL; ++i) keys[e0 + i] = s[i];
         wave_lds_fence();
-        for (int g = l; g < G; g += LPT) {
+#pragma unroll
+        for (int n = 0; n < ROUTE_MAX_GROUPS / LPT; ++n) {
+            const int g = n * LPT + l;
+            if (g >= G) break;
             KEY b0 = -(KEY)inf, b1 = -(KEY)inf;
 #pragma unroll 8
             for (int i = 0; i < per; ++i) {
@@ -246,12 +250,20 @@ __device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL]
                 b0 = k > b0 ? k : b0;
             }
             values[g] = a.group_best == 2 && b1 > -(KEY)inf ? b0 + b1 : b0;
+            // What a value is off by at most: two scores; and, in parts of the larger key, since keys of either sign cancel in a sum, 2^-24 for each of them, 2 2^-24 for the sum
+            // and 2 2^-24 for the comparison below.
+            if constexpr (ROUNDED) {
+                const float size = fmaxf(b0 > -inf ? fabsf(b0) : 0.f, b1 > -inf ? fabsf(b1) : 0.f);
+                margins[n] = (a.sigmoid ? 0x1p-20f : 0x1p-15f * largest) + 0x1p-21f * size;
+            }
         }
         wave_lds_fence();
         uint64_t stay = 0;
         KEY in_min = (KEY)inf, out_max = -(KEY)inf;
-        for (int g0 = 0; g0 < G; g0 += LPT) {
-            const int g = g0 + l;
+#pragma unroll
+        for (int n = 0; n < ROUTE_MAX_GROUPS / LPT; ++n) {
+            const int g0 = n * LPT, g = g0 + l;
+            if (g0 >= G) break;
             int rank = 0;
             const KEY v = values[min(g, G - 1)];
 #pragma unroll 8
@@ -260,17 +272,18 @@ __device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL]
                 rank += w > v || (w == v && h < g) ? 1 : 0;
             }
             const bool in = g < G && rank < a.top_groups;
-            if (in && v < in_min) in_min = v;
-            if (g < G && !in && v > out_max) out_max = v;
+            KEY margin = 0;
+            if constexpr (ROUNDED) margin = margins[n];
+            if (in && v - margin < in_min) in_min = v - margin;
+            if (g < G && !in && v + margin > out_max) out_max = v + margin;
             const uint64_t b = __ballot(in) >> ((threadIdx.x & 63) & ~(LPT - 1));
             stay |= (LPT == 64 ? b : b & ((1ull << (LPT & 63)) - 1)) << g0;
         }
         if (ROUNDED && scored) {
             in_min = over_token<LPT>(in_min, Smaller{});
             out_max = over_token<LPT>(out_max, Larger{});
-            // two sums of two, twice over; with biases, their roundings.  (Groups without an expert are the last in any arithmetic.)
-            const float far = (a.sigmoid ? 0x1p-19f : 0x1p-14f * largest) + 0x1p-20f * fabsf((float)out_max);
-            sure = out_max == -(KEY)inf || (float)(in_min - out_max) > far;
+            // (groups without an expert are the last in any arithmetic)
+            sure = out_max == -(KEY)inf || in_min > out_max;
         }
 #pragma unroll
         for (int i = 0; i < EPL; ++i) key[i] = stay >> (min(e0 + i, E - 1) / per) & 1 ? key[i] : O::NONE;

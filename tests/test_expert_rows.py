@@ -238,6 +238,21 @@ def test_keys_next_to_each_other(score, E, tokens):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [40, 4200])
+@pytest.mark.parametrize("score", [ab.ABFT_SOFTMAX, ab.ABFT_SIGMOID])
+@pytest.mark.parametrize("E,groups,top_groups", [(8, 4, 1), (8, 4, 3), (64, 16, 5), (256, 8, 3)])
+def test_groups_whose_best_keys_cancel(score, tokens, E, groups, top_groups):
+    """Biases of either sign and far larger than the scores: a group's two best keys are rounded at the size of the biases, and their sum is that of the scores."""
+    per = E // groups
+    for size in (1e3, 1e5):
+        bias = torch.full((E,), -4 * size)
+        bias[0::per], bias[1::per] = size, -size
+        r = Route("f32", tokens, E, 2, score=score, bias=bias, groups=groups, top_groups=top_groups, best=2, seed=E)
+        r.forward()
+        r.check()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("score", [ab.ABFT_SOFTMAX, ab.ABFT_SIGMOID])
 @pytest.mark.parametrize("normalise", [True, False])
 @pytest.mark.parametrize("groups,top_groups", [(1, 1), (4, 2)])
