@@ -249,7 +249,13 @@ __device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL]
                 b1 = k > b0 ? b0 : k > b1 ? k : b1;
                 b0 = k > b0 ? k : b0;
             }
-            values[g] = a.group_best == 2 && b1 > -(KEY)inf ? b0 + b1 : b0;
+            KEY v = b0;
+            if (a.group_best == 2 && b1 > -(KEY)inf) {
+                v = b0 + b1;
+                // (two near the lowest fp32 number: still ahead of a group without an expert)
+                if constexpr (ROUNDED) v = fmaxf(v, -__FLT_MAX__);
+            }
+            values[g] = v;
             // What a value is off by at most: two scores; and, in parts of the larger key, since keys of either sign cancel in a sum, 2^-24 for each of them, 2 2^-24 for the sum
             // and 2 2^-24 for the comparison below.
             if constexpr (ROUNDED) {

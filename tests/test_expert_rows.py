@@ -253,6 +253,20 @@ def test_groups_whose_best_keys_cancel(score, tokens, E, groups, top_groups):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [5, 4200])
+@pytest.mark.parametrize("score", [ab.ABFT_SOFTMAX, ab.ABFT_SIGMOID])
+def test_biases_of_the_lowest_value_mask_no_group(score, tokens):
+    """Two keys near the lowest value add up to less than fp32 holds: such a group is still ahead of one that is masked, and behind all others."""
+    low, high = torch.finfo(torch.float32).min, torch.finfo(torch.float32).max
+    for bias, top_groups in (([-INF, -INF, low, low, 0, 0], 2), ([low, low, -INF, -INF, -INF, -INF], 1), ([low, low, low / 2, low / 2, 0, 0], 2), ([high, high, high / 2, high / 2, 0, 0], 1),
+                             ([high / 2, high / 2, high, high, 0, 0], 1), ([high, low, 0, 0, low, high], 1)):
+        for best in (1, 2):
+            r = Route("f32", tokens, 6, 2 * top_groups, score=score, bias=torch.tensor(bias), groups=3, top_groups=top_groups, best=best, seed=top_groups)
+            r.forward()
+            r.check()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("score", [ab.ABFT_SOFTMAX, ab.ABFT_SIGMOID])
 @pytest.mark.parametrize("normalise", [True, False])
 @pytest.mark.parametrize("groups,top_groups", [(1, 1), (4, 2)])
