@@ -325,10 +325,11 @@ __device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL]
         if (check) {
             const int next = l < a.topk ? lds.chosen[l + 1] : -1;
             const float next_key = __shfl_down(my_key, 1);
-            // twice what two keys are off, twice over; of a softmax by the larger of the two scores
+            // twice what two keys are off, twice over; of a softmax by the larger of the two scores.  All that are not chosen are held against the last that is, and behind the first of
+            // them there may be one of a larger score, off by more: there by the largest there can be.  (12608 x 128 with a bias 12.6 us; by the largest of those that are not chosen 14.2.)
             if (next >= 0) {
-                const float score = fmaxf(my_key - a.bias[lds.chosen[l]], next_key - a.bias[next]);
-                const float far = (a.sigmoid ? 0x1p-20f : 0x1p-15f * fabsf(score)) + 0x1p-21f * fmaxf(fabsf(my_key), fabsf(next_key));
+                const float score = l == a.topk - 1 ? largest : fabsf(fmaxf(my_key - a.bias[lds.chosen[l]], next_key - a.bias[next]));
+                const float far = (a.sigmoid ? 0x1p-20f : 0x1p-15f * score) + 0x1p-21f * fmaxf(fabsf(my_key), fabsf(next_key));
                 if (!(my_key - next_key > far)) sure = false;
             }
         }

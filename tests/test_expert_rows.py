@@ -267,6 +267,27 @@ def test_biases_of_the_lowest_value_mask_no_group(score, tokens):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [40, 4200])
+@pytest.mark.parametrize("score", [ab.ABFT_SOFTMAX, ab.ABFT_SIGMOID])
+@pytest.mark.parametrize("E,topk", [(8, 1), (40, 3), (128, 8), (200, 2)])
+def test_near_keys_of_very_different_scores(score, E, topk, tokens):
+    """Behind clear choices come three keys 2^-25 apart, of two small scores and of one near 1, whose key is off by more than theirs and may be any of the three."""
+    for seed in range(10):
+        rng = np.random.default_rng(seed)
+        base = rng.normal(size=E) * 0.8
+        big, near1, near2, *clear = rng.permutation(E)[:topk + 2]
+        base[big] += 9
+        s = 1 / (1 + np.exp(-base)) if score else np.exp(base) / np.exp(base).sum()
+        bias = np.full(E, -2.0)
+        bias[clear] = 2 + 0.5 * np.arange(topk - 1)
+        bias[near1], bias[near2], bias[big] = 0.01 - s[near1], 0.01 - s[near2] - 2e-8, 0.01 - s[big] + 6e-8 * (rng.random() - 0.5)
+        x = torch.from_numpy((base + rng.normal(size=(tokens, E)) * 1e-6).astype(np.float32))
+        r = Route("f32", tokens, E, topk, score=score, bias=torch.from_numpy(bias.astype(np.float32)), x=x)
+        r.forward()
+        r.check()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("score", [ab.ABFT_SOFTMAX, ab.ABFT_SIGMOID])
 @pytest.mark.parametrize("normalise", [True, False])
 @pytest.mark.parametrize("groups,top_groups", [(1, 1), (4, 2)])
