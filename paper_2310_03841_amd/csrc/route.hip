@@ -298,7 +298,7 @@ __device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL]
     const bool check = ROUNDED && a.bias != nullptr;                         // then one round more, for the first that is not chosen
     const int lane = threadIdx.x & 63;
     [[maybe_unused]] const uint64_t below = ((1ull << lane) - 1) & ~((1ull << (lane & ~(LPT - 1))) - 1);         // the token's lanes ahead of this one
-    float my_key = 0.f;
+    float my_key = 0.f, last_key = 0.f;
     for (int j = 0; j < a.topk + (check ? 1 : 0); ++j) {
         order_t best = O::NONE;
 #pragma unroll
@@ -317,14 +317,17 @@ __device__ __forceinline__ bool choose(const RouteArgs &a, const float (&x)[EPL]
             slot = here ? i : slot;
         }
         if (owner) lds.chosen[j] = best != O::NONE ? e0 + slot : -1;
-        if constexpr (ROUNDED) my_key = l == j ? O::value(best) : my_key;
+        if constexpr (ROUNDED) {
+            last_key = O::value(best);
+            my_key = l == j ? last_key : my_key;
+        }
     }
     wave_lds_fence();
     *mine = l < a.topk ? lds.chosen[l] : -1;
     if constexpr (ROUNDED) {
         if (check) {
             const int next = l < a.topk ? lds.chosen[l + 1] : -1;
-            const float next_key = __shfl_down(my_key, 1);
+            const float down = __shfl_down(my_key, 1), next_key = l == a.topk - 1 ? last_key : down;             // (no lane keeps the key of round 64)
             // twice what two keys are off, twice over; of a softmax by the larger of the two scores.  All that are not chosen are held against the last that is, and behind the first of
             // them there may be one of a larger score, off by more: there by the largest there can be.  (12608 x 128 with a bias 12.6 us; by the largest of those that are not chosen 14.2.)
             if (next >= 0) {
