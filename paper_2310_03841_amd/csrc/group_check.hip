@@ -361,9 +361,10 @@ __global__ __launch_bounds__(64 * ENCODE_WAVES) void mx4_encode_kernel(Mx4Encode
     __shared__ float part[W][4 * 32], tops[W];
     fetch_args<Mx4EncodeArgs>();
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const size_t wg = (size_t)blockIdx.y * gridDim.x + blockIdx.x, wgs = (size_t)gridDim.x * gridDim.y;
+    const unsigned column = blockIdx.z * gridDim.x + blockIdx.x;         // four blocks of K each
+    const size_t wg = ((size_t)blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x, wgs = (size_t)gridDim.x * gridDim.y * gridDim.z;
     for (size_t i = wg * THREADS + tid; i < a.zero_words; i += wgs * THREADS) a.zero[i] = 0u;
-    const int e = blockIdx.y, nb = a.K / 16, block = blockIdx.x * 4 + (tid & 3), at = min(block, nb - 1);
+    const int e = blockIdx.y, nb = a.K / 16, block = column * 4 + (tid & 3), at = min(block, nb - 1);
     const uint8_t *src = a.B + (long)e * a.sB + at * 16, *sc = a.sb + (long)e * a.stride_sb + at;
     float sum[32], top = 0.f;
 #pragma unroll
@@ -401,11 +402,11 @@ __global__ __launch_bounds__(64 * ENCODE_WAVES) void mx4_encode_kernel(Mx4Encode
     top = wave_max(block < nb ? top : 0.f);
     if (lane == 0) tops[wave] = top;
     __syncthreads();
-    if (tid < 128 && blockIdx.x * 4 + (tid >> 5) < (unsigned)nb) {
+    if (tid < 128 && column * 4 + (tid >> 5) < (unsigned)nb) {
         float t = 0.f;
 #pragma unroll
         for (int w = 0; w < W; ++w) t += part[w][tid];
-        a.b_sum[(long)e * 2 * a.K + blockIdx.x * 128 + tid] = __float_as_uint(t);
+        a.b_sum[(long)e * 2 * a.K + (long)column * 128 + tid] = __float_as_uint(t);
     }
     if (tid == 0) {
         float m = 0.f;
@@ -418,7 +419,10 @@ __global__ __launch_bounds__(64 * ENCODE_WAVES) void mx4_encode_kernel(Mx4Encode
 hipError_t launch_mx4_encode(const Mx4Args &g, const Workspace &w, uint32_t *zero, size_t zero_words, hipStream_t st)
 {
     const Mx4EncodeArgs a = {g.B, g.sb, g.N, g.K, g.ldb, g.sB, g.ld_sb, g.stride_sb, w.b_sum, w.b_max, zero, zero_words};
-    hipLaunchKernelGGL(mx4_encode_kernel, dim3((unsigned)((g.K / 16 + 3) / 4), (unsigned)g.groups), dim3(64 * ENCODE_WAVES), 0, st, a);
+    // (up to 2^22 workgroups of 2^10 threads along K, which is more than one direction of a launch has)
+    constexpr unsigned X = 1u << 21;
+    const unsigned wgs = (unsigned)((g.K / 16 + 3) / 4);
+    hipLaunchKernelGGL(mx4_encode_kernel, dim3(wgs < X ? wgs : X, (unsigned)g.groups, (wgs + X - 1) / X), dim3(64 * ENCODE_WAVES), 0, st, a);
     return hipGetLastError();
 }
 

@@ -427,6 +427,31 @@ def test_scales_at_the_ends_of_their_range():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("K", [1 << 29, (1 << 29) - 128])
+def test_the_greatest_depth(K):
+    """One row of A, of ones in some of its blocks and zeros else, and one of B, of ones: sums of small whole numbers, exact in fp32, and a tolerance below one block's."""
+    nb = K // 32
+    A, B = torch.zeros(1, K // 2, dtype=torch.uint8, device="cuda"), torch.full((1, K // 2), 0x22, dtype=torch.uint8, device="cuda")
+    sA, sB = (torch.full((1, up(nb, 16)), 127, dtype=torch.uint8, device="cuda") for _ in range(2))
+    blocks = torch.cat([torch.tensor([0, nb - 1]), torch.randint(0, nb, (998,), generator=torch.Generator().manual_seed(1))]).unique().cuda()
+    A.view(nb, 16)[blocks] = 0x22
+    C, flags = torch.zeros(1, 8, dtype=torch.bfloat16, device="cuda"), [torch.full((n,), 9, dtype=t, device="cuda") for n, t in ((1, torch.uint8), (1, torch.uint8), (8, torch.int32))]
+    ctx = ab.abft_create(1, 1, K, 1)
+    try:
+        shape, q = ab.make_shape(1, 1, K, lda=K, ldb=K, ldc=8), ab.make_mx4(sA, sA.shape[1], sB, sB.shape[1])
+        ok(ab.abft_gemm_mx4(ctx, A, B, None, q, C, ab.ABFT_DETECT, shape, ab.make_result(*flags, tau=16.0)))
+        assert float(C[0, 0]) == float(torch.tensor(32.0 * blocks.numel()).to(torch.bfloat16)) and int(torch.count_nonzero(C[0, 1:])) == 0
+        assert flags[2].tolist()[:3] == [0, 0, 0] and int(flags[0]) == 0 and int(flags[1]) == 0
+        # every block of the encoding: an element of A that meets one wrong there is found
+        B.view(nb, 16)[int(blocks[-2]), 3] = 0x77
+        ok(ab.abft_gemm_mx4(ctx, A, B, None, q, C, ab.ABFT_DETECT | ab.ABFT_B_CHECKSUM_CACHED, shape, ab.make_result(*flags, tau=8.0)))
+        assert int(flags[0]) == 1
+    finally:
+        torch.cuda.synchronize()
+        ab.abft_destroy(ctx)
+
+
+@pytest.mark.gpu
 def test_tolerances_of_the_caller():
     """A flip of the highest bit of a sum's mantissa changes it by d, half of the power of two it begins with: tolerances below and above d, for rows and for columns.  (The sums
     themselves are off by some K 2^-24 of their magnitudes, far below a largest sum's d.)"""
