@@ -370,7 +370,10 @@ typedef struct {
 /* C = A B + bias for such A (M x K) and B (N x K, transB = 1), sums in fp32, the bias added in fp32, rounded once.  lda, ldb and strideB of the shape count elements.  offsets: the
  * rows of A and C sorted by group, exactly as in abft_gemm_grouped, or NULL with batch = 1.  mode: ABFT_OFF or ABFT_DETECT, which may be OR-ed with
  * ABFT_B_CHECKSUM_CACHED (behind abft_encode_mx4 or an earlier protected call, with the same B and shape).  What is checked are the sums ahead of the bias, group by group,
- * as in abft_gemm_grouped for floating point: tolerance 1e-3 K max|A| max|B| of the values (scales included), or abft_result's.  What may follow the
+ * as in abft_gemm_grouped for floating point: tolerance 1e-3 K max|A| max|B| of the values (scales included), or abft_result's.  The checks are fp32 sums of those values, and
+ * scales reach further than they do: they hold while max|A|, max|B| and their product are 1000 n 2^-126 or more, and n max|A|, n max|B| and n K max|A| max|B| below 2^127 (n: the
+ * larger of N and the group's rows); beyond that a clean call may be flagged and a wrong one not.  A NaN in a row of A flags that row and all columns of its group, one in a column of B
+ * that column and all rows.  What may follow the
  * call, the context's limits and those of the shape (K <= 2^29) are also as there; an accumulator flip is armed with the same shape as ABFT_BF16.
  * Gradients: of A by abft_gemm_grouped on the dequantised B, of B by abft_gemm_grouped_wgrad. */
 int abft_gemm_mx4(abft_ctx *ctx, const void *A, const void *B, const int32_t *offsets, const abft_mx4 *q, void *C, int mode, const abft_shape *s,

@@ -412,6 +412,56 @@ def test_blocks_of_nan_stay_in_their_rows_and_columns(ends, N, K):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("ends,N,K", list(KERNELS.values()) + [WIDE, DEEP])
+def test_a_nan_flags_its_own_and_all_that_meet_it_in_a_sum(ends, N, K):
+    """A row of A that is NaN makes the sums of all columns of its group NaN, and no row but itself; a column of B those of all rows of its group."""
+    p = Product(ends, N, K, M=ends[-1] + 2, seed=K)
+    try:
+        sizes = np.diff(ends)
+        for g in np.flatnonzero(sizes)[[0, -1]]:
+            r, c = int(ends[g] + sizes[g] // 2), int(g * N + N // 3)
+            for which, at, rows, cols in ((p.sA, (r, K // 64), [r], list(range(g * N, g * N + N))), (p.sB, (c, (K - 1) // 32), list(range(ends[g], ends[g + 1])), [c])):
+                kept, which[at] = which[at], 255
+                p.upload()
+                p.run(ab.ABFT_DETECT)
+                p.check(clean=False)
+                assert np.flatnonzero(p.row_flag.cpu().numpy()[:ends[-1]]).tolist() == rows
+                assert np.flatnonzero(p.col_flag.cpu().numpy()).tolist() == cols
+                which[at] = kept
+        p.upload()
+        p.run(ab.ABFT_DETECT)
+        p.check()
+    finally:
+        p.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("a,b", [(127, 127), (18, 245), (245, 18), (245, 110), (110, 245), (181, 181), (80, 80), (74, 74), (30, 140), (140, 30)])
+@pytest.mark.parametrize("rows", [4, 70])
+def test_checks_over_the_scales_that_they_hold_for(rows, a, b):
+    """With 96 columns of depth and sums of up to 72: max|A| = 6 2^(a-127), their product and max|B| are at least 72000 2^-126, sums of either at most 72 times that, and predictions 72 96 36
+    2^(a+b-254), stay below 2^127.  Clean calls are clean and a flip of an exponent is found."""
+    N, K = 72, 96
+    big = 6 * 2.0 ** (max(a, b) - 127), 36 * 2.0 ** (a + b - 254)
+    assert 72 * big[0] < 2.0 ** 127 and K * N * big[1] < 2.0 ** 127 and min(6 * 2.0 ** (min(a, b) - 127), big[1]) >= 72000 * 2.0 ** -126
+    p = Product([0, rows], N, K, seed=a)
+    try:
+        p.sA[:, :3], p.sB[:, :3] = a, b
+        p.upload()
+        p.run(ab.ABFT_DETECT)
+        p.check()
+        c = p.want()[0]
+        i, j = np.unravel_index(np.abs(c).argmax(), c.shape)
+        # (the flip makes the largest sum four times or a fourth of what it was: a change by three quarters of it at least, many times the tolerance of 0.096 max|A| max|B|)
+        assert 0.75 * np.abs(c).max() > 4 * 0.096 * 36 * 2.0 ** (a + b - 254)
+        ok(ab.abft_inject(p.ctx, None, ab.ABFT_BF16, p.shape, 0, int(i), int(j), 24, ab.ABFT_INJECT_ACCUMULATOR))
+        p.run(ab.ABFT_DETECT)
+        assert np.flatnonzero(p.row_flag.cpu().numpy()).tolist() == [i] and np.flatnonzero(p.col_flag.cpu().numpy()).tolist() == [j]
+    finally:
+        p.close()
+
+
+@pytest.mark.gpu
 def test_scales_at_the_ends_of_their_range():
     """Powers of two from 2^-127 to 2^127."""
     for a, b in ((0, 254), (254, 0), (254, 1), (127, 127), (190, 190), (64, 64), (100, 100), (183, 183), (253, 110)):
