@@ -523,6 +523,23 @@ def test_gather_rows(dtype, tokens, topk, cols):
     assert torch.equal(y.cpu(), want)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,tokens,topk,cols", [("bf16", 9000, 8, 513), ("f16", 20000, 4, 509), ("i8", 24000, 4, 1021), ("bf16", 8300, 4, 1024), ("bf16", 4000, 5, 1801), ("i8", 9000, 3, 4099)])
+def test_gather_of_many_rows(dtype, tokens, topk, cols):
+    """More than 64 MB of rows of more than 512 bytes, which go past the caches."""
+    n, es = tokens * topk, 1 if dtype == "i8" else 2
+    assert n * cols * es > 64 << 20
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    x = torch.randint(-2 ** 7, 2 ** 7, (tokens, pad(cols, es)), generator=gen, device="cuda").to(TORCH[dtype])
+    order = torch.randperm(n, generator=gen, device="cuda").to(torch.int32)
+    order[::101], order[5], order[n - 1] = -1, n, 2 ** 31 - 1
+    y = torch.full((n + 2, pad(cols, es) + 32), 77, dtype=TORCH[dtype], device="cuda")
+    ok(ab.abft_gather_rows(x, ab.DTYPE_CODE[dtype], tokens, cols, x.shape[1], order, n, topk, y, y.shape[1]))
+    inside = (order >= 0) & (order < n)
+    want = torch.where(inside[:, None], x[torch.where(inside, order, 0).long() // topk, :cols], torch.tensor(77, dtype=TORCH[dtype], device="cuda"))
+    assert torch.equal(y[:n, :cols], want) and torch.all(y[:, cols:] == 77) and torch.all(y[n:] == 77)
+
+
 class Combine:
     def __init__(self, dtype, tokens, topk, cols, base=True, weight=True, seed=0, drop=True):
         gen = torch.Generator().manual_seed(seed)
@@ -593,6 +610,17 @@ def test_combine_rows_and_gradient(dtype, tokens, topk, cols):
         p.forward()
         p.backward()
         p.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens,topk,cols", [(9, 3, 1025), (5, 2, 1541), (4, 2, 2048), (7, 3, 2049), (5, 4, 3001), (3, 2, 4096), (3, 2, 4097), (2048, 2, 513), (2049, 1, 1024), (2051, 3, 1033), (2048, 2, 2056)])
+def test_combine_of_wide_rows(dtype, tokens, topk, cols):
+    """Each number of chunks that a lane holds, at both of its ends; and tokens enough for two chunks to a lane."""
+    p = Combine(dtype, tokens, topk, cols, seed=cols + topk)
+    p.forward()
+    p.backward()
+    p.check()
 
 
 @pytest.mark.gpu

@@ -330,6 +330,17 @@ def test_each_kernel(out, ends, N, K):
         p.close()
 
 
+# 32 columns: one piece of 512 bytes to a wave and fewer workgroups than 64 columns ask for (protected); four pieces, and more than those in turn
+FEW = [([0, 2, 2, 22, 24] + list(range(25, 61)), 600, 264), ([0] + [17 * i + 4 for i in range(1, 9)], 1030, 2100), ([0] + [17 * i + 4 for i in range(1, 9)], 1030, 4480)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ends,N,K", FEW)
+def test_each_kernel_of_few_rows(ends, N, K):
+    assert tile_of(ends, N, K, ab.ABFT_DETECT) == (16, 32) and (K < 512 or tile_of(ends, N, K, ab.ABFT_OFF) == (16, 32))
+    test_each_kernel("bf16", ends, N, K)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("spread", [3, 40])
 @pytest.mark.parametrize("ends,N,K", [([0, 1], 40, 31), ([0, 5, 16], 100, 520), ([0, 3, 24, 40], 70, 1300), ([0, 2], 16, 9000), WIDE, KERNELS[16, 32]])
