@@ -130,7 +130,7 @@ __device__ __forceinline__ void fast_tile(const GemmArgs &g, SRC source, uint8_t
         constexpr int q = decltype(q_c)::value;
         const lds_ptr dst = lds + ((L::ring3(q) ? to.f : to.r) + wave * 8 * SLAB_BYTES) + L::at(q);
         int at = s * (L::is_a(q) ? a_step : b_step);
-        // (4 bits: slabs past the last one lie past the descriptor's end, and cost no memory)
+        // (4 bits: slabs past the last one begin at the descriptor's end, and cost no memory)
         if constexpr (DT == DT_MX4) at = s < nslab ? at : 0x7FFFFFFF;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(L::is_a(q) ? a_src : b_src, (lds_void)dst, 16, off[q], at, 0, 0);
     };
@@ -140,16 +140,16 @@ __device__ __forceinline__ void fast_tile(const GemmArgs &g, SRC source, uint8_t
     constexpr bool MX4 = DT == DT_MX4;
     constexpr int SCALE_LOADS = MX4 ? 2 : 0;
     [[maybe_unused]] uint32_t sa[2][MX4 ? MI : 1], sb[2][MX4 ? NI : 1];
-    [[maybe_unused]] int sa_off, sb_off;
+    [[maybe_unused]] int sa_off, sb_off, sa_end, sb_end;
     [[maybe_unused]] __amdgpu_buffer_rsrc_t sa_src, sb_src;
     typedef const __attribute__((address_space(3))) uint32_t *lds_word;
     constexpr int SCALES_AT = fast_ring_bytes<DT, MODE>();
     auto scale_load = [&](int s) __attribute__((always_inline)) {
         if constexpr (MX4) {
             const lds_ptr dst = lds + (SCALES_AT + (s & 1) * FAST_SCALES + wave * 256);
-            const int at = s < nslab ? s * 8 : 0x7FFFFFFF;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(sa_src, (lds_void)dst, 4, sa_off, at, 0, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(sb_src, (lds_void)(dst + FAST_SCALES / 2), 4, sb_off, at, 0, 0);
+            // (past the last slab at the descriptor's end, not behind it: an offset is held against what the end leaves of that)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(sa_src, (lds_void)dst, 4, sa_off, s < nslab ? s * 8 : sa_end, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(sb_src, (lds_void)(dst + FAST_SCALES / 2), 4, sb_off, s < nslab ? s * 8 : sb_end, 0, 0);
         }
     };
     auto scale_read = [&](auto h_c, int s) __attribute__((always_inline)) {
@@ -175,8 +175,10 @@ __device__ __forceinline__ void fast_tile(const GemmArgs &g, SRC source, uint8_t
     if constexpr (MX4) {
         const auto rows = source.scale_rows(m0, n0);
         // (rows past the end bring zeros)
-        sa_src = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(rows.a), 0, min(M - m0, BM) * rows.lda, RSRC_FLAGS);
-        sb_src = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(rows.b), 0, min(N - n0, 256) * rows.ldb, RSRC_FLAGS);
+        sa_end = min(M - m0, BM) * rows.lda;
+        sb_end = min(N - n0, 256) * rows.ldb;
+        sa_src = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(rows.a), 0, sa_end, RSRC_FLAGS);
+        sb_src = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(rows.b), 0, sb_end, RSRC_FLAGS);
         sa_off = (wave * 32 + (lane >> 1)) * rows.lda + 4 * (lane & 1);
         sb_off = (wave * 32 + (lane >> 1)) * rows.ldb + 4 * (lane & 1);
     }
