@@ -1,4 +1,4 @@
-// Products over groups of few rows of 4-bit operands (single tokens, a few to an expert): sixteen rows of a group and 16 or 32 columns to a workgroup, as
+// Products over groups of few rows of 4-bit operands (single tokens, a few to an expert): sixteen rows of a group and 16, 32 or, protected, 64 columns to a workgroup, as
 // gemm_group_few.hip has it for other types.
 //
 // What bounds these products is reading the groups' matrices, once, or, where those are small, the chain of latencies of a call.  The four waves share out K, 128

@@ -73,8 +73,8 @@ template <int RW> __device__ __forceinline__ void mx4_row_dots(const uint8_t *X,
 }
 
 // The same of sixteen rows, by MFMAs, of up to 32 blocks: the vector in terms of 8 bits in LDS, for all four waves, and every load of B ahead of them.  p[i]: the dot of row
-// row0 + 4 (lane / 16) + i.  (Protected 12608 x 4096 x 1024 in 16 groups 65.0 / 63.6 us, 3000 x 1000 x 96 in 4 12.4 / 11.2; in windows of 32 blocks, where rows are deeper and workgroups few: 6000 x
-// 1024 x 4096 in 8 39.5 / 46.4.)
+// row0 + 4 (lane / 16) + i.  (By vector instructions / so, us: 16 groups of 4096 x 1024, the kernel 11.0 / 9.5; the protected call of 3000 x 1000 x 96 in 4 12.4 / 11.2; in windows of 32 blocks, where rows are
+// deeper and workgroups few, that of 6000 x 1024 x 4096 in 8 39.5 / 46.4.)
 constexpr int DOTS_BLOCKS = 32, DOTS_ROWS = 16;
 __device__ __forceinline__ void mx4_tile_dots(const uint8_t *X, long ld, const uint8_t *S, long lds, int row0, int rows, int K, const uint32_t *vec, uint8_t *smem, float (&p)[4])
 {

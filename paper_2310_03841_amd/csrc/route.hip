@@ -4,7 +4,7 @@
 // nothing is added), equal ones by index; a round takes the best that is left.
 //
 // Bound by the latency of a token's rounds, each a maximum over its lanes and one removed, and of many tokens by their instructions; the logits are read once (12608 x 128 of fp32, 6.5 MB, 1.3 us at
-// 5 TB/s; 7.1 us, both directions back to back 10.2).
+// 5 TB/s; 7.0 us, both directions back to back 10.1).
 #include "abft_device.h"
 #include "gemm_epilogue.h"
 #include "route_args.h"
@@ -495,9 +495,9 @@ template <int DT, int LPT, int EPL> static hipError_t launch_grad(const RouteArg
 }
 template <int DT> static hipError_t launch_type(const RouteArgs &a, hipStream_t st)
 {
-    // Many tokens of few experts: sixteen lanes to a token, four of which share a wave's instructions.  Else a wave, with shorter lists in its lanes.  (us, 8 choices, sixteen lanes / a wave: softmax,
-    // 12608 tokens 64 experts in 8 groups 9.7 / 14.8, 128 experts 6.2 / 9.5, 256 in 8 groups 22.6 / 22.8; sigmoid with bias, 12608 x 256 28.1 / 24.4, 4096 x 64 8.6 / 8.2, 4096 x 128 9.5 / 6.7,
-    // 2048 x 256 20.0 / 11.0; a second look in 64 bits by a few tokens is in those of the bias.)
+    // Many tokens of few experts: sixteen lanes to a token, four of which share a wave's instructions.  Else a wave, with shorter lists in its lanes.  (us in a graph, fp32, 8 choices, sixteen lanes /
+    // a wave: softmax, 12608 tokens 64 experts in 8 groups 9.8 / 14.6, 128 experts 5.8 / 9.2, 256 in 8 groups 22.3 / 21.6, 6000 x 64 3.8 / 5.1, 4096 x 64 3.6 / 4.1; sigmoid with bias, 12608 x 256
+    // 20.9 / 14.6, 6000 x 128 11.0 / 7.7, 4096 x 64 4.5 / 4.6, 4096 x 128 9.9 / 7.0, 2048 x 256 15.9 / 7.7; a second look in 64 bits by a few tokens is in those of the bias, four to a wave.)
     if (a.experts <= 128 && a.topk < 16 && a.tokens > 4096) {
         if (a.experts <= 32)  return launch_one<DT, 16, 2>(a, st);
         if (a.experts <= 64)  return launch_one<DT, 16, 4>(a, st);

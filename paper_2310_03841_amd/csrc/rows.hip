@@ -11,7 +11,7 @@ namespace abft {
 // the group's number, so that nothing is counted with atomics and the order is the entries' own.  Of more entries than one workgroup's, a first kernel counts
 // each workgroup's groups, and every workgroup adds up those ahead of it.
 // Bound by latency: one workgroup for a call's few entries, of no more waves than they and the groups need (64 entries, 32 groups: sixteen waves 4.1 us, one 2.2).  50432 entries, 64 groups:
-// 4096 of them to a workgroup and one thread to a group's counts in all workgroups 4.6 + 6.2 us; 1024, and the threads sharing out the counts, 3.4 + 4.8.
+// 4096 of them to a workgroup and one thread to a group's counts in all workgroups 4.6 + 6.2 us; 1024, and the threads sharing out the counts, 3.4 + 4.8 (behind other kernels 4.6 + 4.9).
 constexpr int ROWS_MOST = 1024;                              // threads
 
 struct GroupRowsArgs {
@@ -199,10 +199,11 @@ struct GatherArgs {
 };
 
 // Rows of more bytes than this go past the caches.  (On their way / so, us, 1024 columns of bf16: 12608 tokens to 4 experts each, 103 MB, 38.8 / 37.3, with the product of 768
-// columns that reads them 131.5 / 125.3, of 128 75.7 / 73.5; 3152 tokens, 26 MB, 15.4 / 15.2, with the product 49.3 / 51.5.)
+// columns that reads them 131.5 / 125.3, of 128 75.7 / 73.5; 3152 tokens, 26 MB, 15.4 / 15.2, with the product 49.3 / 51.5.)  Rows of up to 512 bytes do not: 128 columns, 100000 tokens to 4 experts
+// each, 30.4 / 29.6, with a product of 256 columns 152 / 169; 64 columns, 200000 tokens, 30.5 / 29.8 and 238 / 255.  (From 256 columns on they gain: 60000 tokens 35.9 / 35.0 and 97.8 / 92.8.)
 constexpr long FAR_BYTES = 64L << 20;
 
-// Bound by memory: a row read by each of its copies and written once, 205 MB at 6.2 TB/s there.  (Tokens dealt out to the XCDs, so that their copies meet in one L2: 48 us of the kernel
+// Bound by memory: 103 MB written and, for four copies on eight L2s, 93 read of 26 that there are, 6.6 TB/s in 29.7 us (4.3 of the 129 that have to move).  (Tokens dealt out to the XCDs, so that their copies meet in one L2: 48 us of the kernel
 // alone for 29.)
 // Chunk c of a row of so many bytes
 template <bool FAR> __device__ __forceinline__ void put_bytes(uint8_t *dst, const i32x4 &v, int c, int bytes)
@@ -401,6 +402,8 @@ template <int DT> static hipError_t launch_combine_type(bool grad, const Combine
         if (nch <= 8)  return launch_combine_one<DT, 8, 1>(a, st);
         if (nch <= 16) return launch_combine_one<DT, 16, 1>(a, st);
         if (nch <= 32) return launch_combine_one<DT, 32, 1>(a, st);
+        // two chunks to a lane once there are waves enough: one / two, us, 1024 columns, 1024 tokens of 8 choices 4.9 / 5.5, 2048 7.4 / 7.7, 12608 of 2 13.4 / 12.7; 4096 columns, 2048 tokens of 2
+        // 9.3 / 9.0, 4096 16.2 / 16.5
         if (nch <= 64 || a.tokens < 2048) return launch_combine_one<DT, 64, 1>(a, st);
         return launch_combine_one<DT, 64, 2>(a, st);
     }
